@@ -44,6 +44,7 @@ extern "C" {
 #define JX_U8 0  /* uint8, distances accumulated exactly in int32 */
 #define JX_F32 1 /* float32 */
 #define JX_F16 2 /* IEEE binary16 storage of float data (App. D); distances accumulated in float32 */
+#define JX_BF16 3 /* bfloat16: the attention entry points only */
 
 /* search modes */
 #define JX_EXACT 0  /* distances on the stored full-precision vectors */
@@ -108,6 +109,8 @@ extern "C" {
 #define JX_MAX_L 512    /* largest beam width L / L_build */
 #define JX_MAX_R 256    /* largest out-degree R */
 #define JX_MAX_BF_K 128 /* largest k of jx_bruteforce */
+#define JX_MAX_REQUESTS 8192 /* requests of one jx_kv_plan / jx_kv_release call */
+#define JX_MAX_HEAD_DIM 256 /* elements of an attention head */
 #define JX_STATIC_SCRATCH_BYTES (16 << 20) /* device scratch of jx_bruteforce_static, held per GPU for the life of the process */
 
 typedef struct jx_index jx_index; /* opaque, host side */
@@ -386,6 +389,159 @@ int jx_import_codes(jx_index* idx, int32_t bits, const float* d_rotation, const 
 int jx_rotate(jx_index* idx, const float* d_in, int64_t n, float* d_out, void* stream);
 int jx_rotate_points(jx_index* idx, const void* d_in, int64_t n, float* d_out, void* stream);
 int jx_encode_rotated(jx_index* idx, const float* d_rot, int64_t n, uint8_t* d_codes, float* d_meta, void* stream);
+
+/*
+ * ---- Attention beside the index --------------------------------------------
+ *
+ * For a program that serves a language model and lets it attend to a long past
+ * through an index: the recent tokens of each request lie in a paged cache of
+ * keys and values, the keys of the past in an index (inner products as
+ * distances: jx_mips_augment), and a step of new tokens is
+ *   jx_kv_plan          pages, positions and slots of the new tokens
+ *   jx_qk_norm_rope     queries and keys normalised and rotated, keys and
+ *                       values stored in their slots
+ *   jx_paged_attention  attention over the paged cache
+ *   jx_search           the nearest old keys of every query head
+ *   jx_found_attention  attention over what was found, joined with the first
+ * Each is of use without the others.  These calls need no index.  Types are
+ * JX_F16 and JX_BF16; products and sums are in float32 and rounded once to the
+ * type of the outputs, except that jx_paged_attention rounds the weights of
+ * the values to that type before their product with the values.
+ *
+ * Rows and caches: elements of a head are contiguous; strides are in elements
+ * and may be anything that keeps each head's row on a 16-byte boundary (head
+ * dimensions are multiples of 8, at most JX_MAX_HEAD_DIM).  Outputs are
+ * contiguous [n_tokens][n_heads][head_dim].  Query head h reads key head
+ * h / (n_heads / n_kv_heads).  Outputs may not overlap inputs where nothing
+ * else is said.
+ */
+typedef struct {
+    void* d_k;            /* keys:   page p, token i, head h at d_k + p * page_stride + i * token_stride + h * head_stride */
+    void* d_v;            /* values, laid out alike */
+    int64_t page_stride, token_stride, head_stride;
+    int32_t page;         /* tokens of a page: a power of two, at most 4096 */
+    int32_t n_pages;
+} jx_kv_cache;
+
+/*
+ * Pages, positions and slots of the new tokens of a step.  Request r (of n_req)
+ * has d_len[r] tokens in the cache and brings d_new[r] (negative values count
+ * as 0).  d_table [n_req][table_pages]: the pages of every request in the order
+ * of their tokens.  d_free [n_pages]: the free pages, *d_n_free of them, taken
+ * from the end.  Every request gets the pages that its last one has no room for,
+ *   table[r][a_r + i] = free[n_free - 1 - (s_r + i)],  a_r = ceil(len_r / page),
+ * s_r = what the requests before r asked for.  There is no room for a request
+ * that asks for pages where s_r and its own exceed n_free, whose tokens exceed
+ * table_pages pages, or whose rows exceed n_tokens; its tokens get no slots
+ * and its row stays as it was.
+ * Outputs: d_q_start [n_req + 1], the first row of each request (sums of d_new,
+ * at most n_tokens); d_kv_len [n_req] = len + new, or 0 where there was no room;
+ * d_pos, d_slot [n_tokens]: position and slot (page * tokens of a page + place
+ * in it) of every row, -1 where there was no room, in rows beyond the last
+ * request, and (d_slot alone) where the table names no page; *d_n_free_out, how
+ * many pages are left (not the same address as d_n_free).
+ * n_req <= JX_MAX_REQUESTS.  The call only enqueues; nothing is read back.
+ */
+int jx_kv_plan(const int32_t* d_len, const int32_t* d_new, int32_t n_req, int32_t page, int32_t* d_table, int32_t table_pages,
+               const int32_t* d_free, const int32_t* d_n_free, int32_t n_pages, int32_t* d_n_free_out, int32_t* d_q_start,
+               int32_t* d_kv_len, int32_t* d_pos, int64_t* d_slot, int64_t n_tokens, void* stream);
+
+/* Gives pages back: entries d_first[r] .. d_end[r] - 1 of row r (a finished
+ * request: 0 .. table_pages; tokens that have left a window or moved into an
+ * index: the pages in front).  Entries that name a page go to the end of the
+ * free pages, in the order of requests and entries, and become JX_NONE; the
+ * attention calls pass over such entries.  *d_n_free is updated in place. */
+int jx_kv_release(const int32_t* d_first, const int32_t* d_end, int32_t n_req, int32_t* d_table, int32_t table_pages,
+                  int32_t* d_free, int32_t* d_n_free, int32_t n_pages, void* stream);
+
+/*
+ * Queries and keys of new tokens made ready, and keys and values stored.
+ * For each head's row x of q and k: y = x / sqrt(mean(x^2) + eps) * weight
+ * (d_q_weight / d_k_weight [head_dim] of the same type; NULL: y = x), then the
+ * first rot_dim elements turned in pairs by the angle of the token's position,
+ *   (a, b) -> (a cos - b sin, b cos + a sin),
+ * pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved, cosines and
+ * sines from d_cos, d_sin [n_pos][rot_dim / 2] (float32).  rot_dim: a multiple
+ * of 16, 0 = none.  Queries go to d_q_out (may be d_q itself if that is
+ * contiguous), keys and values (unchanged) to their slots in the cache (slots as
+ * jx_kv_plan gives them; no two rows may have the same).  A token whose position is outside
+ * [0, n_pos) gets zeros as its queries and is not stored, one whose slot is
+ * outside the cache is not stored.
+ */
+typedef struct {
+    int32_t dtype, n_heads, n_kv_heads, head_dim, rot_dim, interleaved;
+    int64_t n_tokens, n_pos;
+    const void *d_q, *d_k, *d_v;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const void *d_q_weight, *d_k_weight;
+    float eps;
+    const float *d_cos, *d_sin;
+    const int32_t* d_pos;  /* [n_tokens] */
+    const int64_t* d_slot; /* [n_tokens] */
+    void* d_q_out;
+    jx_kv_cache cache;
+} jx_rope_args;
+int jx_qk_norm_rope(const jx_rope_args* args, void* stream);
+
+/*
+ * Attention of new tokens over a paged cache.  Rows d_q_start[r] .. d_q_start[r + 1]
+ * - 1 of q are the last tokens of request r, which has d_kv_len[r] tokens in the
+ * cache, those included (jx_qk_norm_rope has stored them): row i of n stands at
+ * position p = kv_len - n + i and sees positions 0 .. p, with window > 0 the
+ * last `window` of them, without those whose page the table does not name (an
+ * entry outside [0, n_pages), or beyond table_pages).
+ *   out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j),  lse = log sum_j w_j
+ * A row that sees nothing, and a row of no request, gets zeros and -infinity.
+ * What is in the cache where a row does not look has no part in its result.
+ * d_lse [n_tokens][n_heads] (float32) may be NULL.  The lengths are read on the
+ * device only.  d_work: jx_paged_attention_bytes(args) bytes of device memory
+ * (may be NULL if that is 0), 256-byte aligned, free again when the call's work
+ * is done.
+ */
+typedef struct {
+    int32_t dtype, n_heads, n_kv_heads, head_dim;
+    int64_t n_tokens;
+    const void* d_q;
+    int64_t q_token_stride, q_head_stride;
+    jx_kv_cache cache;
+    const int32_t* d_table; /* [n_req][table_pages] */
+    int32_t table_pages, n_req;
+    const int32_t *d_q_start, *d_kv_len; /* [n_req + 1], [n_req] */
+    float scale;
+    int32_t window;
+    void* d_out;
+    float* d_lse;
+} jx_attend_args;
+int64_t jx_paged_attention_bytes(const jx_attend_args* args);
+int jx_paged_attention(const jx_attend_args* args, void* d_work, int64_t work_bytes, void* stream);
+
+/*
+ * Attention of every (token, head) over a list of rows of its own, as jx_search
+ * returns them for the queries [n_tokens * n_heads]: d_ids [n_tokens][n_heads][k],
+ * ids outside [0, n_rows) (JX_NONE among them) are passed over, an id that
+ * occurs twice counts twice.  Row i, key head h of d_keys and d_values at
+ * i * row_stride + h * head_stride.  With d_part_out [n_tokens][n_heads][head_dim]
+ * and d_part_lse the result is that over both sets of keys, the list's and
+ * those that the part came from (the part's weight is exp(lse); a part of
+ * -infinity has none); both NULL: the list alone.  d_out may be d_part_out, d_lse
+ * may be d_part_lse or NULL.
+ */
+typedef struct {
+    int32_t dtype, n_heads, n_kv_heads, head_dim;
+    int64_t n_tokens;
+    const void* d_q;
+    int64_t q_token_stride, q_head_stride;
+    const void *d_keys, *d_values;
+    int64_t row_stride, head_stride, n_rows;
+    const uint32_t* d_ids;
+    int32_t k;
+    float scale;
+    const void* d_part_out;
+    const float* d_part_lse;
+    void* d_out;
+    float* d_lse;
+} jx_found_args;
+int jx_found_attention(const jx_found_args* args, void* stream);
 
 const char* jx_strerror(int code);
 const char* jx_last_error(void);

@@ -9,6 +9,7 @@
 #include <mutex>
 #include <new>
 #include <vector>
+#include "attend.h"
 #include "jx_internal.h"
 
 // Scratch of jx_bruteforce_static: one copy per GPU, held from the moment the code object is loaded until the
@@ -302,6 +303,53 @@ void visited_table_for(uint32_t flags, int L, int64_t n, int rec_bytes, int* slo
             *tag_bits = tb;
         }
     }
+}
+
+// ---- attention beside the index ------------------------------------------------------------------------------------------
+
+bool off16(const void* p) { return (uintptr_t)p & 15; }
+
+int check_heads(int dtype, int heads, int kv_heads, int dim, int64_t tokens) {
+    if (dtype != JX_F16 && dtype != JX_BF16) return fail(JX_EINVAL, "attention: dtype must be JX_F16 or JX_BF16");
+    if (kv_heads < 1 || heads < kv_heads || heads % kv_heads || heads > 4096)
+        return fail(JX_EINVAL, "n_heads must be a multiple of n_kv_heads, at most 4096");
+    if (dim < 8 || dim > JX_MAX_HEAD_DIM || dim % 8) return fail(JX_EINVAL, "head_dim must be a multiple of 8, at most 256");
+    if (tokens < 0 || tokens * heads > 0x7FFFFFFFll / 4) return fail(JX_EINVAL, "n_tokens * n_heads out of range");
+    return JX_OK;
+}
+
+int check_rows(const char* what, const void* p, int64_t s0, int64_t s1) {
+    if (!p) return fail(JX_EINVAL, "%s is NULL", what);
+    if (off16(p) || s0 % 8 || s1 % 8) return fail(JX_EINVAL, "%s: rows must lie on 16-byte boundaries", what);
+    return JX_OK;
+}
+
+int check_page(int page, int n_pages) {
+    if (page < 1 || page > 4096 || (page & (page - 1))) return fail(JX_EINVAL, "page must be a power of two, at most 4096");
+    if (n_pages < 1) return fail(JX_EINVAL, "n_pages must be positive");
+    return JX_OK;
+}
+
+int check_cache(const jx_kv_cache& c) {
+    if (int rc = check_page(c.page, c.n_pages)) return rc;
+    if (int rc = check_rows("cache.d_k", c.d_k, c.page_stride, c.token_stride)) return rc;
+    return check_rows("cache.d_v", c.d_v, c.head_stride, 0);
+}
+
+int check_table(const int32_t* table, int table_pages, int page, int n_req) {
+    if (n_req < 0) return fail(JX_EINVAL, "n_req < 0");
+    if (table_pages < 1 || (int64_t)table_pages * page > 0x7FFFFFFFll) return fail(JX_EINVAL, "table_pages out of range");
+    if (!table && n_req) return fail(JX_EINVAL, "d_table is NULL");
+    return JX_OK;
+}
+
+int check_attend(const jx_attend_args* a) {
+    if (!a) return fail(JX_EINVAL, "args is NULL");
+    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
+    if (int rc = check_cache(a->cache)) return rc;
+    if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
+    if (a->window < 0) return fail(JX_EINVAL, "window < 0");
+    return JX_OK;
 }
 
 }  // namespace
@@ -1197,6 +1245,90 @@ int jx_mips_augment(const float* d_in, int64_t n, int32_t dim, float max_norm, i
     if (d_out && dim_out < dim + 1) return fail(JX_EINVAL, "dim_out must be at least dim + 1");
     if (d_out && !(max_norm >= 0.0f)) return fail(JX_EINVAL, "max_norm must be non-negative");
     JX_HIP(jx::launch_mips_augment(d_in, n, dim, max_norm, is_query, d_out, dim_out, d_norms, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_kv_plan(const int32_t* d_len, const int32_t* d_new, int32_t n_req, int32_t page, int32_t* d_table, int32_t table_pages,
+               const int32_t* d_free, const int32_t* d_n_free, int32_t n_pages, int32_t* d_n_free_out, int32_t* d_q_start,
+               int32_t* d_kv_len, int32_t* d_pos, int64_t* d_slot, int64_t n_tokens, void* stream) {
+    if (int rc = check_page(page, n_pages)) return rc;
+    if (int rc = check_table(d_table, table_pages, page, n_req)) return rc;
+    if (n_req > JX_MAX_REQUESTS) return fail(JX_EINVAL, "n_req above JX_MAX_REQUESTS");
+    if (n_tokens < 0 || n_tokens > 0x7FFFFFFFll) return fail(JX_EINVAL, "n_tokens out of range");
+    if ((n_req && (!d_len || !d_new || !d_kv_len)) || !d_free || !d_n_free || !d_n_free_out || !d_q_start || (n_tokens && (!d_pos || !d_slot)))
+        return fail(JX_EINVAL, "NULL argument");
+    if (d_n_free_out == d_n_free) return fail(JX_EINVAL, "d_n_free_out must not be d_n_free");
+    jx::KvPlanArgs a = {d_len, d_new, n_req, jx::log2_of(page), d_table, table_pages, d_free, d_n_free, n_pages,
+                        d_n_free_out, d_q_start, d_kv_len, d_pos, d_slot, n_tokens};
+    JX_HIP(jx::launch_kv_plan(a, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_kv_release(const int32_t* d_first, const int32_t* d_end, int32_t n_req, int32_t* d_table, int32_t table_pages,
+                  int32_t* d_free, int32_t* d_n_free, int32_t n_pages, void* stream) {
+    if (n_pages < 1) return fail(JX_EINVAL, "n_pages must be positive");
+    if (int rc = check_table(d_table, table_pages, 1, n_req)) return rc;
+    if (n_req > JX_MAX_REQUESTS) return fail(JX_EINVAL, "n_req above JX_MAX_REQUESTS");
+    if (n_req == 0) return JX_OK;
+    if (!d_first || !d_end || !d_free || !d_n_free) return fail(JX_EINVAL, "NULL argument");
+    JX_HIP(jx::launch_kv_release(d_first, d_end, n_req, d_table, table_pages, d_free, d_n_free, n_pages, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_qk_norm_rope(const jx_rope_args* a, void* stream) {
+    if (!a) return fail(JX_EINVAL, "args is NULL");
+    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
+    if (a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16)
+        return fail(JX_EINVAL, "rot_dim must be a multiple of 16, at most head_dim");
+    if (a->n_pos < 0 || a->n_pos > 0x7FFFFFFFll) return fail(JX_EINVAL, "n_pos out of range");
+    if (!(a->eps >= 0.0f)) return fail(JX_EINVAL, "eps must be non-negative");
+    if (int rc = check_cache(a->cache)) return rc;
+    if (a->n_tokens == 0) return JX_OK;
+    if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_k", a->d_k, a->k_token_stride, a->k_head_stride)) return rc;
+    if (int rc = check_rows("d_v", a->d_v, a->v_token_stride, a->v_head_stride)) return rc;
+    if (int rc = check_rows("d_q_out", a->d_q_out, 0, 0)) return rc;
+    if (off16(a->d_q_weight) || off16(a->d_k_weight)) return fail(JX_EINVAL, "weights must lie on 16-byte boundaries");
+    if (a->rot_dim && (!a->d_cos || !a->d_sin || off16(a->d_cos) || off16(a->d_sin)))
+        return fail(JX_EINVAL, "d_cos and d_sin must lie on 16-byte boundaries");
+    if (!a->d_pos || !a->d_slot) return fail(JX_EINVAL, "NULL argument");
+    JX_HIP(jx::launch_qk_norm_rope(*a, as_stream(stream)));
+    return JX_OK;
+}
+
+int64_t jx_paged_attention_bytes(const jx_attend_args* a) {
+    if (int rc = check_attend(a)) return rc;
+    return jx::paged_attention_bytes(*a);
+}
+
+int jx_paged_attention(const jx_attend_args* a, void* d_work, int64_t work_bytes, void* stream) {
+    if (int rc = check_attend(a)) return rc;
+    if (a->n_tokens == 0) return JX_OK;
+    if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_out", a->d_out, 0, 0)) return rc;
+    if (a->n_req && (!a->d_q_start || !a->d_kv_len)) return fail(JX_EINVAL, "NULL argument");
+    const int64_t need = jx::paged_attention_bytes(*a);
+    if (need && (!d_work || ((uintptr_t)d_work & 255))) return fail(JX_EINVAL, "d_work must be 256-byte aligned");
+    if (work_bytes < need) return fail(JX_ECAPACITY, "work_bytes: %lld needed", (long long)need);
+    JX_HIP(jx::launch_paged_attention(*a, (uint8_t*)d_work, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_found_attention(const jx_found_args* a, void* stream) {
+    if (!a) return fail(JX_EINVAL, "args is NULL");
+    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
+    if (a->k < 0 || (a->k && (a->n_rows < 0 || a->n_rows > 0xFFFFFFFFll))) return fail(JX_EINVAL, "k or n_rows out of range");
+    if (!a->d_part_out != !a->d_part_lse) return fail(JX_EINVAL, "d_part_out and d_part_lse belong together");
+    if (a->n_tokens == 0) return JX_OK;
+    if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_out", a->d_out, 0, 0)) return rc;
+    if (a->k && !a->d_ids) return fail(JX_EINVAL, "d_ids is NULL");
+    if (a->k && a->n_rows) {
+        if (int rc = check_rows("d_keys", a->d_keys, a->row_stride, a->head_stride)) return rc;
+        if (int rc = check_rows("d_values", a->d_values, 0, 0)) return rc;
+    }
+    if (off16(a->d_part_out)) return fail(JX_EINVAL, "d_part_out: rows must lie on 16-byte boundaries");
+    JX_HIP(jx::launch_found_attention(*a, as_stream(stream)));
     return JX_OK;
 }
 

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -18,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("JX_LIB", os.path.join(_HERE, "libjx.so"))
 
 NONE = 0xFFFFFFFF
-U8, F32, F16 = 0, 1, 2
+U8, F32, F16, BF16 = 0, 1, 2, 3
 EXACT, RABITQ = 0, 1
 CAND_FRONTIER, CAND_VISITED = 0, 1
 RULE_MAXCOS, RULE_MAXABS, RULE_DEFAULT = 0, 1, -1
@@ -27,12 +28,14 @@ FLAG_NO_PAIR, FLAG_NO_INCR_PRUNE, FLAG_NO_GRAM, FLAG_GRAM_U8 = 1 << 0, 1 << 1, 1
 FLAG_VISITED_IDS, FLAG_VISITED_NONE, FLAG_LANES_WIDE, FLAG_LANES_NARROW = 1 << 4, 1 << 5, 1 << 6, 1 << 7
 FLAG_TILED_LOADS, FLAG_WAVES_2, FLAG_WAVES_4, FLAG_QPW_2, FLAG_QPW_4 = 1 << 8, 1 << 9, 1 << 10, 1 << 11, 1 << 12
 MAX_L, MAX_R, MAX_BF_K = 512, 256, 128
+MAX_REQUESTS, MAX_HEAD_DIM = 8192, 256
 
 EXPORTS = [
     "jx_arena_bytes", "jx_create", "jx_destroy", "jx_insert", "jx_quantize", "jx_search", "jx_beam_frontier",
     "jx_bruteforce", "jx_size", "jx_export_graph", "jx_import_graph", "jx_export_codes", "jx_import_codes", "jx_rotate",
     "jx_rotate_points", "jx_encode_rotated", "jx_delete", "jx_consolidate", "jx_compact", "jx_deleted_count", "jx_probe_gather", "jx_mips_augment", "jx_strerror", "jx_last_error",
     "jx_bruteforce_static", "jx_bruteforce_kernel", "jx_set_flags",
+    "jx_kv_plan", "jx_kv_release", "jx_qk_norm_rope", "jx_paged_attention_bytes", "jx_paged_attention", "jx_found_attention",
 ]
 
 
@@ -55,6 +58,46 @@ class Stats(C.Structure):
         return out
 
 
+class KvCache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("page", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class RopeArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_tokens", C.c_int64), ("n_pos", C.c_int64),
+                ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_token_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("d_q_weight", C.c_void_p), ("d_k_weight", C.c_void_p), ("eps", C.c_float), ("d_cos", C.c_void_p),
+                ("d_sin", C.c_void_p), ("d_pos", C.c_void_p), ("d_slot", C.c_void_p), ("d_q_out", C.c_void_p), ("cache", KvCache)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_tokens", C.c_int64), ("d_q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("cache", KvCache), ("d_table", C.c_void_p), ("table_pages", C.c_int32), ("n_req", C.c_int32),
+                ("d_q_start", C.c_void_p), ("d_kv_len", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32),
+                ("d_out", C.c_void_p), ("d_lse", C.c_void_p)]
+
+
+class FoundArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_tokens", C.c_int64), ("d_q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("d_keys", C.c_void_p), ("d_values", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_rows", C.c_int64), ("d_ids", C.c_void_p), ("k", C.c_int32), ("scale", C.c_float),
+                ("d_part_out", C.c_void_p), ("d_part_lse", C.c_void_p), ("d_out", C.c_void_p), ("d_lse", C.c_void_p)]
+
+
+class KvPlan(NamedTuple):
+    """What jx_kv_plan writes beside the table."""
+    q_start: torch.Tensor
+    kv_len: torch.Tensor
+    pos: torch.Tensor
+    slot: torch.Tensor
+    n_free: torch.Tensor
+
+
 class JxError(RuntimeError):
     def __init__(self, code, text):
         super().__init__(f"libjx error {code}: {text}")
@@ -70,6 +113,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.jx_strerror.restype = C.c_char_p
     lib.jx_last_error.restype = C.c_char_p
     lib.jx_bruteforce_kernel.restype = C.c_char_p
+    lib.jx_paged_attention_bytes.restype = C.c_int64
     for name in EXPORTS:
         getattr(lib, name)  # fail loudly on a missing symbol
     return lib
@@ -315,6 +359,126 @@ def probe_gather(table: torch.Tensor, rec_bytes: int, ids: torch.Tensor, blocks:
         _check(_lib.jx_probe_gather(_ptr(table), C.c_int64(n_rec), C.c_int32(rec_bytes), _ptr(ids), C.c_int64(ids.numel()),
                                     C.c_int32(blocks), _ptr(sink), _stream()))
     return sink
+
+
+# -- attention beside the index: jx_kv_plan .. jx_found_attention
+
+_HEAD_TYPES = {torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _rows(t, dtype, shape=None):
+    """Checks of a tensor whose last dimension holds a head's elements; its pointer."""
+    assert t.is_cuda and t.dtype == dtype and (t.stride(-1) == 1 or t.shape[-1] == 1)
+    assert shape is None or tuple(t.shape) == tuple(shape), (tuple(t.shape), tuple(shape))
+    return t.data_ptr()
+
+
+def _array(t, dtype, shape):
+    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == tuple(shape), (t.dtype, tuple(t.shape), tuple(shape))
+    return t.data_ptr()
+
+
+def _kv_cache(k_cache, v_cache, dtype, head_dim):
+    assert k_cache.dim() == 4 and k_cache.shape[3] == head_dim and v_cache.stride() == k_cache.stride()
+    pages, page, _, _ = k_cache.shape
+    sp, st, sh, _ = k_cache.stride()
+    return KvCache(_rows(k_cache, dtype), _rows(v_cache, dtype, k_cache.shape), sp, st, sh, page, pages)
+
+
+def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
+    """jx_kv_plan: `table` gets the new pages in place; `n_free` stays, the number left is in the result.  n_tokens: rows of the
+    step (the host's bound on the sum of `new`).  `out`: a KvPlan to write into."""
+    n, i32 = lens.shape[0], torch.int32
+    if out is None:
+        made = [torch.empty(s, dtype=i32, device=lens.device) for s in ((n + 1,), (n,), (n_tokens,), (1,))]
+        out = KvPlan(made[0], made[1], made[2], torch.empty(n_tokens, dtype=torch.int64, device=lens.device), made[3])
+    with torch.cuda.device(lens.device):
+        _check(_lib.jx_kv_plan(C.c_void_p(_array(lens, i32, (n,))), C.c_void_p(_array(new, i32, (n,))), C.c_int32(n), C.c_int32(page),
+                               C.c_void_p(_array(table, i32, (n, table.shape[1]))), C.c_int32(table.shape[1]),
+                               C.c_void_p(_array(free, i32, (free.numel(),))), C.c_void_p(_array(n_free, i32, (1,))),
+                               C.c_int32(free.numel()), C.c_void_p(_array(out.n_free, i32, (1,))),
+                               C.c_void_p(_array(out.q_start, i32, (n + 1,))), C.c_void_p(_array(out.kv_len, i32, (n,))),
+                               C.c_void_p(_array(out.pos, i32, (n_tokens,))), C.c_void_p(_array(out.slot, torch.int64, (n_tokens,))),
+                               C.c_int64(n_tokens), _stream()))
+    return out
+
+
+def kv_release(first, end, table, free, n_free):
+    """jx_kv_release: pages first[r] .. end[r] - 1 of row r go back; `table`, `free` and `n_free` are updated in place."""
+    n, i32 = first.shape[0], torch.int32
+    with torch.cuda.device(table.device):
+        _check(_lib.jx_kv_release(C.c_void_p(_array(first, i32, (n,))), C.c_void_p(_array(end, i32, (n,))), C.c_int32(n),
+                                  C.c_void_p(_array(table, i32, (n, table.shape[1]))), C.c_int32(table.shape[1]),
+                                  C.c_void_p(_array(free, i32, (free.numel(),))), C.c_void_p(_array(n_free, i32, (1,))),
+                                  C.c_int32(free.numel()), _stream()))
+
+
+def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                 out=None):
+    """jx_qk_norm_rope: the queries [tokens][heads][head_dim] made ready (in `out`, which may be a contiguous q); keys and values
+    go to their slots of the caches [pages][page][kv_heads][head_dim] (any strides, alike in both)."""
+    t, h, d = q.shape
+    kv = k_cache.shape[2]
+    dt = q.dtype
+    if out is None:
+        out = torch.empty((t, h, d), dtype=dt, device=q.device)
+    half = cos.shape[1] if cos is not None else 0
+    n_pos = cos.shape[0] if cos is not None else 0x7FFFFFFF
+    a = RopeArgs(dtype=_HEAD_TYPES[dt], n_heads=h, n_kv_heads=kv, head_dim=d, rot_dim=2 * half, interleaved=int(interleaved), n_tokens=t,
+                 n_pos=n_pos, d_q=_rows(q, dt), d_k=_rows(k, dt, (t, kv, d)), d_v=_rows(v, dt, (t, kv, d)),
+                 q_token_stride=q.stride(0), q_head_stride=q.stride(1), k_token_stride=k.stride(0), k_head_stride=k.stride(1),
+                 v_token_stride=v.stride(0), v_head_stride=v.stride(1),
+                 d_q_weight=_array(q_weight, dt, (d,)) if q_weight is not None else None,
+                 d_k_weight=_array(k_weight, dt, (d,)) if k_weight is not None else None, eps=eps,
+                 d_cos=_array(cos, torch.float32, (n_pos, half)) if half else None,
+                 d_sin=_array(sin, torch.float32, (n_pos, half)) if half else None,
+                 d_pos=_array(pos, torch.int32, (t,)), d_slot=_array(slot, torch.int64, (t,)), d_q_out=_array(out, dt, (t, h, d)),
+                 cache=_kv_cache(k_cache, v_cache, dt, d))
+    with torch.cuda.device(q.device):
+        _check(_lib.jx_qk_norm_rope(C.byref(a), _stream()))
+    return out
+
+
+def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
+    """jx_paged_attention: (out [tokens][heads][head_dim], lse [tokens][heads]).  `out`: those two, to write into; `work`: a uint8
+    tensor as large as the call needs (made here where it is None)."""
+    t, h, d = q.shape
+    n, w = table.shape
+    if out is None:
+        out = (torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=torch.float32, device=q.device))
+    a = AttendArgs(dtype=_HEAD_TYPES[q.dtype], n_heads=h, n_kv_heads=k_cache.shape[2], head_dim=d, n_tokens=t, d_q=_rows(q, q.dtype),
+                   q_token_stride=q.stride(0), q_head_stride=q.stride(1), cache=_kv_cache(k_cache, v_cache, q.dtype, d),
+                   d_table=_array(table, torch.int32, (n, w)), table_pages=w, n_req=n, d_q_start=_array(q_start, torch.int32, (n + 1,)),
+                   d_kv_len=_array(kv_len, torch.int32, (n,)), scale=scale, window=window, d_out=_array(out[0], q.dtype, (t, h, d)),
+                   d_lse=_array(out[1], torch.float32, (t, h)) if out[1] is not None else None)
+    with torch.cuda.device(q.device):
+        if work is None:
+            nbytes = _lib.jx_paged_attention_bytes(C.byref(a))
+            if nbytes < 0:
+                _check(int(nbytes))
+            work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        _check(_lib.jx_paged_attention(C.byref(a), _ptr(work), C.c_int64(work.numel()), _stream()))
+    return out
+
+
+def found_attention(q, keys, values, ids, scale, part=None, out=None):
+    """jx_found_attention: (out, lse) over the rows ids [tokens][heads][k] of keys and values [rows][kv_heads][head_dim] (any
+    strides, alike in both), joined with part = (out, lse) of other keys if given.  `out`: two tensors to write into (may be `part`)."""
+    t, h, d = q.shape
+    n, kv, _ = keys.shape
+    if out is None:
+        out = (torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=torch.float32, device=q.device))
+    assert values.stride() == keys.stride()
+    a = FoundArgs(dtype=_HEAD_TYPES[q.dtype], n_heads=h, n_kv_heads=kv, head_dim=d, n_tokens=t, d_q=_rows(q, q.dtype),
+                  q_token_stride=q.stride(0), q_head_stride=q.stride(1), d_keys=_rows(keys, q.dtype, (n, kv, d)),
+                  d_values=_rows(values, q.dtype, (n, kv, d)), row_stride=keys.stride(0), head_stride=keys.stride(1), n_rows=n,
+                  d_ids=_array(ids, torch.int32, (t, h, ids.shape[2])), k=ids.shape[2], scale=scale,
+                  d_part_out=_array(part[0], q.dtype, (t, h, d)) if part else None,
+                  d_part_lse=_array(part[1], torch.float32, (t, h)) if part else None, d_out=_array(out[0], q.dtype, (t, h, d)),
+                  d_lse=_array(out[1], torch.float32, (t, h)) if out[1] is not None else None)
+    with torch.cuda.device(q.device):
+        _check(_lib.jx_found_attention(C.byref(a), _stream()))
+    return out
 
 
 def ids_to_numpy(t: torch.Tensor):
