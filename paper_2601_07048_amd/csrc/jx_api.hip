@@ -332,6 +332,8 @@ int check_page(int page, int n_pages) {
 
 int check_cache(const jx_kv_cache& c) {
     if (int rc = check_page(c.page, c.n_pages)) return rc;
+    if (c.page_stride < 0 || c.token_stride < 0 || c.head_stride < 0 || c.page_stride >> 34 || c.token_stride >> 34)
+        return fail(JX_EINVAL, "cache strides must be below 2^34 and not negative");
     if (int rc = check_rows("cache.d_k", c.d_k, c.page_stride, c.token_stride)) return rc;
     return check_rows("cache.d_v", c.d_v, c.head_stride, 0);
 }

@@ -5,70 +5,542 @@ namespace jx {
 
 namespace {
 
-// The request of row t (of those that begin at or before it, the last), or -1 for a row that belongs to none
-__device__ __forceinline__ int request_of(const int32_t* q_start, int n_req, long long t) {
-    if (n_req == 0 || t < q_start[0] || t >= q_start[n_req]) return -1;
-    int lo = 0, hi = n_req;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (q_start[mid] <= t) lo = mid;
-        else hi = mid;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int MAX_SLOTS = 2048;  // tiles that are shared out by keys; of more there are enough without
+
+struct PagedArgs {
+    jx_attend_args a;
+    int page_shift, group;  // group: query heads of a key head
+    int slots, n_work;      // tiles at most; workgroups that share them, 0 = a workgroup a tile
+    float* part;            // [2 n_work][ROWS][head_dim + 2]: sums over a part of a tile's keys, its largest score, its weights' sum
+    int4* joins;            // [n_work]
+};
+
+__device__ __attribute__((aligned(16))) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
+
+// ---- a tile: ROWS consecutive rows (token, head of the group) of one request -------------------------------------------
+// Request r has rows (q_start[r + 1] - q_start[r]) * group for each key head.  Its tiles are the slots from
+// q_start[r] * group / ROWS + r on: that leaves room for each request's last, partly filled one without a sum over the requests,
+// at the price of slots that stay empty.
+struct Tile {
+    int r;               // request, -1: an empty slot
+    int first, count;    // first row and number of rows
+    int p0, p1;          // positions of the first and the last row's token
+    int lo, hi;          // the keys that any of its rows sees: [lo, hi), lo rounded down to a multiple of 64
+};
+
+__device__ __forceinline__ int clamp_rows(int start, const jx_attend_args& a) { return min(max(start, 0), (int)a.n_tokens); }
+
+template <int ROWS>
+__device__ __forceinline__ int first_slot(int start, int r, const PagedArgs& g) {
+    return (int)((long long)clamp_rows(start, g.a) * g.group / ROWS) + r;
+}
+
+template <int ROWS>
+__device__ __forceinline__ Tile make_tile(const PagedArgs& g, int r, int slot, int start, int end, int len) {
+    Tile t;
+    const int b = clamp_rows(start, g.a), e = clamp_rows(end, g.a);
+    t.first = (slot - first_slot<ROWS>(start, r, g)) * ROWS;
+    t.count = min((e - b) * g.group - t.first, ROWS);
+    t.r = t.count > 0 && t.first >= 0 ? r : -1;
+    if (t.r < 0) t.count = 0;
+    const int p = max(len, 0) - (e - b);  // n_tokens is below 2^29
+    t.p0 = p + t.first / g.group;
+    t.p1 = p + (t.first + t.count - 1) / g.group;
+    const int hi = min(t.p1 + 1, g.a.table_pages << g.page_shift);
+    const int lo = g.a.window && t.p0 >= g.a.window ? t.p0 + 1 - g.a.window : 0;
+    t.lo = hi > lo ? lo & ~63 : 0;
+    t.hi = hi > lo ? hi : 0;
+    return t;
+}
+
+// The last request whose slots begin at or before `slot`, by all lanes of a wavefront
+template <int ROWS>
+__device__ __forceinline__ int slot_request(const PagedArgs& g, int slot) {
+    int lo = 0, n = g.a.n_req;  // among requests lo .. lo + n - 1
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane_id() * step;
+        const bool before = at < n && first_slot<ROWS>(g.a.d_q_start[lo + at], lo + at, g) <= slot;
+        const int k = max(__popcll(ballot(before)) - 1, 0);
+        lo += k * step;
+        n = min(step, n - k * step);
     }
     return lo;
 }
 
-// One (token, head) a wavefront; see walk_keys
-template <typename T, int LPR>
-__global__ __launch_bounds__(256) void paged_rows_kernel(jx_attend_args a, int page_shift) {
-    const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const long long t = i / a.n_heads;
-    if (t >= a.n_tokens) return;
-    const int h = (int)(i - t * a.n_heads), lane = lane_id(), c8 = lane % LPR * 8;
-    const bool inside = c8 < a.head_dim;
-    f32x8 q = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (inside) q = load8((const T*)a.d_q + t * a.q_token_stride + h * a.q_head_stride + c8);
-    const float scale = a.scale * LOG2E;
-    for (int e = 0; e < 8; e++) q[e] *= scale;
-    long long i0 = 0, i1 = 0;
-    const int r = request_of(a.d_q_start, a.n_req, t);
-    const int32_t* table = a.d_table;
-    if (r >= 0) {
-        const long long pos = (long long)a.d_kv_len[r] - (a.d_q_start[r + 1] - t);
-        i1 = min(pos + 1, (long long)a.table_pages << page_shift);
-        i0 = a.window ? max(pos + 1 - a.window, 0ll) : 0;
-        table += (size_t)r * a.table_pages;
-    }
-    const long long off = h / (a.n_heads / a.n_kv_heads) * a.cache.head_stride;
-    Softmax s = walk_keys<T, LPR>((const T*)a.cache.d_k + off, (const T*)a.cache.d_v + off, q, inside, i0, i1, [&](long long p) {
-        const int32_t id = table[p >> page_shift];
-        return (uint32_t)id < (uint32_t)a.cache.n_pages
-                   ? id * a.cache.page_stride + (p & (a.cache.page - 1)) * a.cache.token_stride : -1ll;
-    });
-    s = gather<LPR>(s);
-    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
-    if (lane < LPR && inside) {
-        for (int e = 0; e < 8; e++) s.acc[e] *= inv;
-        store8((T*)a.d_out + i * a.head_dim + c8, s.acc);
-    }
-    if (lane == 0 && a.d_lse) a.d_lse[i] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * LN2;
+// ---- rows of keys and values in LDS ------------------------------------------------------------------------------------
+// A row is CH chunks of 16 bytes; chunk c of row r lies at place c ^ mix(r).  The matrix instructions' operands are read as the
+// same chunk of 32 consecutive keys (K) and as four consecutive rows of 16 or 32 elements (V, transposed on the way); mix
+// spreads both over the banks: any 8 and any 16 consecutive rows (8 chunks: half as many places) get different places, and so
+// do rows r .. r + 3 beside pairs and quadruples of neighbouring chunks.
+template <int CH>
+__device__ __forceinline__ constexpr int mix(int r) {
+    return CH == 8 ? (r & 1) * 2 ^ (r >> 1 & 1) * 4 ^ (r >> 2 & 1) ^ (r >> 3 & 1) * 2
+                   : (r & 1) * 6 ^ (r >> 1 & 1) * 12 ^ (r >> 2 & 1) ^ (r >> 3 & 1) * 2;
+}
+
+typedef __attribute__((address_space(3))) char* lds_ptr;
+
+__device__ __forceinline__ void load_lds16(const void* from, lds_ptr to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
 template <typename T>
-hipError_t launch(const jx_attend_args& a, hipStream_t st) {
-    const unsigned blocks = (unsigned)((a.n_tokens * a.n_heads + 3) / 4);
-    const int lpr = row_lanes(a.head_dim), shift = log2_of(a.cache.page);
-    if (lpr == 8) paged_rows_kernel<T, 8><<<blocks, 256, 0, st>>>(a, shift);
-    else if (lpr == 16) paged_rows_kernel<T, 16><<<blocks, 256, 0, st>>>(a, shift);
-    else paged_rows_kernel<T, 32><<<blocks, 256, 0, st>>>(a, shift);
+struct Mfma;
+template <>
+struct Mfma<__bf16> {
+    static __device__ __forceinline__ f32x16 mul(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec<__bf16>::x8, a), __builtin_bit_cast(Vec<__bf16>::x8, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Mfma<_Float16> {
+    static __device__ __forceinline__ f32x16 mul(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Vec<_Float16>::x8, a), __builtin_bit_cast(Vec<_Float16>::x8, b), c, 0, 0, 0);
+    }
+};
+
+__device__ __forceinline__ float both_halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_halves_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// ---- many rows: four wavefronts of 32 rows each over the same keys ------------------------------------------------------
+// S^T = K Q^T, 64 keys by 32 rows at a time, so that a lane holds 32 scores of one row (the other lane with that row, 32 further on,
+// the rest); then O^T += V^T P^T, where the scores' registers are already the second operand of the matrix instruction if the keys
+// of the first are taken in the same order.  The running maximum moves only when a row's scores rise by more than 2^8 over it:
+// weights of up to 2^8 round no worse, and most tiles leave the sums alone.
+template <typename T, int NB>
+struct Rows32 {
+    static constexpr int CH = NB <= 2 ? 8 : NB <= 4 ? 16 : 32, PITCH = CH * 16;
+    s16x8 q[2 * NB];
+    f32x16 o[NB];
+    float m, l;
+    int k_at, v_at;  // a lane's first place in a row of keys, of values
+
+    __device__ __forceinline__ void begin() {
+        const int lane = lane_id(), row = lane & 31, h = lane >> 5, i = lane & 15;
+        k_at = row * PITCH + (h ^ mix<CH>(row)) * 16;
+        const int vr = 4 * h + (i >> 2), vc = (lane >> 4 & 1) * 2 + (i >> 1 & 1);
+        v_at = vr * PITCH + (vc ^ mix<CH>(vr)) * 16 + (i & 1) * 8;
+        m = -INFINITY;
+        l = 0.0f;
+        for (int b = 0; b < NB; b++) o[b] = (f32x16)0.0f;
+    }
+
+    // scores of 64 keys
+    __device__ __forceinline__ void scores(lds_ptr k, f32x16 (&s)[2]) const {
+        for (int kb = 0; kb < 2; kb++) s[kb] = (f32x16)0.0f;
+        for (int d = 0; d < 2 * NB; d++)
+            for (int kb = 0; kb < 2; kb++) {
+                const s16x8 x = *(const __attribute__((address_space(3))) s16x8*)(k + (k_at ^ (d * 32)) + kb * 32 * PITCH);
+                s[kb] = Mfma<T>::mul(x, q[d], s[kb]);
+            }
+    }
+
+    // scores to weights; c = scale * log2 e
+    __device__ __forceinline__ void weigh(f32x16 (&s)[2], float c, s16x8 (&p)[4]) {
+        float top = -INFINITY;
+        for (int kb = 0; kb < 2; kb++)
+            for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[kb][i]), s[kb][i + 1]);
+        top = both_halves_max(top) * c;
+        if (ballot(top > m + 8.0f)) {
+            const float to = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
+            m = to;
+            l *= keep;
+            for (int b = 0; b < NB; b++)
+                for (int i = 0; i < 16; i++) o[b][i] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+        float sum[2] = {0.0f, 0.0f};
+        for (int kb = 0; kb < 2; kb++)
+            for (int i = 0; i < 16; i++) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -base));
+                s[kb][i] = w;
+                sum[kb] += w;
+            }
+        l += sum[0] + sum[1];
+        for (int x = 0; x < 4; x++) {
+            f32x8 w;
+            for (int j = 0; j < 8; j++) w[j] = s[x >> 1][(x & 1) * 8 + j];
+            p[x] = __builtin_bit_cast(s16x8, __builtin_convertvector(w, typename Vec<T>::x8));
+        }
+    }
+
+    __device__ __forceinline__ void add_values(lds_ptr v, const s16x8 (&p)[4]) {
+        for (int x = 0; x < 4; x++)
+            for (int b = 0; b < NB; b++) {
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (b * 64)) + x * 16 * PITCH));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (b * 64) ^ 32) + (x * 16 + 8) * PITCH));
+                o[b] = Mfma<T>::mul(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[x], o[b]);
+            }
+    }
+};
+
+// Whether any element of a tile is infinite or not a number
+template <typename T>
+__device__ __forceinline__ bool odd_values_in(lds_ptr v, int bytes) {
+    uint32_t worst = 0;
+    for (int at = lane_id() * 16; at < bytes; at += 64 * 16) {
+        const s16x8 y = *(const __attribute__((address_space(3))) s16x8*)(v + at);
+        for (int j = 0; j < 8; j++) worst = max(worst, (uint32_t)(y[j] & 0x7FFF));
+    }
+    return ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
+}
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedArgs g) {
+    typedef Rows32<T, NB> R;
+    constexpr int ROWS = 128, KEYS = 64, TILE = KEYS * R::PITCH;
+    constexpr int LOADS = KEYS * R::CH / 256;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2] keys, [2] values; slots' sums of units, their requests
+    const jx_attend_args& a = g.a;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const lds_ptr ring = (lds_ptr)lds;
+    int* cum = (int*)(lds + 4 * TILE);                  // [slots + 1]
+    uint16_t* req = (uint16_t*)(cum + g.slots + 1);     // [slots]
+
+    // this workgroup's share: units (64 keys of a tile) x0 .. x1 - 1 of all tiles of all key heads
+    long long x0 = 0, x1 = 1, per_head = 1;
+    int head = 0, slot = 0, work = 0, shares = 1;
+    if (g.n_work) {
+        int* starts = (int*)lds;  // [n_req + 1]
+        for (int i = tid; i <= a.n_req; i += 256) starts[i] = a.d_q_start[i];
+        __syncthreads();
+        for (int s = tid; s < g.slots; s += 256) {
+            int lo = 0, hi = a.n_req;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (first_slot<ROWS>(starts[mid], mid, g) <= s) lo = mid;
+                else hi = mid;
+            }
+            const Tile t = make_tile<ROWS>(g, lo, s, starts[lo], starts[lo + 1], a.d_kv_len[lo]);
+            cum[s + 1] = t.r < 0 ? 0 : max((t.hi - t.lo + KEYS - 1) / KEYS, 1);
+            req[s] = (uint16_t)lo;
+        }
+        if (tid == 0) cum[0] = 0;
+        __syncthreads();
+        if (wave == 0) {
+            int carry = 0;
+            for (int s0 = 0; s0 < g.slots; s0 += 64) {
+                int v = s0 + lane < g.slots ? cum[s0 + lane + 1] : 0;
+                for (int d = 1; d < 64; d *= 2) {
+                    const int o = __shfl_up(v, d, 64);
+                    if (lane >= d) v += o;
+                }
+                if (s0 + lane < g.slots) cum[s0 + lane + 1] = carry + v;
+                carry += __shfl(v, 63, 64);
+            }
+        }
+        __syncthreads();
+        per_head = cum[g.slots];
+        const long long all = per_head * a.n_kv_heads;
+        shares = (int)min((long long)g.n_work, all);  // none is empty
+        // consecutive shares stay on one XCD's cache; few are spread over all
+        work = all < g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8);
+        if (tid == 0) g.joins[work] = make_int4(0, 0, 0, 0);
+        if (work >= shares) return;
+        x0 = all * work / shares;
+        x1 = all * (work + 1) / shares;
+    } else {
+        head = (int)(blockIdx.x % a.n_kv_heads);
+        slot = g.slots - 1 - (int)(blockIdx.x / a.n_kv_heads);
+    }
+
+    const int d = a.head_dim, page_mask = a.cache.page - 1;
+    const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
+    const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);  // a scale of 0 has to leave -infinity what it is
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+    while (x0 < x1) {
+        int u0 = 0, units = 1, u1 = 1;
+        Tile t;
+        if (g.n_work) {
+            head = (int)(x0 / per_head);
+            const int at = (int)(x0 - head * per_head);
+            int lo = 0, hi = g.slots;  // the last slot whose sum is <= at
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (cum[mid] <= at) lo = mid;
+                else hi = mid;
+            }
+            slot = lo;
+            u0 = at - cum[slot];
+            units = cum[slot + 1] - cum[slot];
+            u1 = (int)min((long long)units, u0 + (x1 - x0));
+            const int r = req[slot];
+            t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
+        } else {
+            const int r = slot_request<ROWS>(g, slot);
+            t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
+            if (t.r < 0) return;
+            u1 = units = max((t.hi - t.lo + KEYS - 1) / KEYS, 1);
+        }
+        const bool whole = u0 == 0 && u1 == units;
+        const int key0 = t.lo + u0 * KEYS, key1 = min(t.lo + u1 * KEYS, t.hi);
+
+        // rows of this wavefront
+        R x;
+        x.begin();
+        const int row = wave * 32 + (lane & 31);
+        const bool mine = row < t.count, busy = wave * 32 < t.count;
+        const int rr = t.first + min(row, t.count - 1), token = rr / g.group;
+        const int head_q = head * g.group + (rr - token * g.group);
+        const long long tq = clamp_rows(a.d_q_start[t.r], a) + token;
+        const int pos = t.p0 + token - t.first / g.group;
+        if (busy) {
+            const T* q = (const T*)a.d_q + tq * a.q_token_stride + head_q * a.q_head_stride + (lane >> 5) * 8;
+            for (int i = 0; i < 2 * NB; i++) {
+                uint4 w = i * 16 + (lane >> 5) * 8 < d && mine ? *(const uint4*)(q + i * 16) : make_uint4(0, 0, 0, 0);
+                w = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
+                x.q[i] = __builtin_bit_cast(s16x8, w);
+            }
+        }
+        const int rows_end = min(t.count, wave * 32 + 32) - 1;
+        const int w0 = t.p0 + (t.first + wave * 32) / g.group - t.first / g.group;            // positions of the wavefront's
+        const int w1 = t.p0 + (t.first + max(rows_end, 0)) / g.group - t.first / g.group;    // first and last row
+
+        const char* kb = (const char*)a.cache.d_k + head * a.cache.head_stride * 2;
+        const char* vb = (const char*)a.cache.d_v + head * a.cache.head_stride * 2;
+        const int32_t* table = a.d_table + (size_t)t.r * a.table_pages;
+        auto page_of = [&](int key) {  // the page of key `key`, -1 where there is none to see
+            int id = key < key1 ? table[key >> g.page_shift] : -1;
+            return (uint32_t)id < (uint32_t)a.cache.n_pages ? id : -1;
+        };
+        // Where key `key` lies, in chunks from the head's first; the page has been looked up
+        auto row_at = [&](int id, int key) {
+            return (uint64_t)(uint32_t)id * page_chunks + (uint64_t)(uint32_t)(key & page_mask) * token_chunks;
+        };
+        bool odd_values = false;  // values that are not finite where not every row looks: see below
+        auto stage = [&](int key, int ids, lds_ptr to_k, lds_ptr to_v) {
+            const uint64_t rows = row_at(max(ids, 0), key + lane);
+            const bool all = !ballot(ids < 0) && d == NB * 32;
+            for (int i = 0; i < LOADS; i++) {
+                const int at = i * (256 / R::CH) + tid / R::CH, chunk = tid % R::CH ^ mix<R::CH>(at);
+                const uint64_t off = ((uint64_t)shfl64((long long)rows, at) + chunk) * 16;
+                const char *k = kb + off, *v = vb + off;
+                if (!all) {
+                    const bool there = __shfl(ids, at, 64) >= 0 && chunk * 8 < d;
+                    k = there ? k : (const char*)zero_chunk;
+                    v = there ? v : (const char*)zero_chunk;
+                }
+                load_lds16(k, to_k + (i * 256 + wave * 64) * 16);
+                load_lds16(v, to_v + (i * 256 + wave * 64) * 16);
+            }
+        };
+        // One tile, and the next one on its way into the other half of the ring.  The compiler has to know that those are apart: it
+        // would wait for the one before it reads the other.
+        auto step = [&](int key, uint64_t there, int ids, lds_ptr __restrict k, lds_ptr __restrict v, lds_ptr __restrict next_k,
+                        lds_ptr __restrict next_v) __attribute__((always_inline)) {
+            if (key + KEYS < key1) stage(key + KEYS, ids, next_k, next_v);
+            if (!busy) return;
+            f32x16 s[2];
+            s16x8 p[4];
+            x.scores(k, s);
+            const bool all = there == ~0ull && key + KEYS - 1 <= w0 && (!a.window || key > w1 - a.window);
+            if (!all) {
+                const int after = pos - key;  // the last key that the row sees, from here
+                uint64_t seen = after < 0 ? 0 : after >= 63 ? ~0ull : (2ull << after) - 1;
+                if (a.window) {
+                    const int gone = after - a.window + 1;  // keys that have left the window
+                    seen &= gone <= 0 ? ~0ull : gone > 63 ? 0 : ~0ull << gone;
+                }
+                seen &= there;
+                seen >>= (lane >> 5) * 4;
+                for (int b = 0; b < 2; b++)
+                    for (int i = 0; i < 16; i++)
+                        if (!((uint32_t)(seen >> (b * 32)) >> ((i & 3) + 8 * (i >> 2)) & 1)) s[b][i] = -INFINITY;
+                odd_values |= odd_values_in<T>(v, TILE);
+            }
+            x.weigh(s, c, p);
+            x.add_values(v, p);
+        };
+        __syncthreads();  // the ring is free
+        int ids = page_of(key0 + lane);
+        if (key0 < key1) stage(key0, ids, ring, ring + 2 * TILE);
+        int buf = 0;
+        for (int key = key0; key < key1; key += KEYS, buf ^= 1) {
+            const uint64_t there = ballot(ids >= 0);
+            ids = page_of(key + KEYS + lane);
+            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this tile has arrived
+            __syncthreads();
+            step(key, there, ids, ring + buf * TILE, ring + (2 + buf) * TILE, ring + (buf ^ 1) * TILE, ring + (3 - buf) * TILE);
+        }
+
+        // results
+        const float l = both_halves_sum(x.l);
+        float* part = NULL;
+        if (!whole) {
+            part = g.part + (size_t)(2 * work + (u0 == 0)) * ROWS * (d + 2);
+            if (u0 == 0 && tid == 0) {  // the first of the workgroups that share this tile names it
+                const long long begin = x0, all = per_head * a.n_kv_heads;  // units begin .. begin + units - 1 are the tile's
+                const int last = (int)(((begin + units) * shares - 1) / all);
+                g.joins[work] = make_int4(last - work + 1, head, slot, t.r);
+            }
+        }
+        const long long oi = tq * a.n_heads + head_q;
+        if (busy && !odd_values) {
+            if (mine && whole) {
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                T* out = (T*)a.d_out + oi * d + (lane >> 5) * 4;
+                for (int b = 0; b < NB; b++)
+                    for (int i = 0; i < 4; i++)
+                        if (b * 32 + i * 8 + (lane >> 5) * 4 < d) {
+                            f32x4 w;
+                            for (int j = 0; j < 4; j++) w[j] = x.o[b][i * 4 + j] * inv;
+                            *(typename Vec<T>::x4*)(out + b * 32 + i * 8) = __builtin_convertvector(w, typename Vec<T>::x4);
+                        }
+                if (lane < 32 && a.d_lse) a.d_lse[oi] = l == 0.0f ? -INFINITY : (x.m + __builtin_amdgcn_logf(l)) * LN2;
+            } else if (mine) {
+                float* to = part + (size_t)row * (d + 2);
+                for (int b = 0; b < NB; b++)
+                    for (int i = 0; i < 16; i++) {
+                        const int e = b * 32 + (i & 3) + 8 * (i >> 2) + 4 * (lane >> 5);
+                        if (e < d) to[e] = x.o[b][i];
+                    }
+                if (lane < 32) {
+                    to[d] = x.m;
+                    to[d + 1] = l;
+                }
+            }
+        } else if (busy) {
+            // A weight of 0 times such a value is not 0: these 32 rows are done again, key by key
+            constexpr int LPR = R::CH;
+            const int c8 = lane % LPR * 8;
+            for (int i = wave * 32; i < min(t.count, wave * 32 + 32); i++) {
+                const int ri = t.first + i, tok = ri / g.group, hq = head * g.group + ri - tok * g.group;
+                const long long tt = clamp_rows(a.d_q_start[t.r], a) + tok;
+                const int p = t.p0 + tok - t.first / g.group;
+                f32x8 q = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (c8 < d) q = load8((const T*)a.d_q + tt * a.q_token_stride + hq * a.q_head_stride + c8);
+                for (int e = 0; e < 8; e++) q[e] *= a.scale * LOG2E;
+                const int k0 = a.window ? max(key0, p + 1 - a.window) : key0, k1 = min(key1, p + 1);
+                Softmax s = walk_keys<T, LPR>((const T*)kb, (const T*)vb, q, c8 < d, k0, k1, [&](long long key) {
+                    const int id = page_of((int)key);
+                    return id < 0 ? -1ll : (long long)row_at(id, (int)key) * 8;
+                });
+                s = gather<LPR>(s);
+                const long long o = tt * a.n_heads + hq;
+                if (whole) {
+                    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
+                    for (int e = 0; e < 8; e++) s.acc[e] *= inv;
+                    if (lane < LPR && c8 < d) store8((T*)a.d_out + o * d + c8, s.acc);
+                    if (lane == 0 && a.d_lse) a.d_lse[o] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * LN2;
+                } else {
+                    float* to = part + (size_t)i * (d + 2);
+                    if (lane < LPR && c8 < d)
+                        for (int e = 0; e < 8; e++) to[c8 + e] = s.acc[e];
+                    if (lane == 0) {
+                        to[d] = s.m;
+                        to[d + 1] = s.l;
+                    }
+                }
+            }
+        }
+        x0 += u1 - u0;
+    }
+}
+
+// The parts of a tile that several workgroups shared, as one: workgroup w adds up the tile that workgroup w began and did not end.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs g) {
+    const jx_attend_args& a = g.a;
+    const int4 j = g.joins[blockIdx.x];
+    if (!j.x) return;
+    const int work = (int)blockIdx.x, d = a.head_dim, lane = lane_id();
+    const Tile t = make_tile<ROWS>(g, j.w, j.z, a.d_q_start[j.w], a.d_q_start[j.w + 1], a.d_kv_len[j.w]);
+    for (int row = (int)blockIdx.y * 4 + (threadIdx.x >> 6); row < t.count; row += 4 * gridDim.y) {
+        auto piece = [&](int i) { return g.part + ((size_t)(2 * (work + i) + (i == 0)) * ROWS + row) * (d + 2); };
+        float m = -INFINITY;
+        for (int i = 0; i < j.x; i++) m = fmaxf(m, piece(i)[d]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float l = 0.0f;
+        f32x4 s = {0, 0, 0, 0};
+        for (int i = 0; i < j.x; i++) {
+            const float* p = piece(i);
+            const float w = __builtin_amdgcn_exp2f(p[d] - base);
+            l = fmaf(p[d + 1], w, l);
+            if (lane * 4 < d)
+                for (int e = 0; e < 4; e++) s[e] = fmaf(p[lane * 4 + e], w, s[e]);
+        }
+        const int rr = t.first + row, token = rr / g.group;
+        const long long o = (clamp_rows(a.d_q_start[t.r], a) + (long long)token) * a.n_heads + j.y * g.group + rr - token * g.group;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        for (int e = 0; e < 4; e++) s[e] *= inv;
+        if (lane * 4 < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + lane * 4) = __builtin_convertvector(s, typename Vec<T>::x4);
+        if (lane == 0 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    }
+}
+
+// Rows that belong to no request
+template <typename T>
+__global__ __launch_bounds__(256) void no_request_kernel(jx_attend_args a) {
+    const int b = a.n_req ? clamp_rows(a.d_q_start[0], a) : (int)a.n_tokens, e = a.n_req ? clamp_rows(a.d_q_start[a.n_req], a) : (int)a.n_tokens;
+    const int chunks = a.head_dim / 8;
+    for (long long t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
+        if (t >= b && t < e) continue;
+        for (int i = threadIdx.x; i < a.n_heads * chunks; i += 256) ((uint4*)((T*)a.d_out + t * a.n_heads * a.head_dim))[i] = make_uint4(0, 0, 0, 0);
+        if (a.d_lse)
+            for (int i = threadIdx.x; i < a.n_heads; i += 256) a.d_lse[t * a.n_heads + i] = -INFINITY;
+    }
+}
+
+struct Plan {
+    int slots, n_work;
+    int64_t part, joins, total;
+};
+
+Plan make_plan(const jx_attend_args& a) {
+    constexpr int ROWS = 128;
+    Plan p = {};
+    const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
+    p.slots = (int)(rows / ROWS + a.n_req);
+    if (p.slots <= MAX_SLOTS) p.n_work = a.head_dim <= 128 ? 512 : 256;
+    auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
+    p.part = 0;
+    p.joins = up((int64_t)2 * p.n_work * ROWS * (a.head_dim + 2) * 4);
+    p.total = p.joins + up((int64_t)p.n_work * 16);
+    return p;
+}
+
+template <typename T, int NB>
+hipError_t launch_tiles(const PagedArgs& g, hipStream_t st) {
+    constexpr int TILE = 64 * Rows32<T, NB>::PITCH;
+    const size_t lds = 4 * TILE + (g.n_work ? (size_t)(g.slots + 1) * 4 + (size_t)g.slots * 2 : 0);
+    hipError_t e = hipFuncSetAttribute((const void*)paged_tile_kernel<T, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return e;
+    const unsigned blocks = g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads);
+    paged_tile_kernel<T, NB><<<blocks, 256, lds, st>>>(g);
+    e = hipGetLastError();
+    if (e != hipSuccess || !g.n_work) return e;
+    join_kernel<T, 128><<<dim3(g.n_work, 4), 256, 0, st>>>(g);
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch(const jx_attend_args& a, uint8_t* work, hipStream_t st) {
+    const Plan p = make_plan(a);
+    PagedArgs g = {a, log2_of(a.cache.page), a.n_heads / a.n_kv_heads, p.slots, p.n_work, (float*)(work + p.part), (int4*)(work + p.joins)};
+    no_request_kernel<T><<<64, 256, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.n_req == 0) return e;
+    if (a.head_dim <= 64) return launch_tiles<T, 2>(g, st);
+    if (a.head_dim <= 128) return launch_tiles<T, 4>(g, st);
+    return launch_tiles<T, 8>(g, st);
 }
 
 }  // namespace
 
-int64_t paged_attention_bytes(const jx_attend_args&) { return 0; }
+int64_t paged_attention_bytes(const jx_attend_args& a) { return make_plan(a).total; }
 
-hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t*, hipStream_t st) {
-    return a.dtype == JX_BF16 ? launch<__bf16>(a, st) : launch<_Float16>(a, st);
+hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStream_t st) {
+    return a.dtype == JX_BF16 ? launch<__bf16>(a, work, st) : launch<_Float16>(a, work, st);
 }
 
 }  // namespace jx
