@@ -9,13 +9,15 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
+constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
 constexpr int MAX_SLOTS = 2048;  // tiles that are shared out by keys; of more there are enough without
 
 struct PagedArgs {
     jx_attend_args a;
     int page_shift, group;  // group: query heads of a key head
     int slots, n_work;      // tiles at most; workgroups that share them, 0 = a workgroup a tile
-    float* part;            // [2 n_work][ROWS][head_dim + 2]: sums over a part of a tile's keys, its largest score, its weights' sum
+    float* part;            // [2 n_work][4]: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
+                            // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
     int4* joins;            // [n_work]
 };
 
@@ -87,6 +89,10 @@ typedef __attribute__((address_space(3))) char* lds_ptr;
 __device__ __forceinline__ void load_lds16(const void* from, lds_ptr to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
+
+// Element e of row r (of 32) among the sums that a wavefront leaves for join_kernel; elements 4 i .. 4 i + 3 are together
+__device__ __forceinline__ int part_at(int r, int e) { return ((e >> 3) * 64 + r + (e >> 2 & 1) * 32) * 4 + (e & 3); }
+constexpr int part_floats(int nb) { return nb * 1024 + 64; }
 
 template <typename T>
 struct Mfma;
@@ -195,6 +201,19 @@ __device__ __forceinline__ bool odd_values_in(lds_ptr v, int bytes) {
     return ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
 }
 
+// Rows that belong to no request: zeros and -infinity, by workgroups `block` of `blocks`
+template <typename T>
+__device__ void clear_rows(const jx_attend_args& a, int block, int blocks) {
+    const int n = (int)a.n_tokens, b = a.n_req ? clamp_rows(a.d_q_start[0], a) : n, e = a.n_req ? clamp_rows(a.d_q_start[a.n_req], a) : n;
+    const int chunks = a.n_heads * (a.head_dim / 8), outside = b + max(n - max(b, e), 0);
+    for (int i = block; i < outside; i += blocks) {
+        const long long t = i < b ? i : i - b + max(b, e);
+        for (int c = threadIdx.x; c < chunks; c += 256) ((uint4*)a.d_out)[t * chunks + c] = make_uint4(0, 0, 0, 0);
+        if (a.d_lse)
+            for (int h = threadIdx.x; h < a.n_heads; h += 256) a.d_lse[t * a.n_heads + h] = -INFINITY;
+    }
+}
+
 template <typename T, int NB>
 __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedArgs g) {
     typedef Rows32<T, NB> R;
@@ -203,6 +222,11 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
     extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2] keys, [2] values; slots' sums of units, their requests
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int sharers = (int)gridDim.x - CLEARERS;
+    if ((int)blockIdx.x >= sharers) {
+        clear_rows<T>(a, (int)blockIdx.x - sharers, CLEARERS);
+        return;
+    }
     const lds_ptr ring = (lds_ptr)lds;
     int* cum = (int*)(lds + 4 * TILE);                  // [slots + 1]
     uint16_t* req = (uint16_t*)(cum + g.slots + 1);     // [slots]
@@ -212,7 +236,11 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
     int head = 0, slot = 0, work = 0, shares = 1;
     if (g.n_work) {
         int* starts = (int*)lds;  // [n_req + 1]
-        for (int i = tid; i <= a.n_req; i += 256) starts[i] = a.d_q_start[i];
+        int* lens = starts + a.n_req + 1;
+        for (int i = tid; i <= a.n_req; i += 256) {
+            starts[i] = a.d_q_start[i];
+            lens[i] = i < a.n_req ? a.d_kv_len[i] : 0;
+        }
         __syncthreads();
         for (int s = tid; s < g.slots; s += 256) {
             int lo = 0, hi = a.n_req;
@@ -221,7 +249,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
                 if (first_slot<ROWS>(starts[mid], mid, g) <= s) lo = mid;
                 else hi = mid;
             }
-            const Tile t = make_tile<ROWS>(g, lo, s, starts[lo], starts[lo + 1], a.d_kv_len[lo]);
+            const Tile t = make_tile<ROWS>(g, lo, s, starts[lo], starts[lo + 1], lens[lo]);
             cum[s + 1] = t.r < 0 ? 0 : max((t.hi - t.lo + KEYS - 1) / KEYS, 1);
             req[s] = (uint16_t)lo;
         }
@@ -377,7 +405,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         const float l = both_halves_sum(x.l);
         float* part = NULL;
         if (!whole) {
-            part = g.part + (size_t)(2 * work + (u0 == 0)) * ROWS * (d + 2);
+            part = g.part + ((size_t)(2 * work + (u0 == 0)) * 4 + wave) * part_floats(NB);
             if (u0 == 0 && tid == 0) {  // the first of the workgroups that share this tile names it
                 const long long begin = x0, all = per_head * a.n_kv_heads;  // units begin .. begin + units - 1 are the tile's
                 const int last = (int)(((begin + units) * shares - 1) / all);
@@ -398,16 +426,13 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
                         }
                 if (lane < 32 && a.d_lse) a.d_lse[oi] = l == 0.0f ? -INFINITY : (x.m + __builtin_amdgcn_logf(l)) * LN2;
             } else if (mine) {
-                float* to = part + (size_t)row * (d + 2);
                 for (int b = 0; b < NB; b++)
-                    for (int i = 0; i < 16; i++) {
-                        const int e = b * 32 + (i & 3) + 8 * (i >> 2) + 4 * (lane >> 5);
-                        if (e < d) to[e] = x.o[b][i];
+                    for (int i = 0; i < 4; i++) {
+                        f32x4 w;
+                        for (int j = 0; j < 4; j++) w[j] = x.o[b][i * 4 + j];
+                        *(f32x4*)(part + ((b * 4 + i) * 64 + lane) * 4) = w;
                     }
-                if (lane < 32) {
-                    to[d] = x.m;
-                    to[d + 1] = l;
-                }
+                part[NB * 1024 + lane] = lane < 32 ? x.m : l;
             }
         } else if (busy) {
             // A weight of 0 times such a value is not 0: these 32 rows are done again, key by key
@@ -433,12 +458,11 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
                     if (lane < LPR && c8 < d) store8((T*)a.d_out + o * d + c8, s.acc);
                     if (lane == 0 && a.d_lse) a.d_lse[o] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * LN2;
                 } else {
-                    float* to = part + (size_t)i * (d + 2);
                     if (lane < LPR && c8 < d)
-                        for (int e = 0; e < 8; e++) to[c8 + e] = s.acc[e];
+                        for (int e = 0; e < 8; e++) part[part_at(i & 31, c8 + e)] = s.acc[e];
                     if (lane == 0) {
-                        to[d] = s.m;
-                        to[d + 1] = s.l;
+                        part[NB * 1024 + (i & 31)] = s.m;
+                        part[NB * 1024 + 32 + (i & 31)] = s.l;
                     }
                 }
             }
@@ -447,48 +471,46 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
     }
 }
 
-// The parts of a tile that several workgroups shared, as one: workgroup w adds up the tile that workgroup w began and did not end.
-template <typename T, int ROWS>
+// The parts of a tile that several workgroups shared, as one: the tile that workgroup blockIdx.x began and did not end.
+// blockIdx.y: which 32 elements; a wavefront takes 32 rows, its lanes hold them as they did when the parts were written.
+template <typename T, int NB>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs g) {
+    constexpr int ROWS = 128;
     const jx_attend_args& a = g.a;
     const int4 j = g.joins[blockIdx.x];
     if (!j.x) return;
-    const int work = (int)blockIdx.x, d = a.head_dim, lane = lane_id();
-    const Tile t = make_tile<ROWS>(g, j.w, j.z, a.d_q_start[j.w], a.d_q_start[j.w + 1], a.d_kv_len[j.w]);
-    for (int row = (int)blockIdx.y * 4 + (threadIdx.x >> 6); row < t.count; row += 4 * gridDim.y) {
-        auto piece = [&](int i) { return g.part + ((size_t)(2 * (work + i) + (i == 0)) * ROWS + row) * (d + 2); };
-        float m = -INFINITY;
-        for (int i = 0; i < j.x; i++) m = fmaxf(m, piece(i)[d]);
-        const float base = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f;
-        f32x4 s = {0, 0, 0, 0};
-        for (int i = 0; i < j.x; i++) {
-            const float* p = piece(i);
-            const float w = __builtin_amdgcn_exp2f(p[d] - base);
-            l = fmaf(p[d + 1], w, l);
-            if (lane * 4 < d)
-                for (int e = 0; e < 4; e++) s[e] = fmaf(p[lane * 4 + e], w, s[e]);
+    const int work = (int)blockIdx.x, d = a.head_dim, lane = lane_id(), wave = (int)(threadIdx.x >> 6), b = (int)blockIdx.y;
+    const int start = a.d_q_start[j.w];
+    const Tile t = make_tile<ROWS>(g, j.w, j.z, start, a.d_q_start[j.w + 1], a.d_kv_len[j.w]);
+    const int row = wave * 32 + (lane & 31);
+    if (row >= t.count) return;
+    auto piece = [&](int i) { return g.part + ((size_t)(2 * (work + i) + (i == 0)) * 4 + wave) * part_floats(NB); };
+    float m = -INFINITY;
+#pragma unroll 8
+    for (int i = 0; i < j.x; i++) m = fmaxf(m, piece(i)[NB * 1024 + (lane & 31)]);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    f32x4 s[4];
+    for (int i = 0; i < 4; i++) s[i] = (f32x4)0.0f;
+#pragma unroll 4
+    for (int i = 0; i < j.x; i++) {
+        const float* p = piece(i);
+        const float w = __builtin_amdgcn_exp2f(p[NB * 1024 + (lane & 31)] - base);
+        l = fmaf(p[NB * 1024 + 32 + (lane & 31)], w, l);
+        for (int k = 0; k < 4; k++) {
+            const f32x4 y = *(const f32x4*)(p + ((b * 4 + k) * 64 + lane) * 4);
+            for (int e = 0; e < 4; e++) s[k][e] = fmaf(y[e], w, s[k][e]);
         }
-        const int rr = t.first + row, token = rr / g.group;
-        const long long o = (clamp_rows(a.d_q_start[t.r], a) + (long long)token) * a.n_heads + j.y * g.group + rr - token * g.group;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        for (int e = 0; e < 4; e++) s[e] *= inv;
-        if (lane * 4 < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + lane * 4) = __builtin_convertvector(s, typename Vec<T>::x4);
-        if (lane == 0 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
     }
-}
-
-// Rows that belong to no request
-template <typename T>
-__global__ __launch_bounds__(256) void no_request_kernel(jx_attend_args a) {
-    const int b = a.n_req ? clamp_rows(a.d_q_start[0], a) : (int)a.n_tokens, e = a.n_req ? clamp_rows(a.d_q_start[a.n_req], a) : (int)a.n_tokens;
-    const int chunks = a.head_dim / 8;
-    for (long long t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
-        if (t >= b && t < e) continue;
-        for (int i = threadIdx.x; i < a.n_heads * chunks; i += 256) ((uint4*)((T*)a.d_out + t * a.n_heads * a.head_dim))[i] = make_uint4(0, 0, 0, 0);
-        if (a.d_lse)
-            for (int i = threadIdx.x; i < a.n_heads; i += 256) a.d_lse[t * a.n_heads + i] = -INFINITY;
+    const int rr = t.first + row, token = rr / g.group;
+    const long long o = (clamp_rows(start, a) + (long long)token) * a.n_heads + j.y * g.group + rr - token * g.group;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    for (int k = 0; k < 4; k++) {
+        const int e = b * 32 + k * 8 + (lane >> 5) * 4;
+        for (int i = 0; i < 4; i++) s[k][i] *= inv;
+        if (e < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + e) = __builtin_convertvector(s[k], typename Vec<T>::x4);
     }
+    if (b == 0 && lane < 32 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 struct Plan {
@@ -496,15 +518,18 @@ struct Plan {
     int64_t part, joins, total;
 };
 
+int blocks_of(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 128 ? 4 : 8; }
+
 Plan make_plan(const jx_attend_args& a) {
     constexpr int ROWS = 128;
+    const int nb = blocks_of(a.head_dim);
     Plan p = {};
     const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
-    p.slots = (int)(rows / ROWS + a.n_req);
-    if (p.slots <= MAX_SLOTS) p.n_work = a.head_dim <= 128 ? 512 : 256;
+    p.slots = a.n_req ? (int)(rows / ROWS + a.n_req) : 0;
+    if (p.slots && p.slots <= MAX_SLOTS) p.n_work = a.head_dim <= 128 ? 512 : 256;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
     p.part = 0;
-    p.joins = up((int64_t)2 * p.n_work * ROWS * (a.head_dim + 2) * 4);
+    p.joins = up((int64_t)2 * p.n_work * 4 * part_floats(nb) * 4);
     p.total = p.joins + up((int64_t)p.n_work * 16);
     return p;
 }
@@ -515,11 +540,11 @@ hipError_t launch_tiles(const PagedArgs& g, hipStream_t st) {
     const size_t lds = 4 * TILE + (g.n_work ? (size_t)(g.slots + 1) * 4 + (size_t)g.slots * 2 : 0);
     hipError_t e = hipFuncSetAttribute((const void*)paged_tile_kernel<T, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return e;
-    const unsigned blocks = g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads);
+    const unsigned blocks = (g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
     paged_tile_kernel<T, NB><<<blocks, 256, lds, st>>>(g);
     e = hipGetLastError();
     if (e != hipSuccess || !g.n_work) return e;
-    join_kernel<T, 128><<<dim3(g.n_work, 4), 256, 0, st>>>(g);
+    join_kernel<T, NB><<<dim3(g.n_work, (g.a.head_dim + 31) / 32), 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -527,12 +552,8 @@ template <typename T>
 hipError_t launch(const jx_attend_args& a, uint8_t* work, hipStream_t st) {
     const Plan p = make_plan(a);
     PagedArgs g = {a, log2_of(a.cache.page), a.n_heads / a.n_kv_heads, p.slots, p.n_work, (float*)(work + p.part), (int4*)(work + p.joins)};
-    no_request_kernel<T><<<64, 256, 0, st>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.n_req == 0) return e;
-    if (a.head_dim <= 64) return launch_tiles<T, 2>(g, st);
-    if (a.head_dim <= 128) return launch_tiles<T, 4>(g, st);
-    return launch_tiles<T, 8>(g, st);
+    const int nb = blocks_of(a.head_dim);
+    return nb == 2 ? launch_tiles<T, 2>(g, st) : nb == 4 ? launch_tiles<T, 4>(g, st) : launch_tiles<T, 8>(g, st);
 }
 
 }  // namespace

@@ -114,6 +114,12 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.jx_last_error.restype = C.c_char_p
     lib.jx_bruteforce_kernel.restype = C.c_char_p
     lib.jx_paged_attention_bytes.restype = C.c_int64
+    p, i, n = C.c_void_p, C.c_int32, C.c_int64
+    lib.jx_kv_plan.argtypes = [p, p, i, i, p, i, p, p, i, p, p, p, p, p, n, p]
+    lib.jx_kv_release.argtypes = [p, p, i, p, i, p, p, i, p]
+    lib.jx_qk_norm_rope.argtypes = lib.jx_found_attention.argtypes = [p, p]
+    lib.jx_paged_attention_bytes.argtypes = [p]
+    lib.jx_paged_attention.argtypes = [p, p, n, p]
     for name in EXPORTS:
         getattr(lib, name)  # fail loudly on a missing symbol
     return lib
@@ -136,6 +142,10 @@ def _ptr(t):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+# the stream's handle without an object around it (0.1 instead of 2.8 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _torch_dtype(dtype):
@@ -361,56 +371,63 @@ def probe_gather(table: torch.Tensor, rec_bytes: int, ids: torch.Tensor, blocks:
     return sink
 
 
-# -- attention beside the index: jx_kv_plan .. jx_found_attention
+# -- attention beside the index: jx_kv_plan .. jx_found_attention.  These are called many times in each step of a model, over
+# operands of a few microseconds' work: their checks are written to be quick.
 
 _HEAD_TYPES = {torch.float16: F16, torch.bfloat16: BF16}
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
 
 
-def _rows(t, dtype, shape=None):
-    """Checks of a tensor whose last dimension holds a head's elements; its pointer."""
-    assert t.is_cuda and t.dtype == dtype and (t.stride(-1) == 1 or t.shape[-1] == 1)
-    assert shape is None or tuple(t.shape) == tuple(shape), (tuple(t.shape), tuple(shape))
+def _run(fn, device, *args):
+    """Calls an entry point with the device's current stream as its last argument."""
+    i = device.index
+    if torch.cuda.current_device() == i:
+        rc = fn(*args, _raw_stream(i))
+    else:
+        with torch.cuda.device(i):
+            rc = fn(*args, _raw_stream(i))
+    if rc:
+        _check(rc)
+
+
+def _rows(t, dtype):
+    """A tensor of any strides whose last dimension holds a head's elements."""
+    assert t.is_cuda and t.dtype is dtype and (t.stride(-1) == 1 or t.shape[-1] == 1)
     return t.data_ptr()
 
 
-def _array(t, dtype, shape):
-    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == tuple(shape), (t.dtype, tuple(t.shape), tuple(shape))
+def _array(t, dtype, *shape):
+    assert t.is_cuda and t.is_contiguous() and t.dtype is dtype and t.shape == shape, (t.dtype, tuple(t.shape), shape)
     return t.data_ptr()
 
 
 def _kv_cache(k_cache, v_cache, dtype, head_dim):
-    assert k_cache.dim() == 4 and k_cache.shape[3] == head_dim and v_cache.stride() == k_cache.stride()
-    pages, page, _, _ = k_cache.shape
-    sp, st, sh, _ = k_cache.stride()
-    return KvCache(_rows(k_cache, dtype), _rows(v_cache, dtype, k_cache.shape), sp, st, sh, page, pages)
+    pages, page, _, d = k_cache.shape
+    strides = k_cache.stride()
+    assert d == head_dim and v_cache.shape == k_cache.shape and v_cache.stride() == strides
+    return KvCache(_rows(k_cache, dtype), _rows(v_cache, dtype), strides[0], strides[1], strides[2], page, pages)
 
 
 def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
     """jx_kv_plan: `table` gets the new pages in place; `n_free` stays, the number left is in the result.  n_tokens: rows of the
     step (the host's bound on the sum of `new`).  `out`: a KvPlan to write into."""
-    n, i32 = lens.shape[0], torch.int32
+    n, w, f = lens.shape[0], table.shape[1], free.shape[0]
     if out is None:
-        made = [torch.empty(s, dtype=i32, device=lens.device) for s in ((n + 1,), (n,), (n_tokens,), (1,))]
-        out = KvPlan(made[0], made[1], made[2], torch.empty(n_tokens, dtype=torch.int64, device=lens.device), made[3])
-    with torch.cuda.device(lens.device):
-        _check(_lib.jx_kv_plan(C.c_void_p(_array(lens, i32, (n,))), C.c_void_p(_array(new, i32, (n,))), C.c_int32(n), C.c_int32(page),
-                               C.c_void_p(_array(table, i32, (n, table.shape[1]))), C.c_int32(table.shape[1]),
-                               C.c_void_p(_array(free, i32, (free.numel(),))), C.c_void_p(_array(n_free, i32, (1,))),
-                               C.c_int32(free.numel()), C.c_void_p(_array(out.n_free, i32, (1,))),
-                               C.c_void_p(_array(out.q_start, i32, (n + 1,))), C.c_void_p(_array(out.kv_len, i32, (n,))),
-                               C.c_void_p(_array(out.pos, i32, (n_tokens,))), C.c_void_p(_array(out.slot, torch.int64, (n_tokens,))),
-                               C.c_int64(n_tokens), _stream()))
+        # the 64-bit slots first, then the 32-bit arrays, in one allocation
+        block = torch.empty(3 * n_tokens + 2 * n + 2, dtype=_I32, device=lens.device)
+        slot, pos, q_start, kv_len, left = block.split((2 * n_tokens, n_tokens, n + 1, n, 1))
+        out = KvPlan(q_start, kv_len, pos, slot.view(_I64), left)
+    _run(_lib.jx_kv_plan, lens.device, _array(lens, _I32, n), _array(new, _I32, n), n, page, _array(table, _I32, n, w), w,
+         _array(free, _I32, f), _array(n_free, _I32, 1), f, _array(out.n_free, _I32, 1), _array(out.q_start, _I32, n + 1),
+         _array(out.kv_len, _I32, n), _array(out.pos, _I32, n_tokens), _array(out.slot, _I64, n_tokens), n_tokens)
     return out
 
 
 def kv_release(first, end, table, free, n_free):
     """jx_kv_release: pages first[r] .. end[r] - 1 of row r go back; `table`, `free` and `n_free` are updated in place."""
-    n, i32 = first.shape[0], torch.int32
-    with torch.cuda.device(table.device):
-        _check(_lib.jx_kv_release(C.c_void_p(_array(first, i32, (n,))), C.c_void_p(_array(end, i32, (n,))), C.c_int32(n),
-                                  C.c_void_p(_array(table, i32, (n, table.shape[1]))), C.c_int32(table.shape[1]),
-                                  C.c_void_p(_array(free, i32, (free.numel(),))), C.c_void_p(_array(n_free, i32, (1,))),
-                                  C.c_int32(free.numel()), _stream()))
+    n, w, f = first.shape[0], table.shape[1], free.shape[0]
+    _run(_lib.jx_kv_release, table.device, _array(first, _I32, n), _array(end, _I32, n), n, _array(table, _I32, n, w), w,
+         _array(free, _I32, f), _array(n_free, _I32, 1), f)
 
 
 def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
@@ -422,63 +439,54 @@ def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_wei
     dt = q.dtype
     if out is None:
         out = torch.empty((t, h, d), dtype=dt, device=q.device)
-    half = cos.shape[1] if cos is not None else 0
-    n_pos = cos.shape[0] if cos is not None else 0x7FFFFFFF
-    a = RopeArgs(dtype=_HEAD_TYPES[dt], n_heads=h, n_kv_heads=kv, head_dim=d, rot_dim=2 * half, interleaved=int(interleaved), n_tokens=t,
-                 n_pos=n_pos, d_q=_rows(q, dt), d_k=_rows(k, dt, (t, kv, d)), d_v=_rows(v, dt, (t, kv, d)),
-                 q_token_stride=q.stride(0), q_head_stride=q.stride(1), k_token_stride=k.stride(0), k_head_stride=k.stride(1),
-                 v_token_stride=v.stride(0), v_head_stride=v.stride(1),
-                 d_q_weight=_array(q_weight, dt, (d,)) if q_weight is not None else None,
-                 d_k_weight=_array(k_weight, dt, (d,)) if k_weight is not None else None, eps=eps,
-                 d_cos=_array(cos, torch.float32, (n_pos, half)) if half else None,
-                 d_sin=_array(sin, torch.float32, (n_pos, half)) if half else None,
-                 d_pos=_array(pos, torch.int32, (t,)), d_slot=_array(slot, torch.int64, (t,)), d_q_out=_array(out, dt, (t, h, d)),
-                 cache=_kv_cache(k_cache, v_cache, dt, d))
-    with torch.cuda.device(q.device):
-        _check(_lib.jx_qk_norm_rope(C.byref(a), _stream()))
+    n_pos, half = cos.shape if cos is not None else (0x7FFFFFFF, 0)
+    assert k.shape == v.shape == (t, kv, d)
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    a = RopeArgs(_HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, dt), _rows(k, dt), _rows(v, dt), qs[0], qs[1], ks[0],
+                 ks[1], vs[0], vs[1], _array(q_weight, dt, d) if q_weight is not None else None,
+                 _array(k_weight, dt, d) if k_weight is not None else None, eps, _array(cos, _F32, n_pos, half) if half else None,
+                 _array(sin, _F32, n_pos, half) if half else None, _array(pos, _I32, t), _array(slot, _I64, t), _array(out, dt, t, h, d),
+                 _kv_cache(k_cache, v_cache, dt, d))
+    _run(_lib.jx_qk_norm_rope, q.device, C.byref(a))
     return out
 
 
 def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
-    """jx_paged_attention: (out [tokens][heads][head_dim], lse [tokens][heads]).  `out`: those two, to write into; `work`: a uint8
-    tensor as large as the call needs (made here where it is None)."""
+    """jx_paged_attention: (out [tokens][heads][head_dim], lse [tokens][heads]).  `out`: those two, to write into (lse may be None);
+    `work`: a uint8 tensor as large as the call needs (made here where it is None)."""
     t, h, d = q.shape
     n, w = table.shape
-    if out is None:
-        out = (torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=torch.float32, device=q.device))
-    a = AttendArgs(dtype=_HEAD_TYPES[q.dtype], n_heads=h, n_kv_heads=k_cache.shape[2], head_dim=d, n_tokens=t, d_q=_rows(q, q.dtype),
-                   q_token_stride=q.stride(0), q_head_stride=q.stride(1), cache=_kv_cache(k_cache, v_cache, q.dtype, d),
-                   d_table=_array(table, torch.int32, (n, w)), table_pages=w, n_req=n, d_q_start=_array(q_start, torch.int32, (n + 1,)),
-                   d_kv_len=_array(kv_len, torch.int32, (n,)), scale=scale, window=window, d_out=_array(out[0], q.dtype, (t, h, d)),
-                   d_lse=_array(out[1], torch.float32, (t, h)) if out[1] is not None else None)
-    with torch.cuda.device(q.device):
-        if work is None:
-            nbytes = _lib.jx_paged_attention_bytes(C.byref(a))
-            if nbytes < 0:
-                _check(int(nbytes))
-            work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-        _check(_lib.jx_paged_attention(C.byref(a), _ptr(work), C.c_int64(work.numel()), _stream()))
-    return out
+    dt = q.dtype
+    o, lse = out if out is not None else (torch.empty((t, h, d), dtype=dt, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device))
+    qs = q.stride()
+    a = AttendArgs(_HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, dt, d),
+                   _array(table, _I32, n, w), w, n, _array(q_start, _I32, n + 1), _array(kv_len, _I32, n), scale, window,
+                   _array(o, dt, t, h, d), _array(lse, _F32, t, h) if lse is not None else None)
+    ref = C.byref(a)
+    if work is None:
+        nbytes = _lib.jx_paged_attention_bytes(ref)
+        if nbytes < 0:
+            _check(int(nbytes))
+        work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    _run(_lib.jx_paged_attention, q.device, ref, _array(work, torch.uint8, *work.shape), work.numel())
+    return o, lse
 
 
 def found_attention(q, keys, values, ids, scale, part=None, out=None):
     """jx_found_attention: (out, lse) over the rows ids [tokens][heads][k] of keys and values [rows][kv_heads][head_dim] (any
     strides, alike in both), joined with part = (out, lse) of other keys if given.  `out`: two tensors to write into (may be `part`)."""
     t, h, d = q.shape
-    n, kv, _ = keys.shape
-    if out is None:
-        out = (torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=torch.float32, device=q.device))
-    assert values.stride() == keys.stride()
-    a = FoundArgs(dtype=_HEAD_TYPES[q.dtype], n_heads=h, n_kv_heads=kv, head_dim=d, n_tokens=t, d_q=_rows(q, q.dtype),
-                  q_token_stride=q.stride(0), q_head_stride=q.stride(1), d_keys=_rows(keys, q.dtype, (n, kv, d)),
-                  d_values=_rows(values, q.dtype, (n, kv, d)), row_stride=keys.stride(0), head_stride=keys.stride(1), n_rows=n,
-                  d_ids=_array(ids, torch.int32, (t, h, ids.shape[2])), k=ids.shape[2], scale=scale,
-                  d_part_out=_array(part[0], q.dtype, (t, h, d)) if part else None,
-                  d_part_lse=_array(part[1], torch.float32, (t, h)) if part else None, d_out=_array(out[0], q.dtype, (t, h, d)),
-                  d_lse=_array(out[1], torch.float32, (t, h)) if out[1] is not None else None)
-    with torch.cuda.device(q.device):
-        _check(_lib.jx_found_attention(C.byref(a), _stream()))
-    return out
+    n, kv, kd = keys.shape
+    k = ids.shape[2]
+    dt = q.dtype
+    o, lse = out if out is not None else (torch.empty((t, h, d), dtype=dt, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device))
+    qs, ks = q.stride(), keys.stride()
+    assert kd == d and values.shape == keys.shape and values.stride() == ks
+    a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, dt), qs[0], qs[1], _rows(keys, dt), _rows(values, dt), ks[0], ks[1], n,
+                  _array(ids, _I32, t, h, k), k, scale, _array(part[0], dt, t, h, d) if part else None,
+                  _array(part[1], _F32, t, h) if part else None, _array(o, dt, t, h, d), _array(lse, _F32, t, h) if lse is not None else None)
+    _run(_lib.jx_found_attention, q.device, C.byref(a))
+    return o, lse
 
 
 def ids_to_numpy(t: torch.Tensor):

@@ -491,7 +491,7 @@ def test_steps_of_a_served_request_in_a_graph():
     """Plan, norm and rotation, attention over the cache, search results joined, captured once and replayed with new inputs:
     every replay equals the eager calls."""
     heads, kv, dim, page, n_req = 8, 2, 64, 16, 5
-    lens, new = i32([30, 0, 7, 100, 47]), i32([1, 1, 1, 1, 1])
+    lens, new = i32([30, 1, 7, 100, 47]), i32([1, 1, 1, 1, 1])
     qkv = normal((n_req, heads + 2 * kv, dim), BF, 0)
     q, k, v = qkv.split([heads, kv, kv], 1)
     pages = 64
@@ -499,8 +499,9 @@ def test_steps_of_a_served_request_in_a_graph():
     first = cache.clone()
     perm = torch.randperm(pages, generator=torch.Generator().manual_seed(2)).int().cuda()
     table = torch.full((n_req, 10), -1, dtype=torch.int32, device="cuda")
-    for r, n in enumerate([2, 0, 1, 7, 3]):
+    for r, n in enumerate([2, 1, 1, 7, 3]):
         table[r, :n] = perm[r * 10:r * 10 + n]
+    first_table = table.clone()
     free = perm[50:].contiguous()
     free = torch.cat([free, torch.full((50,), -1, dtype=torch.int32, device="cuda")])
     n_free = i32([14])
@@ -526,9 +527,11 @@ def test_steps_of_a_served_request_in_a_graph():
         qkv.copy_(normal(qkv.shape, BF, 20 + i))
         lens.copy_(i32([30 + i, 1, 7, 96 + i, 47]))
         cache.copy_(first)
+        table.copy_(first_table)  # no page belongs to two requests
         want = [x.clone() for x in step()]
         torch.cuda.synchronize()
         cache.copy_(first)
+        table.copy_(first_table)
         graph.replay()
         torch.cuda.synchronize()
         for a, b in zip(held, want):
