@@ -12,13 +12,19 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
 constexpr int MAX_SLOTS = 2048;  // tiles that are shared out by keys; of more there are enough without
 
+// A tile that several workgroups share: parts 2 work + 1 of the first of them, 2 work of the pieces - 1 that follow.  0 pieces: none
+struct __attribute__((aligned(16))) Join {
+    int pieces, head, first, count;  // of the tile: key head, first row and number of rows
+    int start, unused[3];            // of the request: its first row of q
+};
+
 struct PagedArgs {
     jx_attend_args a;
     int page_shift, group;  // group: query heads of a key head
     int slots, n_work;      // tiles at most; workgroups that share them, 0 = a workgroup a tile
     float* part;            // [2 n_work][4]: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
                             // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
-    int4* joins;            // [n_work]
+    Join* joins;            // [n_work]
 };
 
 __device__ __attribute__((aligned(16))) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
@@ -273,7 +279,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         shares = (int)min((long long)g.n_work, all);  // none is empty
         // consecutive shares stay on one XCD's cache; few are spread over all
         work = all < g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8);
-        if (tid == 0) g.joins[work] = make_int4(0, 0, 0, 0);
+        if (tid == 0) g.joins[work].pieces = 0;
         if (work >= shares) return;
         x0 = all * work / shares;
         x1 = all * (work + 1) / shares;
@@ -316,8 +322,9 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         // rows of this wavefront
         R x;
         x.begin();
-        const int row = wave * 32 + (lane & 31);
-        const bool mine = row < t.count, busy = wave * 32 < t.count;
+        const int rows0 = ((wave + work) & 3) * 32;  // tiles of few rows: the workgroups of a CU keep different SIMDs busy
+        const int row = rows0 + (lane & 31);
+        const bool mine = row < t.count, busy = rows0 < t.count;
         const int rr = t.first + min(row, t.count - 1), token = rr / g.group;
         const int head_q = head * g.group + (rr - token * g.group);
         const long long tq = clamp_rows(a.d_q_start[t.r], a) + token;
@@ -330,8 +337,8 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
                 x.q[i] = __builtin_bit_cast(s16x8, w);
             }
         }
-        const int rows_end = min(t.count, wave * 32 + 32) - 1;
-        const int w0 = t.p0 + (t.first + wave * 32) / g.group - t.first / g.group;            // positions of the wavefront's
+        const int rows_end = min(t.count, rows0 + 32) - 1;
+        const int w0 = t.p0 + (t.first + rows0) / g.group - t.first / g.group;            // positions of the wavefront's
         const int w1 = t.p0 + (t.first + max(rows_end, 0)) / g.group - t.first / g.group;    // first and last row
 
         const char* kb = (const char*)a.cache.d_k + head * a.cache.head_stride * 2;
@@ -405,11 +412,11 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         const float l = both_halves_sum(x.l);
         float* part = NULL;
         if (!whole) {
-            part = g.part + ((size_t)(2 * work + (u0 == 0)) * 4 + wave) * part_floats(NB);
+            part = g.part + ((size_t)(2 * work + (u0 == 0)) * 4 + rows0 / 32) * part_floats(NB);
             if (u0 == 0 && tid == 0) {  // the first of the workgroups that share this tile names it
                 const long long begin = x0, all = per_head * a.n_kv_heads;  // units begin .. begin + units - 1 are the tile's
                 const int last = (int)(((begin + units) * shares - 1) / all);
-                g.joins[work] = make_int4(last - work + 1, head, slot, t.r);
+                g.joins[work] = {last - work + 1, head, t.first, t.count, clamp_rows(a.d_q_start[t.r], a), {0, 0, 0}};
             }
         }
         const long long oi = tq * a.n_heads + head_q;
@@ -438,7 +445,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
             // A weight of 0 times such a value is not 0: these 32 rows are done again, key by key
             constexpr int LPR = R::CH;
             const int c8 = lane % LPR * 8;
-            for (int i = wave * 32; i < min(t.count, wave * 32 + 32); i++) {
+            for (int i = rows0; i < min(t.count, rows0 + 32); i++) {
                 const int ri = t.first + i, tok = ri / g.group, hq = head * g.group + ri - tok * g.group;
                 const long long tt = clamp_rows(a.d_q_start[t.r], a) + tok;
                 const int p = t.p0 + tok - t.first / g.group;
@@ -472,38 +479,73 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
 }
 
 // The parts of a tile that several workgroups shared, as one: the tile that workgroup blockIdx.x began and did not end.
-// blockIdx.y: which 32 elements; a wavefront takes 32 rows, its lanes hold them as they did when the parts were written.
+// blockIdx.y: which 32 elements.  A wavefront takes 32 rows, as their lanes held them when the parts were written; of a tile of few
+// rows the wavefronts share out the pieces.  Bound: the time that a chain of reads takes, hence PIECES at once.
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs g) {
-    constexpr int ROWS = 128;
+    constexpr int PIECES = 4;
+    __shared__ float others[4][18][64];
     const jx_attend_args& a = g.a;
-    const int4 j = g.joins[blockIdx.x];
-    if (!j.x) return;
+    const Join j = g.joins[blockIdx.x];
+    if (!j.pieces) return;
     const int work = (int)blockIdx.x, d = a.head_dim, lane = lane_id(), wave = (int)(threadIdx.x >> 6), b = (int)blockIdx.y;
-    const int start = a.d_q_start[j.w];
-    const Tile t = make_tile<ROWS>(g, j.w, j.z, start, a.d_q_start[j.w + 1], a.d_kv_len[j.w]);
-    const int row = wave * 32 + (lane & 31);
-    if (row >= t.count) return;
-    auto piece = [&](int i) { return g.part + ((size_t)(2 * (work + i) + (i == 0)) * 4 + wave) * part_floats(NB); };
-    float m = -INFINITY;
-#pragma unroll 8
-    for (int i = 0; i < j.x; i++) m = fmaxf(m, piece(i)[NB * 1024 + (lane & 31)]);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
+    const int groups = j.count <= 32 ? 1 : j.count <= 64 ? 2 : 4;  // of rows
+    const int row = wave % groups * 32 + (lane & 31);
+    float m = -INFINITY, l = 0.0f;
     f32x4 s[4];
     for (int i = 0; i < 4; i++) s[i] = (f32x4)0.0f;
-#pragma unroll 4
-    for (int i = 0; i < j.x; i++) {
-        const float* p = piece(i);
-        const float w = __builtin_amdgcn_exp2f(p[NB * 1024 + (lane & 31)] - base);
-        l = fmaf(p[NB * 1024 + 32 + (lane & 31)], w, l);
-        for (int k = 0; k < 4; k++) {
-            const f32x4 y = *(const f32x4*)(p + ((b * 4 + k) * 64 + lane) * 4);
-            for (int e = 0; e < 4; e++) s[k][e] = fmaf(y[e], w, s[k][e]);
+    if (row < j.count) {
+        const float* parts = g.part + (wave % groups) * part_floats(NB) + lane * 4 + b * 1024;
+        const int to_m = NB * 1024 - b * 1024 - lane * 4 + (lane & 31);
+        for (int i0 = wave / groups; i0 < j.pieces; i0 += PIECES * (4 / groups)) {
+            float pm[PIECES], pl[PIECES], top = m;
+            f32x4 y[PIECES][4];
+            for (int u = 0; u < PIECES; u++) {
+                const int i = min(i0 + u * (4 / groups), j.pieces - 1);
+                const float* p = parts + (size_t)(2 * (work + i) + (i == 0)) * 4 * part_floats(NB);
+                pm[u] = p[to_m];
+                pl[u] = p[to_m + 32];
+                for (int k = 0; k < 4; k++) y[u][k] = *(const f32x4*)(p + k * 256);
+            }
+            for (int u = 0; u < PIECES; u++) {
+                if (i0 + u * (4 / groups) >= j.pieces) pm[u] = -INFINITY;
+                top = fmaxf(top, pm[u]);
+            }
+            const float base = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - base);
+            m = top;
+            l *= keep;
+            for (int k = 0; k < 4; k++)
+                for (int e = 0; e < 4; e++) s[k][e] *= keep;
+            for (int u = 0; u < PIECES; u++) {
+                if (pm[u] == -INFINITY) continue;  // nothing, or not a piece
+                const float w = __builtin_amdgcn_exp2f(pm[u] - base);
+                l = fmaf(pl[u], w, l);
+                for (int k = 0; k < 4; k++)
+                    for (int e = 0; e < 4; e++) s[k][e] = fmaf(y[u][k][e], w, s[k][e]);
+            }
         }
     }
-    const int rr = t.first + row, token = rr / g.group;
-    const long long o = (clamp_rows(start, a) + (long long)token) * a.n_heads + j.y * g.group + rr - token * g.group;
+    if (groups < 4) {
+        others[wave][16][lane] = m;
+        others[wave][17][lane] = l;
+        for (int i = 0; i < 16; i++) others[wave][i][lane] = s[i >> 2][i & 3];
+        __syncthreads();
+        if (wave >= groups) return;
+        float top = m;
+        for (int w = wave + groups; w < 4; w += groups) top = fmaxf(top, others[w][16][lane]);
+        const float base = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - base);
+        m = top;
+        l *= keep;
+        for (int i = 0; i < 16; i++) s[i >> 2][i & 3] *= keep;
+        for (int w = wave + groups; w < 4; w += groups) {
+            const float f = __builtin_amdgcn_exp2f(others[w][16][lane] - base);
+            l = fmaf(others[w][17][lane], f, l);
+            for (int i = 0; i < 16; i++) s[i >> 2][i & 3] = fmaf(others[w][i][lane], f, s[i >> 2][i & 3]);
+        }
+    }
+    if (row >= j.count) return;
+    const int rr = j.first + row, token = rr / g.group;
+    const long long o = (j.start + (long long)token) * a.n_heads + j.head * g.group + rr - token * g.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     for (int k = 0; k < 4; k++) {
         const int e = b * 32 + k * 8 + (lane >> 5) * 4;
@@ -530,7 +572,7 @@ Plan make_plan(const jx_attend_args& a) {
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
     p.part = 0;
     p.joins = up((int64_t)2 * p.n_work * 4 * part_floats(nb) * 4);
-    p.total = p.joins + up((int64_t)p.n_work * 16);
+    p.total = p.joins + up((int64_t)p.n_work * sizeof(Join));
     return p;
 }
 
@@ -551,7 +593,7 @@ hipError_t launch_tiles(const PagedArgs& g, hipStream_t st) {
 template <typename T>
 hipError_t launch(const jx_attend_args& a, uint8_t* work, hipStream_t st) {
     const Plan p = make_plan(a);
-    PagedArgs g = {a, log2_of(a.cache.page), a.n_heads / a.n_kv_heads, p.slots, p.n_work, (float*)(work + p.part), (int4*)(work + p.joins)};
+    PagedArgs g = {a, log2_of(a.cache.page), a.n_heads / a.n_kv_heads, p.slots, p.n_work, (float*)(work + p.part), (Join*)(work + p.joins)};
     const int nb = blocks_of(a.head_dim);
     return nb == 2 ? launch_tiles<T, 2>(g, st) : nb == 4 ? launch_tiles<T, 4>(g, st) : launch_tiles<T, 8>(g, st);
 }
