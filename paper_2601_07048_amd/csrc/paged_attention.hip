@@ -10,7 +10,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
-constexpr int MAX_SLOTS = 2048;  // tiles that are shared out by keys; of more there are enough without
+constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys; of more there are enough without
 
 // A tile that several workgroups share: parts 2 work + 1 of the first of them, 2 work of the pieces - 1 that follow.  0 pieces: none
 struct __attribute__((aligned(16))) Join {
@@ -21,6 +21,8 @@ struct __attribute__((aligned(16))) Join {
 struct PagedArgs {
     jx_attend_args a;
     int page_shift, group;  // group: query heads of a key head
+    uint32_t group_mul, group_shift;  // see by_group
+    int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
     int slots, n_work;      // tiles at most; workgroups that share them, 0 = a workgroup a tile
     float* part;            // [2 n_work][4]: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
                             // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
@@ -29,12 +31,19 @@ struct PagedArgs {
 
 __device__ __attribute__((aligned(16))) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
 
+// n / group for 0 <= n < 2^31, by a product with the reciprocal rounded up to 32 bits: group_mul = ceil(2^(31 + b) / group),
+// 2^(b - 1) < group <= 2^b, is too large by less than 1 / 2^31 of itself.
+__device__ __forceinline__ int by_group(const PagedArgs& g, int n) {
+    return g.group == 1 ? n : (int)(__umulhi((uint32_t)n, g.group_mul) >> g.group_shift);
+}
+
 // ---- a tile: ROWS consecutive rows (token, head of the group) of one request -------------------------------------------
 // Request r has rows (q_start[r + 1] - q_start[r]) * group for each key head.  Its tiles are the slots from
 // q_start[r] * group / ROWS + r on: that leaves room for each request's last, partly filled one without a sum over the requests,
 // at the price of slots that stay empty.
 struct Tile {
     int r;               // request, -1: an empty slot
+    int start;           // the request's first row of q
     int first, count;    // first row and number of rows
     int p0, p1;          // positions of the first and the last row's token
     int lo, hi;          // the keys that any of its rows sees: [lo, hi), lo rounded down to a multiple of 64
@@ -51,13 +60,14 @@ template <int ROWS>
 __device__ __forceinline__ Tile make_tile(const PagedArgs& g, int r, int slot, int start, int end, int len) {
     Tile t;
     const int b = clamp_rows(start, g.a), e = clamp_rows(end, g.a);
+    t.start = b;
     t.first = (slot - first_slot<ROWS>(start, r, g)) * ROWS;
     t.count = min((e - b) * g.group - t.first, ROWS);
     t.r = t.count > 0 && t.first >= 0 ? r : -1;
-    if (t.r < 0) t.count = 0;
+    if (t.r < 0) t.count = t.first = 1;
     const int p = max(len, 0) - (e - b);  // n_tokens is below 2^29
-    t.p0 = p + t.first / g.group;
-    t.p1 = p + (t.first + t.count - 1) / g.group;
+    t.p0 = p + by_group(g, t.first);
+    t.p1 = p + by_group(g, t.first + t.count - 1);
     const int hi = min(t.p1 + 1, g.a.table_pages << g.page_shift);
     const int lo = g.a.window && t.p0 >= g.a.window ? t.p0 + 1 - g.a.window : 0;
     t.lo = hi > lo ? lo & ~63 : 0;
@@ -65,18 +75,17 @@ __device__ __forceinline__ Tile make_tile(const PagedArgs& g, int r, int slot, i
     return t;
 }
 
-// The last request whose slots begin at or before `slot`, by all lanes of a wavefront
-template <int ROWS>
-__device__ __forceinline__ int slot_request(const PagedArgs& g, int slot) {
-    int lo = 0, n = g.a.n_req;  // among requests lo .. lo + n - 1
+// The last of 0 .. n - 1 for which before() holds (it holds for all up to that one; 0 if for none), by all lanes of a wavefront
+template <typename Before>
+__device__ __forceinline__ int last_before(int n, Before before) {
+    int lo = 0;
     while (n > 1) {
-        const int step = (n + 63) / 64, at = lane_id() * step;
-        const bool before = at < n && first_slot<ROWS>(g.a.d_q_start[lo + at], lo + at, g) <= slot;
-        const int k = max(__popcll(ballot(before)) - 1, 0);
+        const int step = (n + 63) >> 6, at = lane_id() * step;
+        const int k = max(__popcll(ballot(at < n && before(lo + min(at, n - 1)))) - 1, 0);
         lo += k * step;
         n = min(step, n - k * step);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 // ---- rows of keys and values in LDS ------------------------------------------------------------------------------------
@@ -133,8 +142,8 @@ template <typename T, int NB>
 struct Rows32 {
     static constexpr int CH = NB <= 2 ? 8 : NB <= 4 ? 16 : 32, PITCH = CH * 16;
     s16x8 q[2 * NB];
-    f32x16 o[NB];
-    float m, l;
+    f32x16 o[NB];        // sums
+    float m, l, top;     // running maximum and sum of weights, the scores' largest
     int k_at, v_at;  // a lane's first place in a row of keys, of values
 
     __device__ __forceinline__ void begin() {
@@ -147,52 +156,78 @@ struct Rows32 {
         for (int b = 0; b < NB; b++) o[b] = (f32x16)0.0f;
     }
 
-    // scores of 64 keys
-    __device__ __forceinline__ void scores(lds_ptr k, f32x16 (&s)[2]) const {
-        for (int kb = 0; kb < 2; kb++) s[kb] = (f32x16)0.0f;
-        for (int d = 0; d < 2 * NB; d++)
-            for (int kb = 0; kb < 2; kb++) {
-                const s16x8 x = *(const __attribute__((address_space(3))) s16x8*)(k + (k_at ^ (d * 32)) + kb * 32 * PITCH);
-                s[kb] = Mfma<T>::mul(x, q[d], s[kb]);
-            }
+    __device__ __forceinline__ s16x8 keys_at(lds_ptr k, int i) const {  // operand i of 4 NB: 32 keys by 16 elements
+        return *(const __attribute__((address_space(3))) s16x8*)(k + (k_at ^ (i / 2 * 32)) + i % 2 * 32 * PITCH);
+    }
+    __device__ __forceinline__ s16x8 values_at(lds_ptr v, int i) const {  // operand i of 4 NB: 32 elements by 16 keys
+        const int x = i / NB, b = i % NB;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (b * 64)) + x * 16 * PITCH));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (b * 64) ^ 32) + (x * 16 + 8) * PITCH));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
 
-    // scores to weights; c = scale * log2 e
-    __device__ __forceinline__ void weigh(f32x16 (&s)[2], float c, s16x8 (&p)[4]) {
-        float top = -INFINITY;
-        for (int kb = 0; kb < 2; kb++)
-            for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[kb][i]), s[kb][i + 1]);
-        top = both_halves_max(top) * c;
-        if (ballot(top > m + 8.0f)) {
-            const float to = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
+    // The first tile's scores
+    __device__ __forceinline__ void scores(lds_ptr k, f32x16 (&s)[2]) {
+        for (int kb = 0; kb < 2; kb++) s[kb] = (f32x16)0.0f;
+        for (int i = 0; i < 4 * NB; i++) s[i & 1] = Mfma<T>::mul(keys_at(k, i), q[i / 2], s[i & 1]);
+        largest(s);
+    }
+
+    __device__ __forceinline__ void largest(const f32x16 (&s)[2]) {
+        top = -INFINITY;
+        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, s[i >> 4][i & 15]), s[i >> 4][(i & 15) + 1]);
+    }
+
+    // Moves the running maximum if these scores rise far over it; c = scale * log2 e
+    __device__ __forceinline__ void raise(float c) {
+        const float t = both_halves_max(top) * c;
+        if (ballot(t > m + 8.0f)) {
+            const float to = fmaxf(t, m), keep = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
             m = to;
             l *= keep;
             for (int b = 0; b < NB; b++)
                 for (int i = 0; i < 16; i++) o[b][i] *= keep;
         }
-        const float base = m == -INFINITY ? 0.0f : m;
-        float sum[2] = {0.0f, 0.0f};
-        for (int kb = 0; kb < 2; kb++)
-            for (int i = 0; i < 16; i++) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -base));
-                s[kb][i] = w;
-                sum[kb] += w;
-            }
-        l += sum[0] + sum[1];
-        for (int x = 0; x < 4; x++) {
-            f32x8 w;
-            for (int j = 0; j < 8; j++) w[j] = s[x >> 1][(x & 1) * 8 + j];
-            p[x] = __builtin_bit_cast(s16x8, __builtin_convertvector(w, typename Vec<T>::x8));
-        }
     }
 
-    __device__ __forceinline__ void add_values(lds_ptr v, const s16x8 (&p)[4]) {
-        for (int x = 0; x < 4; x++)
-            for (int b = 0; b < NB; b++) {
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (b * 64)) + x * 16 * PITCH));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (b * 64) ^ 32) + (x * 16 + 8) * PITCH));
-                o[b] = Mfma<T>::mul(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[x], o[b]);
+    // One tile's scores to weights while the next one's scores are formed, then the weighted values, while the next scores' largest
+    // is looked for: matrix and vector instructions alternate, reads of LDS run AHEAD matrix instructions before their use.
+    // What stands between two fences is not moved over them.
+    __device__ __forceinline__ void advance(const f32x16 (&s)[2], f32x16 (&next)[2], lds_ptr k, lds_ptr v, float c) {
+        constexpr int N = 4 * NB, AHEAD = 3, EACH = 32 / N;  // matrix instructions of each half; scores for each of them
+        const float base = m == -INFINITY ? 0.0f : m;
+        next[0] = next[1] = (f32x16)0.0f;
+        s16x8 kf[AHEAD], vf[AHEAD], p[4];
+        float w[8], sum = 0.0f;
+        for (int i = 0; i < AHEAD; i++) kf[i] = keys_at(k, i);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            next[i & 1] = Mfma<T>::mul(kf[i % AHEAD], q[i / 2], next[i & 1]);
+            if (i + AHEAD < N) kf[i % AHEAD] = keys_at(k, i + AHEAD);
+            else vf[i + AHEAD - N] = values_at(v, i + AHEAD - N);
+#pragma unroll
+            for (int e = i * EACH; e < (i + 1) * EACH; e++) {
+                w[e & 7] = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], c, -base));
+                sum += w[e & 7];
+                if ((e & 7) == 7) {
+                    f32x8 y;
+                    for (int j = 0; j < 8; j++) y[j] = w[j];
+                    p[e >> 3] = __builtin_bit_cast(s16x8, __builtin_convertvector(y, typename Vec<T>::x8));
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l += sum;
+        top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            o[i % NB] = Mfma<T>::mul(vf[i % AHEAD], p[i / NB], o[i % NB]);
+            if (i + AHEAD < N) vf[i % AHEAD] = values_at(v, i + AHEAD);
+#pragma unroll
+            for (int e = i * EACH; e < (i + 1) * EACH; e++)
+                if (e & 1) top = fmaxf(fmaxf(top, next[e >> 4][(e & 15) - 1]), next[e >> 4][e & 15]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 };
 
@@ -206,6 +241,12 @@ __device__ __forceinline__ bool odd_values_in(lds_ptr v, int bytes) {
     }
     return ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
 }
+
+// A lane's row: whether there is one, its query head, its token's row of q, its position
+struct RowAt {
+    bool mine;
+    int head, token, pos;
+};
 
 // Rows that belong to no request: zeros and -infinity, by workgroups `block` of `blocks`
 template <typename T>
@@ -234,15 +275,16 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         return;
     }
     const lds_ptr ring = (lds_ptr)lds;
-    int* cum = (int*)(lds + 4 * TILE);                  // [slots + 1]
+    int* starts = (int*)(lds + 4 * TILE);               // [n_req + 1]
+    int* lens = starts + a.n_req + 1;                   // [n_req + 1]
+    int* cum = lens + a.n_req + 1;                      // [slots + 1]
     uint16_t* req = (uint16_t*)(cum + g.slots + 1);     // [slots]
 
-    // this workgroup's share: units (64 keys of a tile) x0 .. x1 - 1 of all tiles of all key heads
-    long long x0 = 0, x1 = 1, per_head = 1;
-    int head = 0, slot = 0, work = 0, shares = 1;
+    // This workgroup's share: units (64 keys of a tile) x0 .. x1 - 1 of all tiles of all key heads.  The first `rem` shares are
+    // `each` + 1 units, the others `each`; the launch has seen to it that all units are less than 2^31.
+    uint32_t x0 = 0, x1 = 1, per_head = 1, each = 1, rem = 0;
+    int head = 0, slot = 0, work = 0;
     if (g.n_work) {
-        int* starts = (int*)lds;  // [n_req + 1]
-        int* lens = starts + a.n_req + 1;
         for (int i = tid; i <= a.n_req; i += 256) {
             starts[i] = a.d_q_start[i];
             lens[i] = i < a.n_req ? a.d_kv_len[i] : 0;
@@ -274,15 +316,17 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
             }
         }
         __syncthreads();
-        per_head = cum[g.slots];
-        const long long all = per_head * a.n_kv_heads;
-        shares = (int)min((long long)g.n_work, all);  // none is empty
+        per_head = __builtin_amdgcn_readfirstlane(cum[g.slots]);
+        const uint32_t all = per_head * a.n_kv_heads, shares = min((uint32_t)g.n_work, all);  // none is empty
         // consecutive shares stay on one XCD's cache; few are spread over all
-        work = all < g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8);
+        work = all < (uint32_t)g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8);
         if (tid == 0) g.joins[work].pieces = 0;
-        if (work >= shares) return;
-        x0 = all * work / shares;
-        x1 = all * (work + 1) / shares;
+        if ((uint32_t)work >= shares) return;
+        each = all / shares;
+        rem = all - each * shares;
+        x0 = work * each + min((uint32_t)work, rem);
+        x1 = x0 + each + ((uint32_t)work < rem);
+        head = (int)(x0 / per_head);
     } else {
         head = (int)(blockIdx.x % a.n_kv_heads);
         slot = g.slots - 1 - (int)(blockIdx.x / a.n_kv_heads);
@@ -296,22 +340,16 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         int u0 = 0, units = 1, u1 = 1;
         Tile t;
         if (g.n_work) {
-            head = (int)(x0 / per_head);
+            if (x0 >= (head + 1) * per_head) head++;
             const int at = (int)(x0 - head * per_head);
-            int lo = 0, hi = g.slots;  // the last slot whose sum is <= at
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (cum[mid] <= at) lo = mid;
-                else hi = mid;
-            }
-            slot = lo;
+            slot = last_before(g.slots, [&](int i) { return cum[i] <= at; });
             u0 = at - cum[slot];
             units = cum[slot + 1] - cum[slot];
-            u1 = (int)min((long long)units, u0 + (x1 - x0));
+            u1 = (int)min((uint32_t)units, u0 + (x1 - x0));
             const int r = req[slot];
-            t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
+            t = make_tile<ROWS>(g, r, slot, starts[r], starts[r + 1], lens[r]);
         } else {
-            const int r = slot_request<ROWS>(g, slot);
+            const int r = last_before(a.n_req, [&](int i) { return first_slot<ROWS>(a.d_q_start[i], i, g) <= slot; });
             t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
             if (t.r < 0) return;
             u1 = units = max((t.hi - t.lo + KEYS - 1) / KEYS, 1);
@@ -323,23 +361,24 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
         R x;
         x.begin();
         const int rows0 = ((wave + work) & 3) * 32;  // tiles of few rows: the workgroups of a CU keep different SIMDs busy
-        const int row = rows0 + (lane & 31);
-        const bool mine = row < t.count, busy = rows0 < t.count;
-        const int rr = t.first + min(row, t.count - 1), token = rr / g.group;
-        const int head_q = head * g.group + (rr - token * g.group);
-        const long long tq = clamp_rows(a.d_q_start[t.r], a) + token;
-        const int pos = t.p0 + token - t.first / g.group;
+        const bool busy = rows0 < t.count;
+        auto row_of = [&](int of_lane) {
+            const int row = rows0 + (of_lane & 31), rr = t.first + min(row, t.count - 1), token = by_group(g, rr);
+            return RowAt{row < t.count, head * g.group + (rr - token * g.group), t.start + token, t.p0 + token - by_group(g, t.first)};
+        };
+        const RowAt at_row = row_of(lane);
+        const int pos = at_row.pos;
         if (busy) {
-            const T* q = (const T*)a.d_q + tq * a.q_token_stride + head_q * a.q_head_stride + (lane >> 5) * 8;
+            const T* q = (const T*)a.d_q + at_row.token * a.q_token_stride + at_row.head * a.q_head_stride + (lane >> 5) * 8;
             for (int i = 0; i < 2 * NB; i++) {
-                uint4 w = i * 16 + (lane >> 5) * 8 < d && mine ? *(const uint4*)(q + i * 16) : make_uint4(0, 0, 0, 0);
+                uint4 w = i * 16 + (lane >> 5) * 8 < d && at_row.mine ? *(const uint4*)(q + i * 16) : make_uint4(0, 0, 0, 0);
                 w = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
                 x.q[i] = __builtin_bit_cast(s16x8, w);
             }
         }
         const int rows_end = min(t.count, rows0 + 32) - 1;
-        const int w0 = t.p0 + (t.first + rows0) / g.group - t.first / g.group;            // positions of the wavefront's
-        const int w1 = t.p0 + (t.first + max(rows_end, 0)) / g.group - t.first / g.group;    // first and last row
+        const int w0 = t.p0 + by_group(g, t.first + rows0) - by_group(g, t.first);            // positions of the wavefront's
+        const int w1 = t.p0 + by_group(g, t.first + max(rows_end, 0)) - by_group(g, t.first);    // first and last row
 
         const char* kb = (const char*)a.cache.d_k + head * a.cache.head_stride * 2;
         const char* vb = (const char*)a.cache.d_v + head * a.cache.head_stride * 2;
@@ -353,31 +392,33 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
             return (uint64_t)(uint32_t)id * page_chunks + (uint64_t)(uint32_t)(key & page_mask) * token_chunks;
         };
         bool odd_values = false;  // values that are not finite where not every row looks: see below
-        auto stage = [&](int key, int ids, lds_ptr to_k, lds_ptr to_v) {
+        // 64 rows of keys or values, from key `key` on, on their way into LDS; lane i has the page of the i-th.  The rows of one load of a
+        // wavefront are neighbours in a page, if that has as many: their place is then a matter of scalar instructions.
+        const uint32_t lane_off = (lane / R::CH * token_chunks + (lane % R::CH ^ mix<R::CH>(tid / R::CH))) * 16;
+        auto stage = [&](const char* from, int key, int ids, lds_ptr to) {
+            if (g.near && d == NB * 32 && !ballot(ids < 0)) {
+                for (int i = 0; i < LOADS; i++) {
+                    const int at = i * (256 / R::CH) + wave * (64 / R::CH);
+                    const uint64_t row = row_at(__builtin_amdgcn_readlane(ids, at), key + at);
+                    load_lds16(from + row * 16 + (lane_off ^ (i & 1) * mix<R::CH>(256 / R::CH) * 16), to + (i * 256 + wave * 64) * 16);
+                }
+                return;
+            }
             const uint64_t rows = row_at(max(ids, 0), key + lane);
-            const bool all = !ballot(ids < 0) && d == NB * 32;
+#pragma unroll 1
             for (int i = 0; i < LOADS; i++) {
                 const int at = i * (256 / R::CH) + tid / R::CH, chunk = tid % R::CH ^ mix<R::CH>(at);
-                const uint64_t off = ((uint64_t)shfl64((long long)rows, at) + chunk) * 16;
-                const char *k = kb + off, *v = vb + off;
-                if (!all) {
-                    const bool there = __shfl(ids, at, 64) >= 0 && chunk * 8 < d;
-                    k = there ? k : (const char*)zero_chunk;
-                    v = there ? v : (const char*)zero_chunk;
-                }
-                load_lds16(k, to_k + (i * 256 + wave * 64) * 16);
-                load_lds16(v, to_v + (i * 256 + wave * 64) * 16);
+                const char* p = from + ((uint64_t)shfl64((long long)rows, at) + chunk) * 16;
+                load_lds16(__shfl(ids, at, 64) >= 0 && chunk * 8 < d ? p : (const char*)zero_chunk, to + (i * 256 + wave * 64) * 16);
             }
         };
-        // One tile, and the next one on its way into the other half of the ring.  The compiler has to know that those are apart: it
-        // would wait for the one before it reads the other.
-        auto step = [&](int key, uint64_t there, int ids, lds_ptr __restrict k, lds_ptr __restrict v, lds_ptr __restrict next_k,
-                        lds_ptr __restrict next_v) __attribute__((always_inline)) {
-            if (key + KEYS < key1) stage(key + KEYS, ids, next_k, next_v);
+        // One tile's weights and values, the next one's scores; the keys after that and the next values on their way into the places that
+        // the last step has read.  The compiler has to know that those are apart: it would wait for what is on its way before it reads.
+        auto step = [&](int key, uint64_t there, int ids_v, int ids_k, f32x16 (&s)[2], f32x16 (&next)[2], const lds_ptr __restrict k,
+                        const lds_ptr __restrict v, const lds_ptr __restrict next_k, const lds_ptr __restrict next_v) __attribute__((always_inline)) {
+            if (key + 2 * KEYS < key1) stage(kb, key + 2 * KEYS, ids_k, next_k);
+            if (key + KEYS < key1) stage(vb, key + KEYS, ids_v, next_v);
             if (!busy) return;
-            f32x16 s[2];
-            s16x8 p[4];
-            x.scores(k, s);
             const bool all = there == ~0ull && key + KEYS - 1 <= w0 && (!a.window || key > w1 - a.window);
             if (!all) {
                 const int after = pos - key;  // the last key that the row sees, from here
@@ -391,37 +432,57 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
                 for (int b = 0; b < 2; b++)
                     for (int i = 0; i < 16; i++)
                         if (!((uint32_t)(seen >> (b * 32)) >> ((i & 3) + 8 * (i >> 2)) & 1)) s[b][i] = -INFINITY;
+                x.largest(s);
                 odd_values |= odd_values_in<T>(v, TILE);
             }
-            x.weigh(s, c, p);
-            x.add_values(v, p);
+            x.raise(c);
+            x.advance(s, next, k, v, c);  // the scores after the last tile are of no use: what lies there is read all the same
         };
+        // Keys of tile i lie in half i & 1 of the ring's first part, values in the same half of its second
+        f32x16 s0[2], s1[2];
         __syncthreads();  // the ring is free
-        int ids = page_of(key0 + lane);
-        if (key0 < key1) stage(key0, ids, ring, ring + 2 * TILE);
-        int buf = 0;
-        for (int key = key0; key < key1; key += KEYS, buf ^= 1) {
-            const uint64_t there = ballot(ids >= 0);
-            ids = page_of(key + KEYS + lane);
-            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this tile has arrived
+        int ids = page_of(key0 + lane), ids_1 = page_of(key0 + KEYS + lane);
+        if (key0 < key1) {
+            stage(kb, key0, ids, ring);
+            stage(vb, key0, ids, ring + 2 * TILE);
+            if (key0 + KEYS < key1) stage(kb, key0 + KEYS, ids_1, ring + TILE);
+            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
             __syncthreads();
-            step(key, there, ids, ring + buf * TILE, ring + (2 + buf) * TILE, ring + (buf ^ 1) * TILE, ring + (3 - buf) * TILE);
+            if (busy) x.scores(ring, s0);
+        }
+        for (int key = key0; key < key1; key += 2 * KEYS) {
+#pragma unroll
+            for (int odd = 0; odd < 2; odd++) {
+                const int at = key + odd * KEYS;
+                if (at >= key1) break;
+                const uint64_t there = ballot(ids >= 0);
+                const int ids_2 = page_of(at + 2 * KEYS + lane);
+                __builtin_amdgcn_s_waitcnt(0x0F70);  // this tile's values and the next one's keys have arrived
+                __syncthreads();
+                if (odd) step(at, there, ids_1, ids_2, s1, s0, ring, ring + 3 * TILE, ring + TILE, ring + 2 * TILE);
+                else step(at, there, ids_1, ids_2, s0, s1, ring + TILE, ring + 2 * TILE, ring, ring + 3 * TILE);
+                ids = ids_1;
+                ids_1 = ids_2;
+            }
         }
 
-        // results
+        // results; the rows' places are worked out again rather than held over the loop
+        int again = lane;
+        asm("" : "+v"(again));
+        const RowAt y = row_of(again);
         const float l = both_halves_sum(x.l);
         float* part = NULL;
         if (!whole) {
             part = g.part + ((size_t)(2 * work + (u0 == 0)) * 4 + rows0 / 32) * part_floats(NB);
             if (u0 == 0 && tid == 0) {  // the first of the workgroups that share this tile names it
-                const long long begin = x0, all = per_head * a.n_kv_heads;  // units begin .. begin + units - 1 are the tile's
-                const int last = (int)(((begin + units) * shares - 1) / all);
-                g.joins[work] = {last - work + 1, head, t.first, t.count, clamp_rows(a.d_q_start[t.r], a), {0, 0, 0}};
+                const uint32_t end = x0 + units - 1, large = rem * (each + 1);  // the tile's last unit, and whose it is
+                const int last = (int)(end < large ? end / (each + 1) : rem + (end - large) / each);
+                g.joins[work] = {last - work + 1, head, t.first, t.count, t.start, {0, 0, 0}};
             }
         }
-        const long long oi = tq * a.n_heads + head_q;
+        const long long oi = (long long)y.token * a.n_heads + y.head;
         if (busy && !odd_values) {
-            if (mine && whole) {
+            if (y.mine && whole) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 T* out = (T*)a.d_out + oi * d + (lane >> 5) * 4;
                 for (int b = 0; b < NB; b++)
@@ -432,7 +493,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
                             *(typename Vec<T>::x4*)(out + b * 32 + i * 8) = __builtin_convertvector(w, typename Vec<T>::x4);
                         }
                 if (lane < 32 && a.d_lse) a.d_lse[oi] = l == 0.0f ? -INFINITY : (x.m + __builtin_amdgcn_logf(l)) * LN2;
-            } else if (mine) {
+            } else if (y.mine) {
                 for (int b = 0; b < NB; b++)
                     for (int i = 0; i < 4; i++) {
                         f32x4 w;
@@ -446,9 +507,9 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_tile_kernel(PagedA
             constexpr int LPR = R::CH;
             const int c8 = lane % LPR * 8;
             for (int i = rows0; i < min(t.count, rows0 + 32); i++) {
-                const int ri = t.first + i, tok = ri / g.group, hq = head * g.group + ri - tok * g.group;
-                const long long tt = clamp_rows(a.d_q_start[t.r], a) + tok;
-                const int p = t.p0 + tok - t.first / g.group;
+                const int ri = t.first + i, tok = by_group(g, ri), hq = head * g.group + ri - tok * g.group;
+                const long long tt = t.start + tok;
+                const int p = t.p0 + tok - by_group(g, t.first);
                 f32x8 q = {0, 0, 0, 0, 0, 0, 0, 0};
                 if (c8 < d) q = load8((const T*)a.d_q + tt * a.q_token_stride + hq * a.q_head_stride + c8);
                 for (int e = 0; e < 8; e++) q[e] *= a.scale * LOG2E;
@@ -544,7 +605,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs g) {
         }
     }
     if (row >= j.count) return;
-    const int rr = j.first + row, token = rr / g.group;
+    const int rr = j.first + row, token = by_group(g, rr);
     const long long o = (j.start + (long long)token) * a.n_heads + j.head * g.group + rr - token * g.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     for (int k = 0; k < 4; k++) {
@@ -568,7 +629,8 @@ Plan make_plan(const jx_attend_args& a) {
     Plan p = {};
     const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
     p.slots = a.n_req ? (int)(rows / ROWS + a.n_req) : 0;
-    if (p.slots && p.slots <= MAX_SLOTS) p.n_work = a.head_dim <= 128 ? 512 : 256;
+    const double units = ((double)a.table_pages * a.cache.page / 64 + 1) * p.slots * a.n_kv_heads;  // at most
+    if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) p.n_work = a.head_dim <= 128 ? 512 : 256;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
     p.part = 0;
     p.joins = up((int64_t)2 * p.n_work * 4 * part_floats(nb) * 4);
@@ -579,7 +641,7 @@ Plan make_plan(const jx_attend_args& a) {
 template <typename T, int NB>
 hipError_t launch_tiles(const PagedArgs& g, hipStream_t st) {
     constexpr int TILE = 64 * Rows32<T, NB>::PITCH;
-    const size_t lds = 4 * TILE + (g.n_work ? (size_t)(g.slots + 1) * 4 + (size_t)g.slots * 2 : 0);
+    const size_t lds = 4 * TILE + (g.n_work ? (size_t)(g.a.n_req + 1) * 8 + (size_t)(g.slots + 1) * 4 + (size_t)g.slots * 2 : 0);
     hipError_t e = hipFuncSetAttribute((const void*)paged_tile_kernel<T, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return e;
     const unsigned blocks = (g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
@@ -593,7 +655,11 @@ hipError_t launch_tiles(const PagedArgs& g, hipStream_t st) {
 template <typename T>
 hipError_t launch(const jx_attend_args& a, uint8_t* work, hipStream_t st) {
     const Plan p = make_plan(a);
-    PagedArgs g = {a, log2_of(a.cache.page), a.n_heads / a.n_kv_heads, p.slots, p.n_work, (float*)(work + p.part), (Join*)(work + p.joins)};
+    const int rows = 64 / (blocks_of(a.head_dim) * 4);
+    const int near = a.cache.page >= rows && a.cache.token_stride * rows < (1 << 29);
+    const int group = a.n_heads / a.n_kv_heads, bits = group == 1 ? 1 : log2_of(group - 1) + 1;
+    const uint32_t mul = (uint32_t)(((1ull << (31 + bits)) + group - 1) / group);
+    PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.n_work, (float*)(work + p.part), (Join*)(work + p.joins)};
     const int nb = blocks_of(a.head_dim);
     return nb == 2 ? launch_tiles<T, 2>(g, st) : nb == 4 ? launch_tiles<T, 4>(g, st) : launch_tiles<T, 8>(g, st);
 }
