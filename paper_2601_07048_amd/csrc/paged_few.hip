@@ -1,0 +1,337 @@
+// Paged attention of few rows for each request, above all of single tokens: tiles of 16 or 32 rows.
+#include <limits.h>
+#include <type_traits>
+#include "paged_tiles.h"
+
+namespace jx {
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ f32x4 mul16(s16x8 a, s16x8 b, f32x4 c);
+template <>
+__device__ __forceinline__ f32x4 mul16<__bf16>(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Vec<__bf16>::x8, a), __builtin_bit_cast(Vec<__bf16>::x8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f32x4 mul16<_Float16>(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Vec<_Float16>::x8, a), __builtin_bit_cast(Vec<_Float16>::x8, b), c, 0, 0, 0);
+}
+
+// 16 bytes for each lane from from + off + step into LDS, zeros where off is OUTSIDE the 2 GiB after `from`.  A buffer load, not a
+// global one: the compiler counts it, while with one of those on its way it waits for all that are where it wants the first.
+constexpr uint32_t OUTSIDE = 0x80000000u;
+__device__ __forceinline__ void load_lds16_at(const char* from, uint32_t off, uint32_t step, lds_ptr to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7FFFFFFF, 0x00020000),
+                                             (__attribute__((address_space(3))) void*)to, 16, off, step, 0, 0);
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most the N latest are on their way
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | 0x0F70 | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// S^T = K Q^T and O^T += V^T P^T as for many rows, by 16x16x32 matrix instructions.  Bound: the bytes of keys and values.  So every
+// wavefront is a reader of its own: it takes 32 keys at a time, K straight into registers, V into its own two places in LDS (where
+// its transposed form is read), the next ones on their way while these are worked on, and nobody waits for another until the
+// segment's end, where the wavefronts' sums are added up.
+template <typename T, int NC, int RB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
+    constexpr int ROWS = RB * 16, KEYS = 32, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32, PITCH = CH * 16, TILE = KEYS * PITCH;
+    constexpr int NV = KEYS * CH / 64, NK = 2 * NC, OB = 2 * NC, THREADS = WAVES * 64;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];  // [WAVES][2] values, later their sums; shares
+    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS];
+    __shared__ int odd_values;  // values that are not finite where not every row looks
+    const jx_attend_args& a = g.a;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, h = lane >> 4, d = a.head_dim;
+    const int sharers = (int)gridDim.x - CLEARERS;
+    if ((int)blockIdx.x >= sharers) {
+        clear_rows<T>(a, (int)blockIdx.x - sharers, CLEARERS);
+        return;
+    }
+    Shares sh;
+    if (!sh.begin<ROWS, THREADS>(g, (int*)(lds + WAVES * 2 * TILE))) return;
+
+    const int page_mask = a.cache.page - 1;
+    const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
+    const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);  // a scale of 0 has to leave -infinity what it is
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+    const lds_ptr mine = (lds_ptr)lds + wave * 2 * TILE;
+    // a lane's place in 16 keys; of a head that ends inside a block the last chunk is read once more, against zeros of the queries
+    const uint32_t k_row = r16 * token_chunks * 16;
+    auto k_chunk = [&](int i) { return (uint32_t)min(i * 4 + h, d / 8 - 1) * 16; };
+    // a lane's place in the 64 / CH rows of one load of values
+    const uint32_t v_row = lane / CH * token_chunks * 16, v_chunk = lane % CH ^ mix<CH>(lane / CH);
+    auto v_off = [&](int i) {
+        const uint32_t chunk = v_chunk ^ mix<CH>(i * (64 / CH) & 15);
+        return v_row + (CH == OB * 2 ? chunk : min(chunk, (uint32_t)d / 8 - 1)) * 16;
+    };
+    const int vr = 4 * h + (r16 >> 2), v_at = vr * PITCH + ((r16 >> 1 & 1) ^ mix<CH>(vr)) * 16 + (r16 & 1) * 8;
+
+    while (sh.x0 < sh.x1) {
+        const Segment e = sh.next<ROWS>(g);
+        const Tile& t = e.t;
+        if (t.r < 0) return;
+        const int head = sh.head;
+        const int key0 = t.lo + e.u0 * UNIT, key1 = min(t.lo + e.u1 * UNIT, t.hi);
+        const char* kb = (const char*)a.cache.d_k + head * a.cache.head_stride * 2;
+        const char* vb = (const char*)a.cache.d_v + head * a.cache.head_stride * 2;
+        const int32_t* table = a.d_table + (size_t)t.r * a.table_pages;
+        const __attribute__((address_space(4))) int32_t* table_s = (const __attribute__((address_space(4))) int32_t*)table;
+
+        int pos[RB];
+        s16x8 q[RB][NC];
+        for (int b = 0; b < RB; b++) {
+            const int row = b * 16 + r16, rr = t.first + min(row, t.count - 1), token = by_group(g, rr), hq = head * g.group + rr - token * g.group;
+            pos[b] = t.p0 + token - by_group(g, t.first);
+            const T* from = (const T*)a.d_q + (long long)(t.start + token) * a.q_token_stride + hq * a.q_head_stride + h * 8;
+            for (int i = 0; i < NC; i++) {
+                uint4 w = i * 32 + h * 8 < d && row < t.count ? *(const uint4*)(from + i * 32) : make_uint4(0, 0, 0, 0);
+                w = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
+                q[b][i] = __builtin_bit_cast(s16x8, w);
+            }
+        }
+        f32x4 o[RB][OB];
+        float m[RB], l[RB];
+        for (int b = 0; b < RB; b++) {
+            m[b] = -INFINITY;
+            l[b] = 0.0f;
+            for (int i = 0; i < OB; i++) o[b][i] = (f32x4)0.0f;
+        }
+
+        // Keys key .. key + 15 lie in one page (a page has at least 16 tokens, and key is a multiple of 16); scalar reads
+        struct Pages {
+            int id[2];  // of 16 keys each
+        };
+        auto there = [&](int id) { return (uint32_t)id < (uint32_t)a.cache.n_pages; };
+        auto pages_at = [&](int key) {
+            Pages p;
+            for (int b = 0; b < 2; b++) p.id[b] = key + b * 16 < key1 ? table_s[(key + b * 16) >> g.page_shift] : -1;
+            return p;
+        };
+        auto row_at = [&](int id, int key) {  // page 0 stands for one that is not there
+            return ((uint64_t)(there(id) ? id : 0) * page_chunks + (uint64_t)(uint32_t)(key & page_mask) * token_chunks) * 16;
+        };
+        s16x8 k[2][NC];
+        auto load_keys = [&](int key, const Pages& p) {
+            for (int b = 0; b < 2; b++) {
+                const char* from = kb + row_at(p.id[b], key + b * 16);
+                for (int i = 0; i < NC; i++) k[b][i] = *(const s16x8*)(from + k_row + k_chunk(i));
+            }
+        };
+        // Zeros for values that are not there: their place is outside the range.  No branch: the loads that are on their way have to be as
+        // many on every path for the compiler to count them.
+        auto load_values = [&](int key, const Pages& p, lds_ptr to) {
+            const int left = key1 - key - (int)(lane / CH);
+            for (int b = 0; b < 2; b++) {
+                const char* from = vb + row_at(p.id[b], key + b * 16);
+                const int rows = there(p.id[b]) ? left : INT_MIN;
+                for (int i = b * NV / 2; i < (b + 1) * NV / 2; i++)
+                    load_lds16_at(from, i * (64 / CH) < rows ? v_off(i) : OUTSIDE, (i - b * NV / 2) * (64 / CH) * 16 * token_chunks, to + i * 1024);
+            }
+        };
+        bool odd = false;
+        // 32 keys; while they are worked on the next ones are on their way, the keys into the registers that the scores have been made of,
+        // the values into the other place.  The compiler has to know that this is another: it would wait for it.
+        auto work_on = [&](auto more, int key, const Pages& here, int next_key, const Pages& next, const lds_ptr __restrict v,
+                           const lds_ptr __restrict next_v) __attribute__((always_inline)) {
+            if (more) load_values(next_key, next, next_v);
+            f32x4 s[RB][2];
+            for (int b = 0; b < RB; b++)
+                for (int x = 0; x < 2; x++) s[b][x] = (f32x4)0.0f;
+            for (int i = 0; i < NC; i++)
+                for (int x = 0; x < 2; x++)
+                    for (int b = 0; b < RB; b++) s[b][x] = mul16<T>(k[x][i], q[b][i], s[b][x]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) load_keys(next_key, next);
+            // what is not seen, and the weights
+            const bool all = key + KEYS <= key1 && there(here.id[0]) && there(here.id[1]) && key + KEYS - 1 <= t.p0 && (!a.window || key > t.p1 - a.window);
+            s16x8 p[RB];
+            for (int b = 0; b < RB; b++) {
+                if (!all)
+                    for (int x = 0; x < 2; x++)
+                        for (int i = 0; i < 4; i++) {
+                            const int at = key + x * 16 + 4 * h + i;
+                            if (at > pos[b] || at >= key1 || (a.window && at <= pos[b] - a.window) || !there(here.id[x])) s[b][x][i] = -INFINITY;
+                        }
+                float top = -INFINITY;
+                for (int i = 0; i < 8; i += 2) top = fmaxf(fmaxf(top, s[b][i >> 2][i & 3]), s[b][i >> 2][(i & 3) + 1]);
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64)) * c;
+                if (ballot(top > m[b] + 8.0f)) {  // the running maximum moves only for a rise by more than 2^8, as for many rows
+                    const float to = fmaxf(top, m[b]), keep = __builtin_amdgcn_exp2f(m[b] - (to == -INFINITY ? 0.0f : to));
+                    m[b] = to;
+                    l[b] *= keep;
+                    for (int i = 0; i < OB; i++)
+                        for (int j = 0; j < 4; j++) o[b][i][j] *= keep;
+                }
+                const float base = m[b] == -INFINITY ? 0.0f : m[b];
+                f32x8 w;
+                for (int i = 0; i < 8; i++) {
+                    w[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i >> 2][i & 3], c, -base));
+                    l[b] += w[i];
+                }
+                p[b] = __builtin_bit_cast(s16x8, __builtin_convertvector(w, typename Vec<T>::x8));
+            }
+            if (more) wait_loads<NV + NK>();
+            else wait_loads<0>();
+            if (!all && t.count > 1) {
+                uint32_t worst = 0;
+                for (int i = lane * 16; i < TILE; i += 1024) {
+                    if ((i % PITCH / 16 ^ mix<CH>(i / PITCH & 15)) * 8 >= d) continue;  // behind the head's end
+                    const s16x4 y0 = *(const __attribute__((address_space(3))) s16x4*)(v + i), y1 = *(const __attribute__((address_space(3))) s16x4*)(v + i + 8);
+                    for (int j = 0; j < 4; j++) worst = max(worst, max((uint32_t)(y0[j] & 0x7FFF), (uint32_t)(y1[j] & 0x7FFF)));
+                }
+                odd |= ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
+            }
+            s16x8 y[OB];
+            for (int i = 0; i < OB; i++) {
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (i * 32))));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (i * 32)) + 16 * PITCH));
+                y[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < OB; i++)
+                for (int b = 0; b < RB; b++) o[b][i] = mul16<T>(y[i], p[b], o[b][i]);
+            __builtin_amdgcn_sched_barrier(0);  // the place has been read before it is filled again
+        };
+        int key = key0 + wave * KEYS, buf = 0;
+        if (key < key1) {
+            constexpr int STEP = WAVES * KEYS;
+            Pages here = pages_at(key), next = pages_at(key + STEP);
+            load_keys(key, here);
+            load_values(key, here, mine);
+            for (; key + STEP < key1; key += STEP, buf ^= TILE) {
+                const Pages then = pages_at(key + 2 * STEP);
+                work_on(std::true_type{}, key, here, key + STEP, next, mine + buf, mine + (buf ^ TILE));
+                here = next;
+                next = then;
+            }
+            work_on(std::false_type{}, key, here, 0, next, mine + buf, mine + (buf ^ TILE));
+        }
+
+        // The wavefronts' sums as one
+        if (tid == 0) odd_values = 0;
+        for (int b = 0; b < RB; b++) {
+            l[b] += __shfl_xor(l[b], 16, 64);
+            l[b] += __shfl_xor(l[b], 32, 64);
+            if (h == 0) {
+                wave_m[wave][b * 16 + r16] = m[b];
+                wave_l[wave][b * 16 + r16] = l[b];
+            }
+        }
+        __syncthreads();
+        if (odd && lane == 0) odd_values = 1;
+        f32x4* sums = (f32x4*)lds;  // [RB][WAVES][OB][64]
+        for (int b = 0; b < RB; b++) {
+            float top = -INFINITY;
+            for (int w = 0; w < WAVES; w++) top = fmaxf(top, wave_m[w][b * 16 + r16]);
+            const float keep = __builtin_amdgcn_exp2f(m[b] - (top == -INFINITY ? 0.0f : top));
+            for (int i = 0; i < OB; i++) {
+                f32x4 y = o[b][i];
+                for (int j = 0; j < 4; j++) y[j] *= keep;
+                sums[((b * WAVES + wave) * OB + i) * 64 + lane] = y;
+            }
+        }
+        __syncthreads();
+        const bool whole = e.whole();
+        float* part = NULL;
+        if (!whole) {
+            part = sh.part(g, e.u0 == 0, NC);
+            if (e.u0 == 0 && tid == 0) sh.name(g, e);
+        }
+        if (!odd_values) {
+            for (int i = tid; i < RB * OB * 64; i += THREADS) {
+                const int b = i / (OB * 64), j = i % (OB * 64), row = b * 16 + (j & 15), el = j / 64 * 16 + (j >> 4 & 3) * 4;
+                if (row >= t.count) continue;
+                f32x4 y = sums[b * WAVES * OB * 64 + j];
+                for (int w = 1; w < WAVES; w++)
+                    for (int x = 0; x < 4; x++) y[x] += sums[(b * WAVES + w) * OB * 64 + j][x];
+                float top = -INFINITY, sum = 0.0f;
+                for (int w = 0; w < WAVES; w++) top = fmaxf(top, wave_m[w][row]);
+                for (int w = 0; w < WAVES; w++) sum += wave_l[w][row] * __builtin_amdgcn_exp2f(wave_m[w][row] - (top == -INFINITY ? 0.0f : top));
+                if (whole) {
+                    const int rr = t.first + row, token = by_group(g, rr);
+                    const long long out = (long long)(t.start + token) * a.n_heads + head * g.group + rr - token * g.group;
+                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    for (int x = 0; x < 4; x++) y[x] *= inv;
+                    if (el < d) *(typename Vec<T>::x4*)((T*)a.d_out + out * d + el) = __builtin_convertvector(y, typename Vec<T>::x4);
+                    if (el == 0 && a.d_lse) a.d_lse[out] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+                } else {
+                    *(f32x4*)(part + part_at(row, el)) = y;
+                    if (el == 0) {
+                        part[NC * 1024 + row] = top;
+                        part[NC * 1024 + 32 + row] = sum;
+                    }
+                }
+            }
+        } else {
+            // A weight of 0 times such a value is not 0: these rows are done again, key by key
+            const int c8 = lane % CH * 8;
+            for (int row = wave; row < t.count; row += WAVES) {
+                const int rr = t.first + row, token = by_group(g, rr), hq = head * g.group + rr - token * g.group;
+                const int p = t.p0 + token - by_group(g, t.first);
+                f32x8 y = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (c8 < d) y = load8((const T*)a.d_q + (long long)(t.start + token) * a.q_token_stride + hq * a.q_head_stride + c8);
+                for (int i = 0; i < 8; i++) y[i] *= a.scale * LOG2E;
+                const int k0 = a.window ? max(key0, p + 1 - a.window) : key0, k1 = min(key1, p + 1);
+                Softmax s = walk_keys<T, CH>((const T*)kb, (const T*)vb, y, c8 < d, k0, k1, [&](long long at) {
+                    const int id = table[at >> g.page_shift];
+                    return there(id) ? (long long)row_at(id, (int)at) / 2 : -1ll;
+                });
+                s = gather<CH>(s);
+                const long long out = (long long)(t.start + token) * a.n_heads + hq;
+                if (whole) {
+                    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
+                    for (int i = 0; i < 8; i++) s.acc[i] *= inv;
+                    if (lane < CH && c8 < d) store8((T*)a.d_out + out * d + c8, s.acc);
+                    if (lane == 0 && a.d_lse) a.d_lse[out] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * LN2;
+                } else {
+                    if (lane < CH && c8 < d)
+                        for (int i = 0; i < 8; i++) part[part_at(row, c8 + i)] = s.acc[i];
+                    if (lane == 0) {
+                        part[NC * 1024 + row] = s.m;
+                        part[NC * 1024 + 32 + row] = s.l;
+                    }
+                }
+            }
+        }
+        __syncthreads();  // before the next segment's values and sums
+        sh.x0 += e.u1 - e.u0;
+    }
+}
+
+template <typename T, int NC, int RB>
+hipError_t launch(const PagedArgs& g, hipStream_t st) {
+    constexpr int WAVES = NC <= 4 ? 8 : 4, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32;
+    const size_t lds = WAVES * 2 * 32 * CH * 16 + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
+    static const hipError_t set = hipFuncSetAttribute((const void*)paged_few_kernel<T, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
+    if (set != hipSuccess) return set;
+    const unsigned blocks = (g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
+    paged_few_kernel<T, NC, RB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
+    return hipGetLastError();
+}
+
+template <typename T, int RB>
+hipError_t launch_dim(const PagedArgs& g, hipStream_t st) {
+    switch (blocks_of(g.a.head_dim)) {
+        case 2: return launch<T, 2, RB>(g, st);
+        case 3: return launch<T, 3, RB>(g, st);
+        case 4: return launch<T, 4, RB>(g, st);
+        case 6: return launch<T, 6, RB>(g, st);
+    }
+    return launch<T, 8, RB>(g, st);
+}
+
+}  // namespace
+
+hipError_t launch_paged_few(const PagedArgs& g, int rows, hipStream_t st) {
+    if (g.a.dtype == JX_BF16) return rows == 16 ? launch_dim<__bf16, 1>(g, st) : launch_dim<__bf16, 2>(g, st);
+    return rows == 16 ? launch_dim<_Float16, 1>(g, st) : launch_dim<_Float16, 2>(g, st);
+}
+
+}  // namespace jx

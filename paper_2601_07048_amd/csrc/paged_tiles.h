@@ -1,0 +1,258 @@
+// Tiles of a paged attention call: what they are, how they are shared out over workgroups, how rows lie in LDS.
+#pragma once
+#include "attend_walk.h"
+
+namespace jx {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
+constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys; of more there are enough without
+
+// A tile that several workgroups share: parts 2 work + 1 of the first of them, 2 work of the pieces - 1 that follow.  0 pieces: none
+struct __attribute__((aligned(16))) Join {
+    int pieces, head, first, count;  // of the tile: key head, first row and number of rows
+    int start, unused[3];            // of the request: its first row of q
+};
+
+struct PagedArgs {
+    jx_attend_args a;
+    int page_shift, group;  // group: query heads of a key head
+    uint32_t group_mul, group_shift;  // see by_group
+    int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
+    int slots, n_work;      // tiles at most; workgroups that share them, 0 = a workgroup a tile
+    int part_rows;          // tiles' rows / 32
+    float* part;            // [2 n_work][part_rows]: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
+                            // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
+    Join* joins;            // [n_work]
+};
+
+hipError_t launch_paged_many(const PagedArgs& g, hipStream_t st);
+hipError_t launch_paged_few(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 16 or 32
+
+// blocks of 32 elements that hold a head: those for which there is a kernel
+inline int blocks_of(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 96 ? 3 : head_dim <= 128 ? 4 : head_dim <= 192 ? 6 : 8; }
+
+namespace {
+
+__device__ __attribute__((aligned(16))) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
+
+// n / group for 0 <= n < 2^31, by a product with the reciprocal rounded up to 32 bits: group_mul = ceil(2^(31 + b) / group),
+// 2^(b - 1) < group <= 2^b, is too large by less than 1 / 2^31 of itself.
+__device__ __forceinline__ int by_group(const PagedArgs& g, int n) {
+    return g.group == 1 ? n : (int)(__umulhi((uint32_t)n, g.group_mul) >> g.group_shift);
+}
+
+// ---- a tile: ROWS consecutive rows (token, head of the group) of one request -------------------------------------------
+// Request r has rows (q_start[r + 1] - q_start[r]) * group for each key head.  Its tiles are the slots from
+// q_start[r] * group / ROWS + r on: that leaves room for each request's last, partly filled one without a sum over the requests,
+// at the price of slots that stay empty.
+struct Tile {
+    int r;               // request, -1: an empty slot
+    int start;           // the request's first row of q
+    int first, count;    // first row and number of rows
+    int p0, p1;          // positions of the first and the last row's token
+    int lo, hi;          // the keys that any of its rows sees: [lo, hi), lo rounded down to a multiple of 64
+};
+
+__device__ __forceinline__ int clamp_rows(int start, const jx_attend_args& a) { return min(max(start, 0), (int)a.n_tokens); }
+
+template <int ROWS>
+__device__ __forceinline__ int first_slot(int start, int r, const PagedArgs& g) {
+    return (int)((long long)clamp_rows(start, g.a) * g.group / ROWS) + r;
+}
+
+template <int ROWS>
+__device__ __forceinline__ Tile make_tile(const PagedArgs& g, int r, int slot, int start, int end, int len) {
+    Tile t;
+    const int b = clamp_rows(start, g.a), e = clamp_rows(end, g.a);
+    t.start = b;
+    t.first = (slot - first_slot<ROWS>(start, r, g)) * ROWS;
+    t.count = min((e - b) * g.group - t.first, ROWS);
+    t.r = t.count > 0 && t.first >= 0 ? r : -1;
+    if (t.r < 0) t.count = t.first = 1;
+    const int p = max(len, 0) - (e - b);  // n_tokens is below 2^29
+    t.p0 = p + by_group(g, t.first);
+    t.p1 = p + by_group(g, t.first + t.count - 1);
+    const int hi = min(t.p1 + 1, g.a.table_pages << g.page_shift);
+    const int lo = g.a.window && t.p0 >= g.a.window ? t.p0 + 1 - g.a.window : 0;
+    t.lo = hi > lo ? lo & ~63 : 0;
+    t.hi = hi > lo ? hi : 0;
+    return t;
+}
+
+// The last of 0 .. n - 1 for which before() holds (it holds for all up to that one; 0 if for none), by all lanes of a wavefront
+template <typename Before>
+__device__ __forceinline__ int last_before(int n, Before before) {
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, at = lane_id() * step;
+        const int k = max(__popcll(ballot(at < n && before(lo + min(at, n - 1)))) - 1, 0);
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// ---- rows of keys and values in LDS ------------------------------------------------------------------------------------
+// A row is CH chunks of 16 bytes; chunk c of row r lies at place c ^ mix(r).  The matrix instructions' operands are read as the
+// same chunk of 32 consecutive keys (K) and as four consecutive rows of 16 or 32 elements (V, transposed on the way); mix
+// spreads both over the banks: any 8 and any 16 consecutive rows (8 chunks: half as many places) get different places, and so
+// do rows r .. r + 3 beside pairs and quadruples of neighbouring chunks.
+template <int CH>
+__device__ __forceinline__ constexpr int mix(int r) {
+    return CH == 8 ? (r & 1) * 2 ^ (r >> 1 & 1) * 4 ^ (r >> 2 & 1) ^ (r >> 3 & 1) * 2
+                   : (r & 1) * 6 ^ (r >> 1 & 1) * 12 ^ (r >> 2 & 1) ^ (r >> 3 & 1) * 2;
+}
+
+typedef __attribute__((address_space(3))) char* lds_ptr;
+
+__device__ __forceinline__ void load_lds16(const void* from, lds_ptr to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// Element e of row r (of 32) among the sums that a wavefront leaves for join_kernel; elements 4 i .. 4 i + 3 are together
+__device__ __forceinline__ int part_at(int r, int e) { return ((e >> 3) * 64 + r + (e >> 2 & 1) * 32) * 4 + (e & 3); }
+constexpr int part_floats(int nb) { return nb * 1024 + 64; }
+
+// ---- tiles shared out ---------------------------------------------------------------------------------------------------
+// All tiles of all key heads, UNIT keys of one a unit, are cut into equal shares, one for each workgroup, whatever the lengths of the
+// requests are; where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its share for itself: from the
+// first rows and lengths of all requests (8 bytes each) it counts the units of every slot and adds them up in LDS.  With more than MAX_SLOTS
+// slots there are tiles enough, and each is a workgroup's.
+constexpr int UNIT = 64;
+
+struct Segment {  // units u0 .. u1 - 1 of the tile's
+    Tile t;
+    int u0, u1, units;
+    __device__ __forceinline__ bool whole() const { return u0 == 0 && u1 == units; }
+};
+
+__host__ __device__ inline size_t shares_bytes(int n_req, int slots) { return (size_t)(n_req + 1) * 8 + (size_t)(slots + 1) * 4 + (size_t)slots * 2; }
+
+__device__ __forceinline__ int units_of(const Tile& t) { return max((t.hi - t.lo + UNIT - 1) / UNIT, 1); }  // results have to be written
+
+struct Shares {
+    int *starts, *lens;  // [n_req + 1]
+    int* cum;            // [slots + 1] units before each slot
+    uint16_t* req;       // [slots]
+    // Units x0 .. x1 - 1 are this workgroup's.  The first `rem` shares are `each` + 1 units, the others `each`; the launch has seen to it that
+    // there are less than 2^31 in all.
+    uint32_t x0, x1, per_head, each, rem;
+    int head, work;
+
+    // false: nothing to do
+    template <int ROWS, int THREADS>
+    __device__ __forceinline__ bool begin(const PagedArgs& g, int* lds) {
+        const jx_attend_args& a = g.a;
+        const int tid = threadIdx.x, lane = lane_id();
+        x0 = 0;
+        x1 = 1;
+        if (!g.n_work) {
+            head = (int)(blockIdx.x % a.n_kv_heads);
+            work = g.slots - 1 - (int)(blockIdx.x / a.n_kv_heads);  // the slot: long ones first where there is one request
+            return true;
+        }
+        starts = lds;
+        lens = starts + a.n_req + 1;
+        cum = lens + a.n_req + 1;
+        req = (uint16_t*)(cum + g.slots + 1);
+        for (int i = tid; i <= a.n_req; i += THREADS) {
+            starts[i] = a.d_q_start[i];
+            lens[i] = i < a.n_req ? a.d_kv_len[i] : 0;
+        }
+        __syncthreads();
+        for (int s = tid; s < g.slots; s += THREADS) {
+            int lo = 0, hi = a.n_req;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (first_slot<ROWS>(starts[mid], mid, g) <= s) lo = mid;
+                else hi = mid;
+            }
+            const Tile t = make_tile<ROWS>(g, lo, s, starts[lo], starts[lo + 1], lens[lo]);
+            cum[s + 1] = t.r < 0 ? 0 : units_of(t);
+            req[s] = (uint16_t)lo;
+        }
+        if (tid == 0) cum[0] = 0;
+        __syncthreads();
+        if (tid < 64) {
+            int carry = 0;
+            for (int s0 = 0; s0 < g.slots; s0 += 64) {
+                int v = s0 + lane < g.slots ? cum[s0 + lane + 1] : 0;
+                for (int d = 1; d < 64; d *= 2) {
+                    const int o = __shfl_up(v, d, 64);
+                    if (lane >= d) v += o;
+                }
+                if (s0 + lane < g.slots) cum[s0 + lane + 1] = carry + v;
+                carry += __shfl(v, 63, 64);
+            }
+        }
+        __syncthreads();
+        per_head = __builtin_amdgcn_readfirstlane(cum[g.slots]);
+        const uint32_t all = per_head * a.n_kv_heads, shares = min((uint32_t)g.n_work, all);  // none is empty
+        // consecutive shares stay on one XCD's cache; few are spread over all
+        work = all < (uint32_t)g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8);
+        if (tid == 0) g.joins[work].pieces = 0;
+        if ((uint32_t)work >= shares) return false;
+        each = all / shares;
+        rem = all - each * shares;
+        x0 = work * each + min((uint32_t)work, rem);
+        x1 = x0 + each + ((uint32_t)work < rem);
+        head = (int)(x0 / per_head);
+        return true;
+    }
+
+    // The segment that begins with unit x0
+    template <int ROWS>
+    __device__ __forceinline__ Segment next(const PagedArgs& g) {
+        const jx_attend_args& a = g.a;
+        Segment e;
+        if (!g.n_work) {
+            const int r = last_before(a.n_req, [&](int i) { return first_slot<ROWS>(a.d_q_start[i], i, g) <= work; });
+            e.t = make_tile<ROWS>(g, r, work, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
+            e.u0 = 0;
+            e.u1 = e.units = e.t.r < 0 ? 1 : units_of(e.t);
+            x1 = x0 + e.units;
+            return e;
+        }
+        if (x0 >= (head + 1) * per_head) head++;
+        const int at = (int)(x0 - head * per_head);
+        const int slot = last_before(g.slots, [&](int i) { return cum[i] <= at; });
+        e.u0 = at - cum[slot];
+        e.units = cum[slot + 1] - cum[slot];
+        e.u1 = (int)min((uint32_t)e.units, e.u0 + (x1 - x0));
+        const int r = req[slot];
+        e.t = make_tile<ROWS>(g, r, slot, starts[r], starts[r + 1], lens[r]);
+        return e;
+    }
+
+    // Where this workgroup leaves its part of a tile
+    __device__ __forceinline__ float* part(const PagedArgs& g, bool first, int nb) const {
+        return g.part + (size_t)(2 * work + first) * g.part_rows * part_floats(nb);
+    }
+
+    // The first of the workgroups that share a tile says who they are
+    __device__ __forceinline__ void name(const PagedArgs& g, const Segment& e) const {
+        const uint32_t end = x0 + e.units - 1, large = rem * (each + 1);  // the tile's last unit, and whose it is
+        const int last = (int)(end < large ? end / (each + 1) : rem + (end - large) / each);
+        g.joins[work] = {last - work + 1, head, e.t.first, e.t.count, e.t.start, {0, 0, 0}};
+    }
+};
+
+// Rows that belong to no request: zeros and -infinity, by workgroups `block` of `blocks`
+template <typename T>
+__device__ void clear_rows(const jx_attend_args& a, int block, int blocks) {
+    const int n = (int)a.n_tokens, b = a.n_req ? clamp_rows(a.d_q_start[0], a) : n, e = a.n_req ? clamp_rows(a.d_q_start[a.n_req], a) : n;
+    const int chunks = a.n_heads * (a.head_dim / 8), outside = b + max(n - max(b, e), 0);
+    for (int i = block; i < outside; i += blocks) {
+        const long long t = i < b ? i : i - b + max(b, e);
+        for (int c = threadIdx.x; c < chunks; c += 256) ((uint4*)a.d_out)[t * chunks + c] = make_uint4(0, 0, 0, 0);
+        if (a.d_lse)
+            for (int h = threadIdx.x; h < a.n_heads; h += 256) a.d_lse[t * a.n_heads + h] = -INFINITY;
+    }
+}
+
+}  // namespace
+
+}  // namespace jx

@@ -417,9 +417,16 @@ def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
         block = torch.empty(3 * n_tokens + 2 * n + 2, dtype=_I32, device=lens.device)
         slot, pos, q_start, kv_len, left = block.split((2 * n_tokens, n_tokens, n + 1, n, 1))
         out = KvPlan(q_start, kv_len, pos, slot.view(_I64), left)
+        p_slot = block.data_ptr()
+        p_pos = p_slot + 8 * n_tokens
+        p_start = p_pos + 4 * n_tokens
+        p_len = p_start + 4 * (n + 1)
+        p_left = p_len + 4 * n
+    else:
+        p_left, p_start, p_len = _array(out.n_free, _I32, 1), _array(out.q_start, _I32, n + 1), _array(out.kv_len, _I32, n)
+        p_pos, p_slot = _array(out.pos, _I32, n_tokens), _array(out.slot, _I64, n_tokens)
     _run(_lib.jx_kv_plan, lens.device, _array(lens, _I32, n), _array(new, _I32, n), n, page, _array(table, _I32, n, w), w,
-         _array(free, _I32, f), _array(n_free, _I32, 1), f, _array(out.n_free, _I32, 1), _array(out.q_start, _I32, n + 1),
-         _array(out.kv_len, _I32, n), _array(out.pos, _I32, n_tokens), _array(out.slot, _I64, n_tokens), n_tokens)
+         _array(free, _I32, f), _array(n_free, _I32, 1), f, p_left, p_start, p_len, p_pos, p_slot, n_tokens)
     return out
 
 
@@ -439,16 +446,27 @@ def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_wei
     dt = q.dtype
     if out is None:
         out = torch.empty((t, h, d), dtype=dt, device=q.device)
+    else:
+        _array(out, dt, t, h, d)
     n_pos, half = cos.shape if cos is not None else (0x7FFFFFFF, 0)
     assert k.shape == v.shape == (t, kv, d)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     a = RopeArgs(_HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, dt), _rows(k, dt), _rows(v, dt), qs[0], qs[1], ks[0],
                  ks[1], vs[0], vs[1], _array(q_weight, dt, d) if q_weight is not None else None,
                  _array(k_weight, dt, d) if k_weight is not None else None, eps, _array(cos, _F32, n_pos, half) if half else None,
-                 _array(sin, _F32, n_pos, half) if half else None, _array(pos, _I32, t), _array(slot, _I64, t), _array(out, dt, t, h, d),
+                 _array(sin, _F32, n_pos, half) if half else None, _array(pos, _I32, t), _array(slot, _I64, t), out.data_ptr(),
                  _kv_cache(k_cache, v_cache, dt, d))
     _run(_lib.jx_qk_norm_rope, q.device, C.byref(a))
     return out
+
+
+def _outputs(out, q, t, h, d):
+    """The pair to write into, made here if there is none, and its pointers."""
+    if out is None:
+        o, lse = torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device)
+        return o, lse, o.data_ptr(), lse.data_ptr()
+    o, lse = out
+    return o, lse, _array(o, q.dtype, t, h, d), _array(lse, _F32, t, h) if lse is not None else None
 
 
 def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
@@ -457,18 +475,20 @@ def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0
     t, h, d = q.shape
     n, w = table.shape
     dt = q.dtype
-    o, lse = out if out is not None else (torch.empty((t, h, d), dtype=dt, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device))
+    o, lse, p_out, p_lse = _outputs(out, q, t, h, d)
     qs = q.stride()
     a = AttendArgs(_HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, dt, d),
-                   _array(table, _I32, n, w), w, n, _array(q_start, _I32, n + 1), _array(kv_len, _I32, n), scale, window,
-                   _array(o, dt, t, h, d), _array(lse, _F32, t, h) if lse is not None else None)
+                   _array(table, _I32, n, w), w, n, _array(q_start, _I32, n + 1), _array(kv_len, _I32, n), scale, window, p_out, p_lse)
     ref = C.byref(a)
     if work is None:
         nbytes = _lib.jx_paged_attention_bytes(ref)
         if nbytes < 0:
             _check(int(nbytes))
         work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _run(_lib.jx_paged_attention, q.device, ref, _array(work, torch.uint8, *work.shape), work.numel())
+    else:
+        nbytes = work.shape[0]
+        _array(work, torch.uint8, nbytes)
+    _run(_lib.jx_paged_attention, q.device, ref, work.data_ptr(), nbytes)
     return o, lse
 
 
@@ -479,12 +499,12 @@ def found_attention(q, keys, values, ids, scale, part=None, out=None):
     n, kv, kd = keys.shape
     k = ids.shape[2]
     dt = q.dtype
-    o, lse = out if out is not None else (torch.empty((t, h, d), dtype=dt, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device))
+    o, lse, p_out, p_lse = _outputs(out, q, t, h, d)
     qs, ks = q.stride(), keys.stride()
     assert kd == d and values.shape == keys.shape and values.stride() == ks
     a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, dt), qs[0], qs[1], _rows(keys, dt), _rows(values, dt), ks[0], ks[1], n,
                   _array(ids, _I32, t, h, k), k, scale, _array(part[0], dt, t, h, d) if part else None,
-                  _array(part[1], _F32, t, h) if part else None, _array(o, dt, t, h, d), _array(lse, _F32, t, h) if lse is not None else None)
+                  _array(part[1], _F32, t, h) if part else None, p_out, p_lse)
     _run(_lib.jx_found_attention, q.device, C.byref(a))
     return o, lse
 
