@@ -5,81 +5,72 @@ namespace jx {
 
 namespace {
 
-// The parts of a tile that several workgroups shared, as one: the tile that workgroup blockIdx.x began and did not end.
-// blockIdx.y: which 32 elements.  A wavefront takes 32 rows, as their lanes held them when the parts were written; of a tile of few
-// rows the wavefronts share out the pieces.  Bound: the time that a chain of reads takes, hence PIECES at once.
+// The parts of a tile that several shares cut, as one: the tile that share blockIdx.x began and did not end; blockIdx.y: which 32 rows.
+// A wavefront takes 32 elements, as its lanes held them when the parts were written, and of few rows two or four pieces side by side.
+// Bound: the time that a chain of reads takes, hence PIECES at once.  Most shares began no such tile; their workgroups end at once.
 template <typename T, int NB>
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs g) {
+__global__ __launch_bounds__(NB * 64) void join_kernel(PagedArgs g) {
     constexpr int PIECES = 4;
-    __shared__ float others[4][18][64];
     const jx_attend_args& a = g.a;
-    const Join j = g.joins[blockIdx.x];
-    if (!j.pieces) return;
-    const int work = (int)blockIdx.x, d = a.head_dim, lane = lane_id(), wave = (int)(threadIdx.x >> 6), b = (int)blockIdx.y;
-    const int groups = j.count <= 32 ? 1 : j.count <= 64 ? 2 : 4;  // of rows
-    const int row = wave % groups * 32 + (lane & 31);
+    const int work = (int)blockIdx.x, lane = lane_id(), b = (int)(threadIdx.x >> 6), d = a.head_dim;
+    const Join j = g.joins[work];
+    const int count = j.pieces ? j.count - (int)blockIdx.y * 32 : 0;
+    if (count <= 0 || b * 32 >= d) return;
+    const int wide = count <= 8 ? 16 : count <= 16 ? 32 : 64, side = 64 / wide;  // lanes of a piece, pieces side by side
+    const int row = lane & (wide / 2 - 1), half = lane / (wide / 2) & 1;
+    const float* parts = g.part + blockIdx.y * part_floats(NB);
+    const int to_s = b * 1024 + (row + 32 * half) * 4, to_m = NB * 1024 + row;
     float m = -INFINITY, l = 0.0f;
     f32x4 s[4];
-    for (int i = 0; i < 4; i++) s[i] = (f32x4)0.0f;
-    if (row < j.count) {
-        const float* parts = g.part + (wave % groups) * part_floats(NB) + lane * 4 + b * 1024;
-        const int to_m = NB * 1024 - b * 1024 - lane * 4 + (lane & 31);
-        for (int i0 = wave / groups; i0 < j.pieces; i0 += PIECES * (4 / groups)) {
-            float pm[PIECES], pl[PIECES], top = m;
-            f32x4 y[PIECES][4];
-            for (int u = 0; u < PIECES; u++) {
-                const int i = min(i0 + u * (4 / groups), j.pieces - 1);
-                const float* p = parts + (size_t)(2 * (work + i) + (i == 0)) * g.part_rows * part_floats(NB);
-                pm[u] = p[to_m];
-                pl[u] = p[to_m + 32];
-                for (int k = 0; k < 4; k++) y[u][k] = *(const f32x4*)(p + k * 256);
-            }
-            for (int u = 0; u < PIECES; u++) {
-                if (i0 + u * (4 / groups) >= j.pieces) pm[u] = -INFINITY;
-                top = fmaxf(top, pm[u]);
-            }
-            const float base = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - base);
-            m = top;
-            l *= keep;
-            for (int k = 0; k < 4; k++)
-                for (int e = 0; e < 4; e++) s[k][e] *= keep;
-            for (int u = 0; u < PIECES; u++) {
-                if (pm[u] == -INFINITY) continue;  // nothing, or not a piece
-                const float w = __builtin_amdgcn_exp2f(pm[u] - base);
-                l = fmaf(pl[u], w, l);
-                for (int k = 0; k < 4; k++)
-                    for (int e = 0; e < 4; e++) s[k][e] = fmaf(y[u][k][e], w, s[k][e]);
-            }
+    for (int k = 0; k < 4; k++) s[k] = (f32x4)0.0f;
+    for (int i0 = lane / wide; i0 < j.pieces; i0 += PIECES * side) {
+        float pm[PIECES], pl[PIECES], top = m;
+        f32x4 y[PIECES][4];
+        for (int u = 0; u < PIECES; u++) {
+            const int i = min(i0 + u * side, j.pieces - 1);
+            const float* p = parts + (size_t)(2 * (work + i) + (i == 0)) * g.part_rows * part_floats(NB);
+            pm[u] = p[to_m];
+            pl[u] = p[to_m + 32];
+            for (int k = 0; k < 4; k++) y[u][k] = *(const f32x4*)(p + to_s + k * 256);
         }
-    }
-    if (groups < 4) {
-        others[wave][16][lane] = m;
-        others[wave][17][lane] = l;
-        for (int i = 0; i < 16; i++) others[wave][i][lane] = s[i >> 2][i & 3];
-        __syncthreads();
-        if (wave >= groups) return;
-        float top = m;
-        for (int w = wave + groups; w < 4; w += groups) top = fmaxf(top, others[w][16][lane]);
+        for (int u = 0; u < PIECES; u++) {
+            if (i0 + u * side >= j.pieces) pm[u] = -INFINITY;
+            top = fmaxf(top, pm[u]);
+        }
         const float base = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - base);
         m = top;
         l *= keep;
-        for (int i = 0; i < 16; i++) s[i >> 2][i & 3] *= keep;
-        for (int w = wave + groups; w < 4; w += groups) {
-            const float f = __builtin_amdgcn_exp2f(others[w][16][lane] - base);
-            l = fmaf(others[w][17][lane], f, l);
-            for (int i = 0; i < 16; i++) s[i >> 2][i & 3] = fmaf(others[w][i][lane], f, s[i >> 2][i & 3]);
+        for (int k = 0; k < 4; k++)
+            for (int e = 0; e < 4; e++) s[k][e] *= keep;
+        for (int u = 0; u < PIECES; u++) {
+            const float w = __builtin_amdgcn_exp2f(pm[u] - base);
+            const bool counts = pm[u] != -INFINITY;  // else nothing, or not a piece
+            l = counts ? fmaf(pl[u], w, l) : l;
+            for (int k = 0; k < 4; k++)
+                for (int e = 0; e < 4; e++) s[k][e] = counts ? fmaf(y[u][k][e], w, s[k][e]) : s[k][e];
         }
     }
-    if (row >= j.count) return;
-    const int rr = j.first + row, token = by_group(g, rr);
+    float top = m;
+    for (int x = wide; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const float keep = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    l *= keep;
+    for (int k = 0; k < 4; k++)
+        for (int e = 0; e < 4; e++) s[k][e] *= keep;
+    for (int x = wide; x < 64; x *= 2) {
+        l += __shfl_xor(l, x, 64);
+        for (int k = 0; k < 4; k++)
+            for (int e = 0; e < 4; e++) s[k][e] += __shfl_xor(s[k][e], x, 64);
+    }
+    if (lane >= wide || row >= count) return;
+    const int rr = j.first + (int)blockIdx.y * 32 + row, token = by_group(g, rr);
     const long long o = (j.start + (long long)token) * a.n_heads + j.head * g.group + rr - token * g.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     for (int k = 0; k < 4; k++) {
-        const int e = b * 32 + k * 8 + (lane >> 5) * 4;
+        const int e = b * 32 + k * 8 + half * 4;
         for (int i = 0; i < 4; i++) s[k][i] *= inv;
         if (e < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + e) = __builtin_convertvector(s[k], typename Vec<T>::x4);
     }
-    if (b == 0 && lane < 32 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (b == 0 && half == 0 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 struct Plan {
@@ -98,8 +89,9 @@ Plan make_plan(const jx_attend_args& a) {
     p.part_rows = p.rows == 128 ? 4 : 1;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
-    // as many workgroups as the card holds at a time
-    if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) p.n_work = a.head_dim <= (p.rows == 128 ? 128 : 64) ? 512 : 256;
+    // as many shares as the card holds workgroups or wavefronts at a time
+    const int per_cu = p.rows == 128 ? (a.head_dim <= 128 ? 2 : 1) : FEW_WAVES(nb) * (nb <= 2 ? 2 : 1);
+    if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) p.n_work = 256 * per_cu;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
     p.joins = up((int64_t)2 * p.n_work * p.part_rows * part_floats(nb) * 4);
     p.total = p.joins + up((int64_t)p.n_work * sizeof(Join));
@@ -108,14 +100,13 @@ Plan make_plan(const jx_attend_args& a) {
 
 template <typename T>
 void join(const PagedArgs& g, hipStream_t st) {
-    const int nb = blocks_of(g.a.head_dim);
-    const dim3 grid(g.n_work, (g.a.head_dim + 31) / 32);
-    switch (nb) {
-        case 2: join_kernel<T, 2><<<grid, 256, 0, st>>>(g); break;
-        case 3: join_kernel<T, 3><<<grid, 256, 0, st>>>(g); break;
-        case 4: join_kernel<T, 4><<<grid, 256, 0, st>>>(g); break;
-        case 6: join_kernel<T, 6><<<grid, 256, 0, st>>>(g); break;
-        default: join_kernel<T, 8><<<grid, 256, 0, st>>>(g);
+    const dim3 grid(g.n_work, g.part_rows);
+    switch (blocks_of(g.a.head_dim)) {
+        case 2: join_kernel<T, 2><<<grid, 2 * 64, 0, st>>>(g); break;
+        case 3: join_kernel<T, 3><<<grid, 3 * 64, 0, st>>>(g); break;
+        case 4: join_kernel<T, 4><<<grid, 4 * 64, 0, st>>>(g); break;
+        case 6: join_kernel<T, 6><<<grid, 6 * 64, 0, st>>>(g); break;
+        default: join_kernel<T, 8><<<grid, 8 * 64, 0, st>>>(g);
     }
 }
 

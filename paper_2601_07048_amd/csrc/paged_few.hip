@@ -34,17 +34,21 @@ __device__ __forceinline__ void wait_loads() {  // until at most the N latest ar
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// The largest of two pairs of 16-bit values
+__device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 // S^T = K Q^T and O^T += V^T P^T as for many rows, by 16x16x32 matrix instructions.  Bound: the bytes of keys and values.  So every
-// wavefront is a reader of its own: it takes 32 keys at a time, K straight into registers, V into its own two places in LDS (where
-// its transposed form is read), the next ones on their way while these are worked on, and nobody waits for another until the
-// segment's end, where the wavefronts' sums are added up.
+// wavefront is a reader of its own, with a share of its own: it takes 32 keys at a time, K straight into registers, V into its own two
+// places in LDS (where its transposed form is read), the next ones on their way while these are worked on, and never waits for
+// another.  Four wavefronts of a workgroup that took a tile's keys in turn lost a fifth of the time where they met at its end.
 template <typename T, int NC, int RB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     constexpr int ROWS = RB * 16, KEYS = 32, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32, PITCH = CH * 16, TILE = KEYS * PITCH;
-    constexpr int NV = KEYS * CH / 64, NK = 2 * NC, OB = 2 * NC, THREADS = WAVES * 64;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];  // [WAVES][2] values, later their sums; shares
-    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS];
-    __shared__ int odd_values;  // values that are not finite where not every row looks
+    constexpr int NV = KEYS * CH / 64, NK = 2 * NC, OB = 2 * NC;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];  // [WAVES][2] values; shares
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, h = lane >> 4, d = a.head_dim;
@@ -54,7 +58,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         return;
     }
     Shares sh;
-    if (!sh.begin<ROWS, THREADS>(g, (int*)(lds + WAVES * 2 * TILE))) return;
+    if (!sh.begin<ROWS, WAVES>(g, (int*)(lds + WAVES * 2 * TILE), wave)) return;
 
     const int page_mask = a.cache.page - 1;
     const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     const uint32_t v_row = lane / CH * token_chunks * 16, v_chunk = lane % CH ^ mix<CH>(lane / CH);
     auto v_off = [&](int i) {
         const uint32_t chunk = v_chunk ^ mix<CH>(i * (64 / CH) & 15);
-        return v_row + (CH == OB * 2 ? chunk : min(chunk, (uint32_t)d / 8 - 1)) * 16;
+        return v_row + min(chunk, (uint32_t)d / 8 - 1) * 16;
     };
     const int vr = 4 * h + (r16 >> 2), v_at = vr * PITCH + ((r16 >> 1 & 1) ^ mix<CH>(vr)) * 16 + (r16 & 1) * 8;
 
@@ -82,26 +86,6 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         const char* vb = (const char*)a.cache.d_v + head * a.cache.head_stride * 2;
         const int32_t* table = a.d_table + (size_t)t.r * a.table_pages;
         const __attribute__((address_space(4))) int32_t* table_s = (const __attribute__((address_space(4))) int32_t*)table;
-
-        int pos[RB];
-        s16x8 q[RB][NC];
-        for (int b = 0; b < RB; b++) {
-            const int row = b * 16 + r16, rr = t.first + min(row, t.count - 1), token = by_group(g, rr), hq = head * g.group + rr - token * g.group;
-            pos[b] = t.p0 + token - by_group(g, t.first);
-            const T* from = (const T*)a.d_q + (long long)(t.start + token) * a.q_token_stride + hq * a.q_head_stride + h * 8;
-            for (int i = 0; i < NC; i++) {
-                uint4 w = i * 32 + h * 8 < d && row < t.count ? *(const uint4*)(from + i * 32) : make_uint4(0, 0, 0, 0);
-                w = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
-                q[b][i] = __builtin_bit_cast(s16x8, w);
-            }
-        }
-        f32x4 o[RB][OB];
-        float m[RB], l[RB];
-        for (int b = 0; b < RB; b++) {
-            m[b] = -INFINITY;
-            l[b] = 0.0f;
-            for (int i = 0; i < OB; i++) o[b][i] = (f32x4)0.0f;
-        }
 
         // Keys key .. key + 15 lie in one page (a page has at least 16 tokens, and key is a multiple of 16); scalar reads
         struct Pages {
@@ -134,12 +118,39 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                     load_lds16_at(from, i * (64 / CH) < rows ? v_off(i) : OUTSIDE, (i - b * NV / 2) * (64 / CH) * 16 * token_chunks, to + i * 1024);
             }
         };
-        bool odd = false;
+        Pages here = pages_at(key0), next = pages_at(key0 + KEYS);
+        load_keys(key0, here);
+        load_values(key0, here, mine);
+
+        auto row_of = [&](int row) {
+            const int rr = t.first + min(row, t.count - 1), token = by_group(g, rr);
+            return RowAt{row < t.count, head * g.group + rr - token * g.group, t.start + token, t.p0 + token - by_group(g, t.first)};
+        };
+        int pos[RB];
+        s16x8 q[RB][NC];
+        for (int b = 0; b < RB; b++) {
+            const RowAt row = row_of(b * 16 + r16);
+            pos[b] = row.pos;
+            const T* from = (const T*)a.d_q + (long long)row.token * a.q_token_stride + row.head * a.q_head_stride + h * 8;
+            for (int i = 0; i < NC; i++) {
+                uint4 w = i * 32 + h * 8 < d && row.mine ? *(const uint4*)(from + i * 32) : make_uint4(0, 0, 0, 0);
+                w = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
+                q[b][i] = __builtin_bit_cast(s16x8, w);
+            }
+        }
+        f32x4 o[RB][OB];
+        float m[RB], l[RB];
+        for (int b = 0; b < RB; b++) {
+            m[b] = -INFINITY;
+            l[b] = 0.0f;
+            for (int i = 0; i < OB; i++) o[b][i] = (f32x4)0.0f;
+        }
+        uint32_t worst = 0;  // the largest pair of values, signs aside, where not every row looks
         // 32 keys; while they are worked on the next ones are on their way, the keys into the registers that the scores have been made of,
         // the values into the other place.  The compiler has to know that this is another: it would wait for it.
-        auto work_on = [&](auto more, int key, const Pages& here, int next_key, const Pages& next, const lds_ptr __restrict v,
+        auto work_on = [&](auto more, int key, const Pages& here, const Pages& next, const lds_ptr __restrict v,
                            const lds_ptr __restrict next_v) __attribute__((always_inline)) {
-            if (more) load_values(next_key, next, next_v);
+            if (more) load_values(key + KEYS, next, next_v);
             f32x4 s[RB][2];
             for (int b = 0; b < RB; b++)
                 for (int x = 0; x < 2; x++) s[b][x] = (f32x4)0.0f;
@@ -147,17 +158,18 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                 for (int x = 0; x < 2; x++)
                     for (int b = 0; b < RB; b++) s[b][x] = mul16<T>(k[x][i], q[b][i], s[b][x]);
             __builtin_amdgcn_sched_barrier(0);
-            if (more) load_keys(next_key, next);
+            if (more) load_keys(key + KEYS, next);
             // what is not seen, and the weights
             const bool all = key + KEYS <= key1 && there(here.id[0]) && there(here.id[1]) && key + KEYS - 1 <= t.p0 && (!a.window || key > t.p1 - a.window);
             s16x8 p[RB];
             for (int b = 0; b < RB; b++) {
-                if (!all)
-                    for (int x = 0; x < 2; x++)
-                        for (int i = 0; i < 4; i++) {
-                            const int at = key + x * 16 + 4 * h + i;
-                            if (at > pos[b] || at >= key1 || (a.window && at <= pos[b] - a.window) || !there(here.id[x])) s[b][x][i] = -INFINITY;
-                        }
+                if (!all) {
+                    const int last = min(pos[b], key1 - 1) - key - 4 * h, first = a.window ? max(pos[b] + 1 - a.window - key, 0) - 4 * h : -4 * h;
+                    for (int x = 0; x < 2; x++) {
+                        const int most = there(here.id[x]) ? last - x * 16 : INT_MIN;
+                        for (int i = 0; i < 4; i++) s[b][x][i] = i <= most && i >= first - x * 16 ? s[b][x][i] : -INFINITY;
+                    }
+                }
                 float top = -INFINITY;
                 for (int i = 0; i < 8; i += 2) top = fmaxf(fmaxf(top, s[b][i >> 2][i & 3]), s[b][i >> 2][(i & 3) + 1]);
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -179,15 +191,6 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             }
             if (more) wait_loads<NV + NK>();
             else wait_loads<0>();
-            if (!all && t.count > 1) {
-                uint32_t worst = 0;
-                for (int i = lane * 16; i < TILE; i += 1024) {
-                    if ((i % PITCH / 16 ^ mix<CH>(i / PITCH & 15)) * 8 >= d) continue;  // behind the head's end
-                    const s16x4 y0 = *(const __attribute__((address_space(3))) s16x4*)(v + i), y1 = *(const __attribute__((address_space(3))) s16x4*)(v + i + 8);
-                    for (int j = 0; j < 4; j++) worst = max(worst, max((uint32_t)(y0[j] & 0x7FFF), (uint32_t)(y1[j] & 0x7FFF)));
-                }
-                odd |= ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
-            }
             s16x8 y[OB];
             for (int i = 0; i < OB; i++) {
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (i * 32))));
@@ -195,123 +198,97 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                 y[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             }
             __builtin_amdgcn_sched_barrier(0);
+            if (!all)
+                for (int i = 0; i < OB; i++) {
+                    const uint4 w = __builtin_bit_cast(uint4, y[i]);
+                    worst = max_pairs(worst, max_pairs(max_pairs(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), max_pairs(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu)));
+                }
             for (int i = 0; i < OB; i++)
                 for (int b = 0; b < RB; b++) o[b][i] = mul16<T>(y[i], p[b], o[b][i]);
             __builtin_amdgcn_sched_barrier(0);  // the place has been read before it is filled again
         };
-        int key = key0 + wave * KEYS, buf = 0;
-        if (key < key1) {
-            constexpr int STEP = WAVES * KEYS;
-            Pages here = pages_at(key), next = pages_at(key + STEP);
-            load_keys(key, here);
-            load_values(key, here, mine);
-            for (; key + STEP < key1; key += STEP, buf ^= TILE) {
-                const Pages then = pages_at(key + 2 * STEP);
-                work_on(std::true_type{}, key, here, key + STEP, next, mine + buf, mine + (buf ^ TILE));
+        if (key0 < key1) {
+            int key = key0, buf = 0;
+            for (; key + KEYS < key1; key += KEYS, buf ^= TILE) {
+                const Pages then = pages_at(key + 2 * KEYS);
+                work_on(std::true_type{}, key, here, next, mine + buf, mine + (buf ^ TILE));
                 here = next;
                 next = then;
             }
-            work_on(std::false_type{}, key, here, 0, next, mine + buf, mine + (buf ^ TILE));
+            work_on(std::false_type{}, key, here, next, mine + buf, mine + (buf ^ TILE));
+        } else {
+            wait_loads<0>();  // what was on its way for a tile without keys
         }
 
-        // The wavefronts' sums as one
-        if (tid == 0) odd_values = 0;
-        for (int b = 0; b < RB; b++) {
-            l[b] += __shfl_xor(l[b], 16, 64);
-            l[b] += __shfl_xor(l[b], 32, 64);
-            if (h == 0) {
-                wave_m[wave][b * 16 + r16] = m[b];
-                wave_l[wave][b * 16 + r16] = l[b];
-            }
-        }
-        __syncthreads();
-        if (odd && lane == 0) odd_values = 1;
-        f32x4* sums = (f32x4*)lds;  // [RB][WAVES][OB][64]
-        for (int b = 0; b < RB; b++) {
-            float top = -INFINITY;
-            for (int w = 0; w < WAVES; w++) top = fmaxf(top, wave_m[w][b * 16 + r16]);
-            const float keep = __builtin_amdgcn_exp2f(m[b] - (top == -INFINITY ? 0.0f : top));
-            for (int i = 0; i < OB; i++) {
-                f32x4 y = o[b][i];
-                for (int j = 0; j < 4; j++) y[j] *= keep;
-                sums[((b * WAVES + wave) * OB + i) * 64 + lane] = y;
-            }
-        }
-        __syncthreads();
         const bool whole = e.whole();
         float* part = NULL;
         if (!whole) {
             part = sh.part(g, e.u0 == 0, NC);
-            if (e.u0 == 0 && tid == 0) sh.name(g, e);
+            if (e.u0 == 0 && lane == 0) sh.name(g, e);
         }
-        if (!odd_values) {
-            for (int i = tid; i < RB * OB * 64; i += THREADS) {
-                const int b = i / (OB * 64), j = i % (OB * 64), row = b * 16 + (j & 15), el = j / 64 * 16 + (j >> 4 & 3) * 4;
-                if (row >= t.count) continue;
-                f32x4 y = sums[b * WAVES * OB * 64 + j];
-                for (int w = 1; w < WAVES; w++)
-                    for (int x = 0; x < 4; x++) y[x] += sums[(b * WAVES + w) * OB * 64 + j][x];
-                float top = -INFINITY, sum = 0.0f;
-                for (int w = 0; w < WAVES; w++) top = fmaxf(top, wave_m[w][row]);
-                for (int w = 0; w < WAVES; w++) sum += wave_l[w][row] * __builtin_amdgcn_exp2f(wave_m[w][row] - (top == -INFINITY ? 0.0f : top));
+        constexpr uint32_t ODD = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;  // infinities and what is not a number
+        if (!ballot((worst & 0xFFFF) >= ODD || worst >> 16 >= ODD)) {
+            for (int b = 0; b < RB; b++) {
+                float sum = l[b] + __shfl_xor(l[b], 16, 64);
+                sum += __shfl_xor(sum, 32, 64);
+                const RowAt row = row_of(b * 16 + r16);
+                if (!row.mine) continue;
                 if (whole) {
-                    const int rr = t.first + row, token = by_group(g, rr);
-                    const long long out = (long long)(t.start + token) * a.n_heads + head * g.group + rr - token * g.group;
                     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    for (int x = 0; x < 4; x++) y[x] *= inv;
-                    if (el < d) *(typename Vec<T>::x4*)((T*)a.d_out + out * d + el) = __builtin_convertvector(y, typename Vec<T>::x4);
-                    if (el == 0 && a.d_lse) a.d_lse[out] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
-                } else {
-                    *(f32x4*)(part + part_at(row, el)) = y;
-                    if (el == 0) {
-                        part[NC * 1024 + row] = top;
-                        part[NC * 1024 + 32 + row] = sum;
+                    const long long at = (long long)row.token * a.n_heads + row.head;
+                    T* out = (T*)a.d_out + at * d + h * 4;
+                    for (int i = 0; i < OB; i++) {
+                        f32x4 w = o[b][i];
+                        for (int j = 0; j < 4; j++) w[j] *= inv;
+                        if (i * 16 + h * 4 < d) *(typename Vec<T>::x4*)(out + i * 16) = __builtin_convertvector(w, typename Vec<T>::x4);
                     }
+                    if (h == 0 && a.d_lse) a.d_lse[at] = sum == 0.0f ? -INFINITY : (m[b] + __builtin_amdgcn_logf(sum)) * LN2;
+                } else {
+                    for (int i = 0; i < OB; i++) *(f32x4*)(part + part_at(b * 16 + r16, i * 16 + h * 4)) = o[b][i];
+                    if (h < 2) part[NC * 1024 + h * 32 + b * 16 + r16] = h ? sum : m[b];
                 }
             }
         } else {
             // A weight of 0 times such a value is not 0: these rows are done again, key by key
             const int c8 = lane % CH * 8;
-            for (int row = wave; row < t.count; row += WAVES) {
-                const int rr = t.first + row, token = by_group(g, rr), hq = head * g.group + rr - token * g.group;
-                const int p = t.p0 + token - by_group(g, t.first);
-                f32x8 y = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (c8 < d) y = load8((const T*)a.d_q + (long long)(t.start + token) * a.q_token_stride + hq * a.q_head_stride + c8);
-                for (int i = 0; i < 8; i++) y[i] *= a.scale * LOG2E;
-                const int k0 = a.window ? max(key0, p + 1 - a.window) : key0, k1 = min(key1, p + 1);
-                Softmax s = walk_keys<T, CH>((const T*)kb, (const T*)vb, y, c8 < d, k0, k1, [&](long long at) {
+            for (int i = 0; i < t.count; i++) {
+                const RowAt row = row_of(i);
+                f32x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (c8 < d) x = load8((const T*)a.d_q + (long long)row.token * a.q_token_stride + row.head * a.q_head_stride + c8);
+                for (int j = 0; j < 8; j++) x[j] *= a.scale * LOG2E;
+                const int k0 = a.window ? max(key0, row.pos + 1 - a.window) : key0, k1 = min(key1, row.pos + 1);
+                Softmax s = walk_keys<T, CH>((const T*)kb, (const T*)vb, x, c8 < d, k0, k1, [&](long long at) {
                     const int id = table[at >> g.page_shift];
                     return there(id) ? (long long)row_at(id, (int)at) / 2 : -1ll;
                 });
                 s = gather<CH>(s);
-                const long long out = (long long)(t.start + token) * a.n_heads + hq;
+                const long long out = (long long)row.token * a.n_heads + row.head;
                 if (whole) {
                     const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
-                    for (int i = 0; i < 8; i++) s.acc[i] *= inv;
+                    for (int j = 0; j < 8; j++) s.acc[j] *= inv;
                     if (lane < CH && c8 < d) store8((T*)a.d_out + out * d + c8, s.acc);
                     if (lane == 0 && a.d_lse) a.d_lse[out] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * LN2;
                 } else {
                     if (lane < CH && c8 < d)
-                        for (int i = 0; i < 8; i++) part[part_at(row, c8 + i)] = s.acc[i];
+                        for (int j = 0; j < 8; j++) part[part_at(i, c8 + j)] = s.acc[j];
                     if (lane == 0) {
-                        part[NC * 1024 + row] = s.m;
-                        part[NC * 1024 + 32 + row] = s.l;
+                        part[NC * 1024 + i] = s.m;
+                        part[NC * 1024 + 32 + i] = s.l;
                     }
                 }
             }
         }
-        __syncthreads();  // before the next segment's values and sums
         sh.x0 += e.u1 - e.u0;
     }
 }
 
 template <typename T, int NC, int RB>
 hipError_t launch(const PagedArgs& g, hipStream_t st) {
-    constexpr int WAVES = NC <= 4 ? 8 : 4, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32;
+    constexpr int WAVES = FEW_WAVES(NC), CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32;
     const size_t lds = WAVES * 2 * 32 * CH * 16 + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
     static const hipError_t set = hipFuncSetAttribute((const void*)paged_few_kernel<T, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
     if (set != hipSuccess) return set;
-    const unsigned blocks = (g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
+    const unsigned shares = g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads), blocks = (shares + WAVES - 1) / WAVES + CLEARERS;
     paged_few_kernel<T, NC, RB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();
 }

@@ -138,12 +138,6 @@ __device__ __forceinline__ bool odd_values_in(lds_ptr v, int bytes) {
     return ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
 }
 
-// A lane's row: whether there is one, its query head, its token's row of q, its position
-struct RowAt {
-    bool mine;
-    int head, token, pos;
-};
-
 template <typename T, int NB>
 __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_many_kernel(PagedArgs g) {
     typedef Rows32<T, NB> R;
@@ -159,7 +153,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_many_kernel(PagedA
     }
     const lds_ptr ring = (lds_ptr)lds;
     Shares sh;
-    if (!sh.begin<ROWS, 256>(g, (int*)(lds + 4 * TILE))) return;
+    if (!sh.begin<ROWS, 1>(g, (int*)(lds + 4 * TILE), 0)) return;
 
     const int d = a.head_dim, page_mask = a.cache.page - 1;
     if (d < R::CH * 8)  // what lies behind a key meets zeros of the queries, so it has to be a number

@@ -10,7 +10,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
 constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys; of more there are enough without
 
-// A tile that several workgroups share: parts 2 work + 1 of the first of them, 2 work of the pieces - 1 that follow.  0 pieces: none
+// A tile that several shares cut: parts 2 work + 1 of the first of them, 2 work of the pieces - 1 that follow.  0 pieces: none
 struct __attribute__((aligned(16))) Join {
     int pieces, head, first, count;  // of the tile: key head, first row and number of rows
     int start, unused[3];            // of the request: its first row of q
@@ -21,7 +21,7 @@ struct PagedArgs {
     int page_shift, group;  // group: query heads of a key head
     uint32_t group_mul, group_shift;  // see by_group
     int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
-    int slots, n_work;      // tiles at most; workgroups that share them, 0 = a workgroup a tile
+    int slots, n_work;      // tiles at most; shares of them, 0 = a share a tile
     int part_rows;          // tiles' rows / 32
     float* part;            // [2 n_work][part_rows]: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
                             // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
@@ -30,6 +30,9 @@ struct PagedArgs {
 
 hipError_t launch_paged_many(const PagedArgs& g, hipStream_t st);
 hipError_t launch_paged_few(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 16 or 32
+
+// wavefronts of a workgroup that takes few rows, by blocks of 32 elements: as many as have room for their values in LDS
+constexpr int FEW_WAVES(int nb) { return nb <= 4 ? 8 : 4; }
 
 // blocks of 32 elements that hold a head: those for which there is a kernel
 inline int blocks_of(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 96 ? 3 : head_dim <= 128 ? 4 : head_dim <= 192 ? 6 : 8; }
@@ -117,8 +120,8 @@ __device__ __forceinline__ int part_at(int r, int e) { return ((e >> 3) * 64 + r
 constexpr int part_floats(int nb) { return nb * 1024 + 64; }
 
 // ---- tiles shared out ---------------------------------------------------------------------------------------------------
-// All tiles of all key heads, UNIT keys of one a unit, are cut into equal shares, one for each workgroup, whatever the lengths of the
-// requests are; where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its share for itself: from the
+// All tiles of all key heads, UNIT keys of one a unit, are cut into equal shares, whatever the lengths of the requests are, one for each
+// workgroup (many rows) or wavefront (few); where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its share for itself: from the
 // first rows and lengths of all requests (8 bytes each) it counts the units of every slot and adds them up in LDS.  With more than MAX_SLOTS
 // slots there are tiles enough, and each is a workgroup's.
 constexpr int UNIT = 64;
@@ -140,19 +143,21 @@ struct Shares {
     // Units x0 .. x1 - 1 are this workgroup's.  The first `rem` shares are `each` + 1 units, the others `each`; the launch has seen to it that
     // there are less than 2^31 in all.
     uint32_t x0, x1, per_head, each, rem;
-    int head, work;
+    int head, slot, work;
 
-    // false: nothing to do
-    template <int ROWS, int THREADS>
-    __device__ __forceinline__ bool begin(const PagedArgs& g, int* lds) {
+    // For share `sub` of PER shares of the workgroup, by all of it.  false: nothing to do
+    template <int ROWS, int PER>
+    __device__ __forceinline__ bool begin(const PagedArgs& g, int* lds, int sub) {
+        const int THREADS = (int)blockDim.x;
         const jx_attend_args& a = g.a;
         const int tid = threadIdx.x, lane = lane_id();
         x0 = 0;
         x1 = 1;
         if (!g.n_work) {
-            head = (int)(blockIdx.x % a.n_kv_heads);
-            work = g.slots - 1 - (int)(blockIdx.x / a.n_kv_heads);  // the slot: long ones first where there is one request
-            return true;
+            const uint32_t i = blockIdx.x * PER + sub;
+            head = (int)(i % a.n_kv_heads);
+            slot = g.slots - 1 - (int)(i / a.n_kv_heads);  // long ones first where there is one request
+            return slot >= 0;
         }
         starts = lds;
         lens = starts + a.n_req + 1;
@@ -192,14 +197,15 @@ struct Shares {
         per_head = __builtin_amdgcn_readfirstlane(cum[g.slots]);
         const uint32_t all = per_head * a.n_kv_heads, shares = min((uint32_t)g.n_work, all);  // none is empty
         // consecutive shares stay on one XCD's cache; few are spread over all
-        work = all < (uint32_t)g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8);
-        if (tid == 0) g.joins[work].pieces = 0;
+        work = all < (uint32_t)g.n_work ? sub * (g.n_work / PER) + (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8) * PER + sub;
+        if (PER == 1 ? tid == 0 : lane == 0) g.joins[work].pieces = 0;
         if ((uint32_t)work >= shares) return false;
         each = all / shares;
         rem = all - each * shares;
         x0 = work * each + min((uint32_t)work, rem);
         x1 = x0 + each + ((uint32_t)work < rem);
         head = (int)(x0 / per_head);
+        slot = -1;
         return true;
     }
 
@@ -209,16 +215,25 @@ struct Shares {
         const jx_attend_args& a = g.a;
         Segment e;
         if (!g.n_work) {
-            const int r = last_before(a.n_req, [&](int i) { return first_slot<ROWS>(a.d_q_start[i], i, g) <= work; });
-            e.t = make_tile<ROWS>(g, r, work, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
+            const int r = last_before(a.n_req, [&](int i) { return first_slot<ROWS>(a.d_q_start[i], i, g) <= slot; });
+            e.t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
             e.u0 = 0;
             e.u1 = e.units = e.t.r < 0 ? 1 : units_of(e.t);
             x1 = x0 + e.units;
             return e;
         }
-        if (x0 >= (head + 1) * per_head) head++;
+        if (x0 >= (head + 1) * per_head) {
+            head++;
+            slot = -1;
+        }
         const int at = (int)(x0 - head * per_head);
-        const int slot = last_before(g.slots, [&](int i) { return cum[i] <= at; });
+        if (slot < 0 && at) {
+            slot = last_before(g.slots, [&](int i) { return cum[i] <= at; });
+        } else {
+            do slot++;
+            while (cum[slot + 1] <= at);
+        }
+        slot = __builtin_amdgcn_readfirstlane(slot);
         e.u0 = at - cum[slot];
         e.units = cum[slot + 1] - cum[slot];
         e.u1 = (int)min((uint32_t)e.units, e.u0 + (x1 - x0));
@@ -227,17 +242,23 @@ struct Shares {
         return e;
     }
 
-    // Where this workgroup leaves its part of a tile
+    // Where this share's part of a tile is left
     __device__ __forceinline__ float* part(const PagedArgs& g, bool first, int nb) const {
         return g.part + (size_t)(2 * work + first) * g.part_rows * part_floats(nb);
     }
 
-    // The first of the workgroups that share a tile says who they are
+    // The first of the shares that cut a tile says who they are
     __device__ __forceinline__ void name(const PagedArgs& g, const Segment& e) const {
         const uint32_t end = x0 + e.units - 1, large = rem * (each + 1);  // the tile's last unit, and whose it is
         const int last = (int)(end < large ? end / (each + 1) : rem + (end - large) / each);
         g.joins[work] = {last - work + 1, head, e.t.first, e.t.count, e.t.start, {0, 0, 0}};
     }
+};
+
+// A lane's row: whether there is one, its query head, its token's row of q, its position
+struct RowAt {
+    bool mine;
+    int head, token, pos;
 };
 
 // Rows that belong to no request: zeros and -infinity, by workgroups `block` of `blocks`
@@ -247,9 +268,9 @@ __device__ void clear_rows(const jx_attend_args& a, int block, int blocks) {
     const int chunks = a.n_heads * (a.head_dim / 8), outside = b + max(n - max(b, e), 0);
     for (int i = block; i < outside; i += blocks) {
         const long long t = i < b ? i : i - b + max(b, e);
-        for (int c = threadIdx.x; c < chunks; c += 256) ((uint4*)a.d_out)[t * chunks + c] = make_uint4(0, 0, 0, 0);
+        for (int c = threadIdx.x; c < chunks; c += blockDim.x) ((uint4*)a.d_out)[t * chunks + c] = make_uint4(0, 0, 0, 0);
         if (a.d_lse)
-            for (int h = threadIdx.x; h < a.n_heads; h += 256) a.d_lse[t * a.n_heads + h] = -INFINITY;
+            for (int h = threadIdx.x; h < a.n_heads; h += blockDim.x) a.d_lse[t * a.n_heads + h] = -INFINITY;
     }
 }
 

@@ -152,6 +152,20 @@ def test_what_a_row_does_not_see_has_no_part_in_it(heads, kv, dim, bad):
             cache[page, place] = keep
 
 
+@pytest.mark.parametrize("heads,kv", [(1, 1), (8, 2), (40, 2)])
+@pytest.mark.parametrize("dim", [64, 128, 200])
+def test_single_tokens_do_not_see_what_has_left_their_window(heads, kv, dim):
+    """Before the window, behind the length and in pages that the table does not name there may be anything."""
+    p = Paged(BF, heads, kv, dim, 16, [150, 75, 33, 16], [1] * 4, seed=dim)
+    want = p.want(window=20)
+    for r, n in enumerate((150, 75, 33, 16)):
+        for j in range(n - 20):
+            page, place = int(p.table[r, j // 16]), j % 16
+            p.k[page, place] = math.inf if j % 2 else math.nan
+            p.v[page, place] = math.nan if j % 3 else -math.inf
+    plain.check(p.run(window=20), want)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
 def test_values_that_are_infinite_reach_the_rows_that_see_them(dtype):
     p = Paged(dtype, 4, 2, 64, 16, [50], [20], seed=4)
