@@ -90,7 +90,7 @@ Plan make_plan(const jx_attend_args& a) {
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
     // as many shares as the card holds workgroups or wavefronts at a time
-    const int per_cu = p.rows == 128 ? (a.head_dim <= 128 ? 2 : 1) : FEW_WAVES(nb) * (nb <= 2 ? 2 : 1);
+    const int per_cu = p.rows == 128 ? MANY_PER_CU(nb) : FEW_WAVES(nb) * (nb <= 2 ? 2 : 1);
     if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) p.n_work = 256 * per_cu;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
     p.joins = up((int64_t)2 * p.n_work * p.part_rows * part_floats(nb) * 4);

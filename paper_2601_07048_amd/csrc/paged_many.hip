@@ -64,8 +64,16 @@ struct Rows32 {
 
     // The first tile's scores
     __device__ __forceinline__ void scores(lds_ptr k, f32x16 (&s)[2]) {
+        constexpr int N = 4 * NB, AHEAD = 6;
+        s16x8 kf[AHEAD];
         for (int kb = 0; kb < 2; kb++) s[kb] = (f32x16)0.0f;
-        for (int i = 0; i < 4 * NB; i++) s[i & 1] = Mfma<T>::mul(keys_at(k, i), q[i / 2], s[i & 1]);
+        for (int i = 0; i < AHEAD; i++) kf[i] = keys_at(k, i);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            s[i & 1] = Mfma<T>::mul(kf[i % AHEAD], q[i / 2], s[i & 1]);
+            if (i + AHEAD < N) kf[i % AHEAD] = keys_at(k, i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         largest(s);
     }
 
@@ -139,7 +147,7 @@ __device__ __forceinline__ bool odd_values_in(lds_ptr v, int bytes) {
 }
 
 template <typename T, int NB>
-__global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void paged_many_kernel(PagedArgs g) {
+__global__ __launch_bounds__(256, MANY_PER_CU(NB)) void paged_many_kernel(PagedArgs g) {
     typedef Rows32<T, NB> R;
     constexpr int ROWS = 128, KEYS = UNIT, TILE = KEYS * R::PITCH;
     constexpr int LOADS = KEYS * R::CH / 256;
