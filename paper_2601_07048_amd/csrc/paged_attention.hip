@@ -74,7 +74,7 @@ __global__ __launch_bounds__(NB * 64) void join_kernel(PagedArgs g) {
 }
 
 struct Plan {
-    int rows;  // of a tile: 16, 32: few rows, 128: many
+    int rows;  // of a tile: 16, 32: few rows, 128, 256: many
     int slots, n_work, part_rows;
     int64_t joins, total;  // bytes before the joins, in all
 };
@@ -85,12 +85,12 @@ Plan make_plan(const jx_attend_args& a) {
     const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
     // few rows: those of 16 neighbouring keys have to lie in one page
     const bool pages = a.cache.page >= 16 && a.cache.token_stride < (1 << 25);
-    p.rows = pages && rows <= 16ll * a.n_req ? 16 : pages && rows <= 32ll * a.n_req ? 32 : 128;
-    p.part_rows = p.rows == 128 ? 4 : 1;
+    p.rows = pages && rows <= 16ll * a.n_req ? 16 : pages && rows <= 32ll * a.n_req ? 32 : nb <= 4 && rows >= 512ll * a.n_req ? 256 : 128;
+    p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
     // as many shares as the card holds workgroups or wavefronts at a time
-    const int per_cu = p.rows == 128 ? MANY_PER_CU(nb) : FEW_WAVES(nb) * (nb <= 2 ? 2 : 1);
+    const int per_cu = p.rows >= 128 ? MANY_PER_CU(nb, p.rows) : FEW_WAVES(nb) * (nb <= 2 ? 2 : 1);
     if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) p.n_work = 256 * per_cu;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
     p.joins = up((int64_t)2 * p.n_work * p.part_rows * part_floats(nb) * 4);
@@ -122,7 +122,7 @@ hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStr
     const uint32_t mul = (uint32_t)(((1ull << (31 + bits)) + group - 1) / group);
     const PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.n_work, p.part_rows, (float*)work,
                          (Join*)(work + p.joins)};
-    hipError_t e = p.rows == 128 ? launch_paged_many(g, st) : launch_paged_few(g, p.rows, st);
+    hipError_t e = p.rows >= 128 ? launch_paged_many(g, p.rows, st) : launch_paged_few(g, p.rows, st);
     if (e != hipSuccess || !p.n_work) return e;
     if (a.dtype == JX_BF16) join<__bf16>(g, st);
     else join<_Float16>(g, st);

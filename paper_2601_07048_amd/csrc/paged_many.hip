@@ -29,7 +29,7 @@ __device__ __forceinline__ float both_halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// ---- many rows: four wavefronts of 32 rows each over the same keys ------------------------------------------------------
+// ---- many rows: four or eight wavefronts of 32 rows each over the same keys ---------------------------------------------
 // S^T = K Q^T, 64 keys by 32 rows at a time, so that a lane holds 32 scores of one row (the other lane with that row, 32 further on,
 // the rest); then O^T += V^T P^T, where the scores' registers are already the second operand of the matrix instruction if the keys
 // of the first are taken in the same order.  The running maximum moves only when a row's scores rise by more than 2^8 over it:
@@ -53,7 +53,7 @@ struct Rows32 {
     }
 
     __device__ __forceinline__ s16x8 keys_at(lds_ptr k, int i) const {  // operand i of 4 NB: 32 keys by 16 elements
-        return *(const __attribute__((address_space(3))) s16x8*)(k + (k_at ^ (i / 2 * 32)) + i % 2 * 32 * PITCH);
+        return *(const __attribute__((address_space(3))) s16x8*)(k + (k_at ^ (i % (2 * NB) * 32)) + i / (2 * NB) * 32 * PITCH);
     }
     __device__ __forceinline__ s16x8 values_at(lds_ptr v, int i) const {  // operand i of 4 NB: 32 elements by 16 keys
         const int x = i / NB, b = i % NB;
@@ -70,7 +70,7 @@ struct Rows32 {
         for (int i = 0; i < AHEAD; i++) kf[i] = keys_at(k, i);
 #pragma unroll
         for (int i = 0; i < N; i++) {
-            s[i & 1] = Mfma<T>::mul(kf[i % AHEAD], q[i / 2], s[i & 1]);
+            s[i / (2 * NB)] = Mfma<T>::mul(kf[i % AHEAD], q[i % (2 * NB)], s[i / (2 * NB)]);
             if (i + AHEAD < N) kf[i % AHEAD] = keys_at(k, i + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -100,13 +100,13 @@ struct Rows32 {
     __device__ __forceinline__ void advance(const f32x16 (&s)[2], f32x16 (&next)[2], lds_ptr k, lds_ptr v, float c) {
         constexpr int N = 4 * NB, AHEAD = 3;  // matrix instructions of each half, with 32 / N scores each
         const float base = m == -INFINITY ? 0.0f : m;
-        next[0] = next[1] = (f32x16)0.0f;
         s16x8 kf[AHEAD], vf[AHEAD], p[4];
         float w[8], sum = 0.0f;
         for (int i = 0; i < AHEAD; i++) kf[i] = keys_at(k, i);
 #pragma unroll
         for (int i = 0; i < N; i++) {
-            next[i & 1] = Mfma<T>::mul(kf[i % AHEAD], q[i / 2], next[i & 1]);
+            f32x16& to = next[i / (2 * NB)];  // the second half takes the registers that the first half's weights have left
+            to = Mfma<T>::mul(kf[i % AHEAD], q[i % (2 * NB)], i % (2 * NB) ? to : (f32x16)0.0f);
             if (i + AHEAD < N) kf[i % AHEAD] = keys_at(k, i + AHEAD);
             else vf[i + AHEAD - N] = values_at(v, i + AHEAD - N);
 #pragma unroll
@@ -146,11 +146,11 @@ __device__ __forceinline__ bool odd_values_in(lds_ptr v, int bytes) {
     return ballot(worst >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u)) != 0;
 }
 
-template <typename T, int NB>
-__global__ __launch_bounds__(256, MANY_PER_CU(NB)) void paged_many_kernel(PagedArgs g) {
+template <typename T, int NB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel(PagedArgs g) {
     typedef Rows32<T, NB> R;
-    constexpr int ROWS = 128, KEYS = UNIT, TILE = KEYS * R::PITCH;
-    constexpr int LOADS = KEYS * R::CH / 256;
+    constexpr int ROWS = WAVES * 32, THREADS = WAVES * 64, KEYS = UNIT, TILE = KEYS * R::PITCH;
+    constexpr int LOADS = KEYS * R::CH / THREADS;
     extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2] keys, [2] values; slots' sums of units, their requests
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -164,8 +164,8 @@ __global__ __launch_bounds__(256, MANY_PER_CU(NB)) void paged_many_kernel(PagedA
     if (!sh.begin<ROWS, 1>(g, (int*)(lds + 4 * TILE), 0)) return;
 
     const int d = a.head_dim, page_mask = a.cache.page - 1;
-    if (d < R::CH * 8)  // what lies behind a key meets zeros of the queries, so it has to be a number
-        for (int i = tid; i < 2 * TILE / 16; i += 256) *(uint4*)(lds + i * 16) = make_uint4(0, 0, 0, 0);
+    if (d < R::CH * 8)  // what lies behind a head meets zeros of the queries, so it has to be a number
+        for (int i = tid; i < 4 * TILE / 16; i += THREADS) *(uint4*)(lds + i * 16) = make_uint4(0, 0, 0, 0);
     const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
     const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);  // a scale of 0 has to leave -infinity what it is
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256, MANY_PER_CU(NB)) void paged_many_kernel(PagedA
         // rows of this wavefront
         R x;
         x.begin();
-        const int rows0 = ((wave + work) & 3) * 32;  // tiles of few rows: the workgroups of a CU keep different SIMDs busy
+        const int rows0 = ((wave + work) & (WAVES - 1)) * 32;  // tiles of few rows: the workgroups of a CU keep different SIMDs busy
         const bool busy = rows0 < t.count;
         auto row_of = [&](int of_lane) {
             const int row = rows0 + (of_lane & 31), rr = t.first + min(row, t.count - 1), token = by_group(g, rr);
@@ -218,21 +218,21 @@ __global__ __launch_bounds__(256, MANY_PER_CU(NB)) void paged_many_kernel(PagedA
         auto stage = [&](const char* from, int key, int ids, lds_ptr to) {
             if (g.near && !ballot(ids < 0)) {
                 for (int i = 0; i < LOADS; i++) {
-                    const int at = i * (256 / R::CH) + wave * (64 / R::CH), odd = (i & 1) * mix<R::CH>(256 / R::CH);
+                    const int at = i * (THREADS / R::CH) + wave * (64 / R::CH), odd = mix<R::CH>(i * (THREADS / R::CH) & 15);
                     const uint64_t row = row_at(__builtin_amdgcn_readlane(ids, at), key + at);
                     const uint32_t off = lane_row + (lane_chunk ^ odd) * 16;
-                    if (d == R::CH * 8) load_lds16(from + row * 16 + off, to + (i * 256 + wave * 64) * 16);
+                    if (d == R::CH * 8) load_lds16(from + row * 16 + off, to + (i * THREADS + wave * 64) * 16);
                     else if ((lane_chunk ^ odd) * 8 < d)  // the other places are never written: see above
-                        load_lds16(from + row * 16 + off, to + (i * 256 + wave * 64) * 16);
+                        load_lds16(from + row * 16 + off, to + (i * THREADS + wave * 64) * 16);
                 }
                 return;
             }
             const uint64_t rows = row_at(max(ids, 0), key + lane);
 #pragma unroll 1
             for (int i = 0; i < LOADS; i++) {
-                const int at = i * (256 / R::CH) + tid / R::CH, chunk = tid % R::CH ^ mix<R::CH>(at);
+                const int at = i * (THREADS / R::CH) + tid / R::CH, chunk = tid % R::CH ^ mix<R::CH>(at);
                 const char* p = from + ((uint64_t)shfl64((long long)rows, at) + chunk) * 16;
-                load_lds16(__shfl(ids, at, 64) >= 0 && chunk * 8 < d ? p : (const char*)zero_chunk, to + (i * 256 + wave * 64) * 16);
+                load_lds16(__shfl(ids, at, 64) >= 0 && chunk * 8 < d ? p : (const char*)zero_chunk, to + (i * THREADS + wave * 64) * 16);
             }
         };
         // One tile's weights and values, the next one's scores; the keys after that and the next values on their way into the places that
@@ -358,32 +358,33 @@ __global__ __launch_bounds__(256, MANY_PER_CU(NB)) void paged_many_kernel(PagedA
     }
 }
 
-template <typename T, int NB>
+template <typename T, int NB, int WAVES>
 hipError_t launch(const PagedArgs& g, hipStream_t st) {
-    constexpr int TILE = 64 * Rows32<T, NB>::PITCH;
+    constexpr int TILE = UNIT * Rows32<T, NB>::PITCH;
     const size_t lds = 4 * TILE + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
-    static const hipError_t set = hipFuncSetAttribute((const void*)paged_many_kernel<T, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    static const hipError_t set = hipFuncSetAttribute((const void*)paged_many_kernel<T, NB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (set != hipSuccess) return set;
     const unsigned blocks = (g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
-    paged_many_kernel<T, NB><<<blocks, 256, lds, st>>>(g);
+    paged_many_kernel<T, NB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_dim(const PagedArgs& g, hipStream_t st) {
+hipError_t launch_dim(const PagedArgs& g, int rows, hipStream_t st) {
+    const bool wide = rows == 256;
     switch (blocks_of(g.a.head_dim)) {
-        case 2: return launch<T, 2>(g, st);
-        case 3: return launch<T, 3>(g, st);
-        case 4: return launch<T, 4>(g, st);
-        case 6: return launch<T, 6>(g, st);
+        case 2: return wide ? launch<T, 2, 8>(g, st) : launch<T, 2, 4>(g, st);
+        case 3: return wide ? launch<T, 3, 8>(g, st) : launch<T, 3, 4>(g, st);
+        case 4: return wide ? launch<T, 4, 8>(g, st) : launch<T, 4, 4>(g, st);
+        case 6: return launch<T, 6, 4>(g, st);
     }
-    return launch<T, 8>(g, st);
+    return launch<T, 8, 4>(g, st);
 }
 
 }  // namespace
 
-hipError_t launch_paged_many(const PagedArgs& g, hipStream_t st) {
-    return g.a.dtype == JX_BF16 ? launch_dim<__bf16>(g, st) : launch_dim<_Float16>(g, st);
+hipError_t launch_paged_many(const PagedArgs& g, int rows, hipStream_t st) {
+    return g.a.dtype == JX_BF16 ? launch_dim<__bf16>(g, rows, st) : launch_dim<_Float16>(g, rows, st);
 }
 
 }  // namespace jx

@@ -28,14 +28,14 @@ struct PagedArgs {
     Join* joins;            // [n_work]
 };
 
-hipError_t launch_paged_many(const PagedArgs& g, hipStream_t st);
+hipError_t launch_paged_many(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 128, or 256 up to 128 elements
 hipError_t launch_paged_few(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 16 or 32
 
 // wavefronts of a workgroup that takes few rows, by blocks of 32 elements: as many as have room for their values in LDS
 constexpr int FEW_WAVES(int nb) { return nb <= 4 ? 8 : 4; }
 
 // workgroups for many rows that a CU holds, by their registers
-constexpr int MANY_PER_CU(int nb) { return nb <= 4 ? 2 : 1; }
+constexpr int MANY_PER_CU(int nb, int rows) { return nb <= 4 && rows == 128 ? 2 : 1; }
 
 // blocks of 32 elements that hold a head: those for which there is a kernel
 inline int blocks_of(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 96 ? 3 : head_dim <= 128 ? 4 : head_dim <= 192 ? 6 : 8; }
