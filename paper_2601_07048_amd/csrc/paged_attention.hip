@@ -5,33 +5,36 @@ namespace jx {
 
 namespace {
 
-// The parts of a tile that several shares cut, as one: the tile that share blockIdx.x began and did not end; blockIdx.y: which 32 rows.
-// A wavefront takes 32 elements, as its lanes held them when the parts were written, and of few rows two or four pieces side by side.
-// Bound: the time that a chain of reads takes, hence PIECES at once.  Most shares began no such tile; their workgroups end at once.
+// Elements of a tile's rows that a wavefront joins: up to eight or sixteen wavefronts for all of them
+constexpr int JOIN_ELEMENTS(int nb) { return nb <= 4 ? 8 : 16; }
+
+// The parts of a tile whose keys several workgroups share, as one: the tile that workgroup blockIdx.x began and did not end;
+// blockIdx.y: which 32 rows.  A wavefront takes 8 or 16 elements, as the lanes held them when the parts were written, and of few rows
+// two or four pieces side by side.  Bound: the time that a chain of reads takes, hence PIECES at once.
 template <typename T, int NB>
-__global__ __launch_bounds__(NB * 64) void join_kernel(PagedArgs g) {
-    constexpr int PIECES = 4;
+__global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(PagedArgs g) {
+    constexpr int PIECES = 8, K = JOIN_ELEMENTS(NB) / 8;
     const jx_attend_args& a = g.a;
-    const int work = (int)blockIdx.x, lane = lane_id(), b = (int)(threadIdx.x >> 6), d = a.head_dim;
-    const Join j = g.joins[work];
+    const int lane = lane_id(), e0 = (int)(threadIdx.x >> 6) * JOIN_ELEMENTS(NB), d = a.head_dim;
+    const Join j = g.joins[blockIdx.x];
     const int count = j.pieces ? j.count - (int)blockIdx.y * 32 : 0;
-    if (count <= 0 || b * 32 >= d) return;
+    if (count <= 0 || e0 >= d) return;
     const int wide = count <= 8 ? 16 : count <= 16 ? 32 : 64, side = 64 / wide;  // lanes of a piece, pieces side by side
     const int row = lane & (wide / 2 - 1), half = lane / (wide / 2) & 1;
     const float* parts = g.part + blockIdx.y * part_floats(NB);
-    const int to_s = b * 1024 + (row + 32 * half) * 4, to_m = NB * 1024 + row;
+    const int to_s = part_at(row, e0 + half * 4), to_m = NB * 1024 + row;
     float m = -INFINITY, l = 0.0f;
-    f32x4 s[4];
-    for (int k = 0; k < 4; k++) s[k] = (f32x4)0.0f;
+    f32x4 s[K];
+    for (int k = 0; k < K; k++) s[k] = (f32x4)0.0f;
     for (int i0 = lane / wide; i0 < j.pieces; i0 += PIECES * side) {
         float pm[PIECES], pl[PIECES], top = m;
-        f32x4 y[PIECES][4];
+        f32x4 y[PIECES][K];
         for (int u = 0; u < PIECES; u++) {
             const int i = min(i0 + u * side, j.pieces - 1);
-            const float* p = parts + (size_t)(2 * (work + i) + (i == 0)) * g.part_rows * part_floats(NB);
+            const float* p = parts + (size_t)(2 * (blockIdx.x + i) + (i == 0)) * g.part_rows * part_floats(NB);
             pm[u] = p[to_m];
             pl[u] = p[to_m + 32];
-            for (int k = 0; k < 4; k++) y[u][k] = *(const f32x4*)(p + to_s + k * 256);
+            for (int k = 0; k < K; k++) y[u][k] = *(const f32x4*)(p + to_s + k * 256);
         }
         for (int u = 0; u < PIECES; u++) {
             if (i0 + u * side >= j.pieces) pm[u] = -INFINITY;
@@ -40,13 +43,13 @@ __global__ __launch_bounds__(NB * 64) void join_kernel(PagedArgs g) {
         const float base = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - base);
         m = top;
         l *= keep;
-        for (int k = 0; k < 4; k++)
+        for (int k = 0; k < K; k++)
             for (int e = 0; e < 4; e++) s[k][e] *= keep;
         for (int u = 0; u < PIECES; u++) {
             const float w = __builtin_amdgcn_exp2f(pm[u] - base);
             const bool counts = pm[u] != -INFINITY;  // else nothing, or not a piece
             l = counts ? fmaf(pl[u], w, l) : l;
-            for (int k = 0; k < 4; k++)
+            for (int k = 0; k < K; k++)
                 for (int e = 0; e < 4; e++) s[k][e] = counts ? fmaf(y[u][k][e], w, s[k][e]) : s[k][e];
         }
     }
@@ -54,28 +57,28 @@ __global__ __launch_bounds__(NB * 64) void join_kernel(PagedArgs g) {
     for (int x = wide; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 64));
     const float keep = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
     l *= keep;
-    for (int k = 0; k < 4; k++)
+    for (int k = 0; k < K; k++)
         for (int e = 0; e < 4; e++) s[k][e] *= keep;
     for (int x = wide; x < 64; x *= 2) {
         l += __shfl_xor(l, x, 64);
-        for (int k = 0; k < 4; k++)
+        for (int k = 0; k < K; k++)
             for (int e = 0; e < 4; e++) s[k][e] += __shfl_xor(s[k][e], x, 64);
     }
     if (lane >= wide || row >= count) return;
     const int rr = j.first + (int)blockIdx.y * 32 + row, token = by_group(g, rr);
     const long long o = (j.start + (long long)token) * a.n_heads + j.head * g.group + rr - token * g.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    for (int k = 0; k < 4; k++) {
-        const int e = b * 32 + k * 8 + half * 4;
+    for (int k = 0; k < K; k++) {
+        const int e = e0 + k * 8 + half * 4;
         for (int i = 0; i < 4; i++) s[k][i] *= inv;
         if (e < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + e) = __builtin_convertvector(s[k], typename Vec<T>::x4);
     }
-    if (b == 0 && half == 0 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * LN2;
+    if (e0 == 0 && half == 0 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 struct Plan {
     int rows;  // of a tile: 16, 32: few rows, 128, 256: many
-    int slots, n_work, part_rows;
+    int slots, groups, n_work, part_rows;
     int64_t joins, total;  // bytes before the joins, in all
 };
 
@@ -85,29 +88,35 @@ Plan make_plan(const jx_attend_args& a) {
     const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
     // few rows: those of 16 neighbouring keys have to lie in one page
     const bool pages = a.cache.page >= 16 && a.cache.token_stride < (1 << 25);
-    p.rows = pages && rows <= 16ll * a.n_req ? 16 : pages && rows <= 32ll * a.n_req ? 32 : nb <= 4 && rows >= 512ll * a.n_req ? 256 : 128;
+    p.rows = pages && rows <= 16ll * a.n_req ? 16 : pages && rows <= 32ll * a.n_req ? 32 : nb <= 4 && rows >= (a.n_req == 1 ? 512 : 2048ll * a.n_req) ? 256 : 128;
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
-    // as many shares as the card holds workgroups or wavefronts at a time
-    const int per_cu = p.rows >= 128 ? MANY_PER_CU(nb, p.rows) : FEW_WAVES(nb) * (nb <= 2 ? 2 : 1);
-    if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) p.n_work = 256 * per_cu;
+    // as many shares as the card holds workgroups (many rows) or wavefronts (few) at a time
+    if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) {
+        p.groups = 256 * (p.rows >= 128 ? MANY_PER_CU(nb, p.rows) : nb <= 2 ? 2 : 1);
+        p.n_work = p.rows >= 128 ? p.groups : p.groups * FEW_WAVES(nb);
+    }
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
-    p.joins = up((int64_t)2 * p.n_work * p.part_rows * part_floats(nb) * 4);
-    p.total = p.joins + up((int64_t)p.n_work * sizeof(Join));
+    p.joins = up(((int64_t)2 * p.groups * p.part_rows + (p.rows >= 128 ? 0 : p.n_work)) * part_floats(nb) * 4);
+    p.total = p.joins + up((int64_t)p.groups * sizeof(Join));
     return p;
 }
 
-template <typename T>
+template <typename T, int NB>
 void join(const PagedArgs& g, hipStream_t st) {
-    const dim3 grid(g.n_work, g.part_rows);
+    join_kernel<T, NB><<<dim3(g.groups, g.part_rows), NB * 2048 / JOIN_ELEMENTS(NB), 0, st>>>(g);
+}
+
+template <typename T>
+void join_dim(const PagedArgs& g, hipStream_t st) {
     switch (blocks_of(g.a.head_dim)) {
-        case 2: join_kernel<T, 2><<<grid, 2 * 64, 0, st>>>(g); break;
-        case 3: join_kernel<T, 3><<<grid, 3 * 64, 0, st>>>(g); break;
-        case 4: join_kernel<T, 4><<<grid, 4 * 64, 0, st>>>(g); break;
-        case 6: join_kernel<T, 6><<<grid, 6 * 64, 0, st>>>(g); break;
-        default: join_kernel<T, 8><<<grid, 8 * 64, 0, st>>>(g);
+        case 2: return join<T, 2>(g, st);
+        case 3: return join<T, 3>(g, st);
+        case 4: return join<T, 4>(g, st);
+        case 6: return join<T, 6>(g, st);
     }
+    join<T, 8>(g, st);
 }
 
 }  // namespace
@@ -120,12 +129,12 @@ hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStr
     const int near = a.cache.page >= rows && a.cache.token_stride * rows < (1 << 29);
     const int group = a.n_heads / a.n_kv_heads, bits = group == 1 ? 1 : log2_of(group - 1) + 1;
     const uint32_t mul = (uint32_t)(((1ull << (31 + bits)) + group - 1) / group);
-    const PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.n_work, p.part_rows, (float*)work,
+    const PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.part_rows, (float*)work,
                          (Join*)(work + p.joins)};
     hipError_t e = p.rows >= 128 ? launch_paged_many(g, p.rows, st) : launch_paged_few(g, p.rows, st);
     if (e != hipSuccess || !p.n_work) return e;
-    if (a.dtype == JX_BF16) join<__bf16>(g, st);
-    else join<_Float16>(g, st);
+    if (a.dtype == JX_BF16) join_dim<__bf16>(g, st);
+    else join_dim<_Float16>(g, st);
     return hipGetLastError();
 }
 

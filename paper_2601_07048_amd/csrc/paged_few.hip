@@ -42,13 +42,18 @@ __device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {
 
 // S^T = K Q^T and O^T += V^T P^T as for many rows, by 16x16x32 matrix instructions.  Bound: the bytes of keys and values.  So every
 // wavefront is a reader of its own, with a share of its own: it takes 32 keys at a time, K straight into registers, V into its own two
-// places in LDS (where its transposed form is read), the next ones on their way while these are worked on, and never waits for
-// another.  Four wavefronts of a workgroup that took a tile's keys in turn lost a fifth of the time where they met at its end.
+// places in LDS (where its transposed form is read), the next ones on their way while these are worked on, and waits for another
+// only when its share is done.  Wavefronts that took a tile's keys in turn lost a fifth of the time where they met at its end.
+// The shares of a workgroup follow each other, so that tiles which they cut are put together in LDS, and only those which the
+// workgroup itself found begun or leaves open are left for join_kernel.
 template <typename T, int NC, int RB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     constexpr int ROWS = RB * 16, KEYS = 32, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32, PITCH = CH * 16, TILE = KEYS * PITCH;
     constexpr int NV = KEYS * CH / 64, NK = 2 * NC, OB = 2 * NC;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];  // [WAVES][2] values; shares
+    extern __shared__ __attribute__((aligned(1024))) char lds[];  // [WAVES][2] values, at last sums of open tiles; shares
+    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS];
+    enum { CLOSED, BEGUN, WITHIN };  // how a share ends: with a tile, in one that it has begun, in one that it lies in
+    __shared__ int wave_end[WAVES];
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, h = lane >> 4, d = a.head_dim;
@@ -58,7 +63,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         return;
     }
     Shares sh;
-    if (!sh.begin<ROWS, WAVES>(g, (int*)(lds + WAVES * 2 * TILE), wave)) return;
+    if (!sh.begin<ROWS, WAVES>(g, (int*)(lds + WAVES * 2 * TILE), wave) && !g.n_work) return;
 
     const int page_mask = a.cache.page - 1;
     const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
@@ -76,11 +81,39 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     };
     const int vr = 4 * h + (r16 >> 2), v_at = vr * PITCH + ((r16 >> 1 & 1) ^ mix<CH>(vr)) * 16 + (r16 & 1) * 8;
 
+    const f32x8 none = {0, 0, 0, 0, 0, 0, 0, 0};
+    Tile t;
+    int head = 0, ends = CLOSED, units = 0;
+    // a row of the tile, by its number
+    auto row_of = [&](int row) {
+        const int rr = t.first + min(row, t.count - 1), token = by_group(g, rr);
+        return RowAt{row < t.count, head * g.group + rr - token * g.group, t.start + token, t.p0 + token - by_group(g, t.first)};
+    };
+    // the result of 16 rows; l: the weights' whole sum
+    auto write_rows = [&](int b, const f32x4 (&o)[OB], float m, float l) {
+        const RowAt row = row_of(b * 16 + r16);
+        if (!row.mine) return;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const long long at = (long long)row.token * a.n_heads + row.head;
+        T* out = (T*)a.d_out + at * d + h * 4;
+        for (int i = 0; i < OB; i++) {
+            f32x4 w = o[i];
+            for (int j = 0; j < 4; j++) w[j] *= inv;
+            if (i * 16 + h * 4 < d) *(typename Vec<T>::x4*)(out + i * 16) = __builtin_convertvector(w, typename Vec<T>::x4);
+        }
+        if (h == 0 && a.d_lse) a.d_lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    };
+    auto write_part = [&](float* part, int b, const f32x4 (&o)[OB], float m, float l) {
+        if (b * 16 + r16 >= t.count) return;
+        for (int i = 0; i < OB; i++) *(f32x4*)(part + part_at(b * 16 + r16, i * 16 + h * 4)) = o[i];
+        if (h < 2) part[NC * 1024 + h * 32 + b * 16 + r16] = h ? l : m;
+    };
     while (sh.x0 < sh.x1) {
         const Segment e = sh.next<ROWS>(g);
-        const Tile& t = e.t;
+        t = e.t;
         if (t.r < 0) return;
-        const int head = sh.head;
+        head = sh.head;
+        units = e.units;
         const int key0 = t.lo + e.u0 * UNIT, key1 = min(t.lo + e.u1 * UNIT, t.hi);
         const char* kb = (const char*)a.cache.d_k + head * a.cache.head_stride * 2;
         const char* vb = (const char*)a.cache.d_v + head * a.cache.head_stride * 2;
@@ -122,10 +155,6 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         load_keys(key0, here);
         load_values(key0, here, mine);
 
-        auto row_of = [&](int row) {
-            const int rr = t.first + min(row, t.count - 1), token = by_group(g, rr);
-            return RowAt{row < t.count, head * g.group + rr - token * g.group, t.start + token, t.p0 + token - by_group(g, t.first)};
-        };
         int pos[RB];
         s16x8 q[RB][NC];
         for (int b = 0; b < RB; b++) {
@@ -191,20 +220,23 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             }
             if (more) wait_loads<NV + NK>();
             else wait_loads<0>();
-            s16x8 y[OB];
-            for (int i = 0; i < OB; i++) {
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (i * 32))));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ (i * 32)) + 16 * PITCH));
-                y[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if (!all)
-                for (int i = 0; i < OB; i++) {
-                    const uint4 w = __builtin_bit_cast(uint4, y[i]);
-                    worst = max_pairs(worst, max_pairs(max_pairs(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), max_pairs(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu)));
+            constexpr int AT_ONCE = RB == 1 ? OB : OB / 2;  // by the registers that are free
+            for (int i0 = 0; i0 < OB; i0 += AT_ONCE) {
+                s16x8 y[AT_ONCE];
+                for (int i = 0; i < AT_ONCE; i++) {
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ ((i0 + i) * 32))));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + (v_at ^ ((i0 + i) * 32)) + 16 * PITCH));
+                    y[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 }
-            for (int i = 0; i < OB; i++)
-                for (int b = 0; b < RB; b++) o[b][i] = mul16<T>(y[i], p[b], o[b][i]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (!all)
+                    for (int i = 0; i < AT_ONCE; i++) {
+                        const uint4 w = __builtin_bit_cast(uint4, y[i]);
+                        worst = max_pairs(worst, max_pairs(max_pairs(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), max_pairs(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu)));
+                    }
+                for (int i = 0; i < AT_ONCE; i++)
+                    for (int b = 0; b < RB; b++) o[b][i0 + i] = mul16<T>(y[i], p[b], o[b][i0 + i]);
+            }
             __builtin_amdgcn_sched_barrier(0);  // the place has been read before it is filled again
         };
         if (key0 < key1) {
@@ -220,32 +252,26 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             wait_loads<0>();  // what was on its way for a tile without keys
         }
 
-        const bool whole = e.whole();
-        float* part = NULL;
-        if (!whole) {
-            part = sh.part(g, e.u0 == 0, NC);
-            if (e.u0 == 0 && lane == 0) sh.name(g, e);
-        }
+        // Results: of a whole tile, of a part that ends one, or of one that is open at the share's end
+        const bool whole = e.whole(), open = e.u1 < e.units;
+        if (open) ends = e.u0 == 0 ? BEGUN : WITHIN;
+        float* part = whole || open ? NULL : wave == 0 ? sh.part(g, false, NC) : sh.inner(g, sh.work, NC);
+        float* sums = (float*)(lds + wave * 2 * TILE);  // [RB][OB][64][4], as the lanes hold them
         constexpr uint32_t ODD = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;  // infinities and what is not a number
         if (!ballot((worst & 0xFFFF) >= ODD || worst >> 16 >= ODD)) {
             for (int b = 0; b < RB; b++) {
                 float sum = l[b] + __shfl_xor(l[b], 16, 64);
                 sum += __shfl_xor(sum, 32, 64);
-                const RowAt row = row_of(b * 16 + r16);
-                if (!row.mine) continue;
                 if (whole) {
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    const long long at = (long long)row.token * a.n_heads + row.head;
-                    T* out = (T*)a.d_out + at * d + h * 4;
-                    for (int i = 0; i < OB; i++) {
-                        f32x4 w = o[b][i];
-                        for (int j = 0; j < 4; j++) w[j] *= inv;
-                        if (i * 16 + h * 4 < d) *(typename Vec<T>::x4*)(out + i * 16) = __builtin_convertvector(w, typename Vec<T>::x4);
-                    }
-                    if (h == 0 && a.d_lse) a.d_lse[at] = sum == 0.0f ? -INFINITY : (m[b] + __builtin_amdgcn_logf(sum)) * LN2;
+                    write_rows(b, o[b], m[b], sum);
+                } else if (!open) {
+                    write_part(part, b, o[b], m[b], sum);
                 } else {
-                    for (int i = 0; i < OB; i++) *(f32x4*)(part + part_at(b * 16 + r16, i * 16 + h * 4)) = o[b][i];
-                    if (h < 2) part[NC * 1024 + h * 32 + b * 16 + r16] = h ? sum : m[b];
+                    for (int i = 0; i < OB; i++) *(f32x4*)(sums + ((b * OB + i) * 64 + lane) * 4) = o[b][i];
+                    if (h == 0) {
+                        wave_m[wave][b * 16 + r16] = m[b];
+                        wave_l[wave][b * 16 + r16] = sum;
+                    }
                 }
             }
         } else {
@@ -253,7 +279,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             const int c8 = lane % CH * 8;
             for (int i = 0; i < t.count; i++) {
                 const RowAt row = row_of(i);
-                f32x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+                f32x8 x = none;
                 if (c8 < d) x = load8((const T*)a.d_q + (long long)row.token * a.q_token_stride + row.head * a.q_head_stride + c8);
                 for (int j = 0; j < 8; j++) x[j] *= a.scale * LOG2E;
                 const int k0 = a.window ? max(key0, row.pos + 1 - a.window) : key0, k1 = min(key1, row.pos + 1);
@@ -268,17 +294,59 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                     for (int j = 0; j < 8; j++) s.acc[j] *= inv;
                     if (lane < CH && c8 < d) store8((T*)a.d_out + out * d + c8, s.acc);
                     if (lane == 0 && a.d_lse) a.d_lse[out] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * LN2;
-                } else {
+                } else if (!open) {
                     if (lane < CH && c8 < d)
                         for (int j = 0; j < 8; j++) part[part_at(i, c8 + j)] = s.acc[j];
                     if (lane == 0) {
                         part[NC * 1024 + i] = s.m;
                         part[NC * 1024 + 32 + i] = s.l;
                     }
+                } else {
+                    if (lane < CH && c8 < OB * 16)
+                        for (int j = 0; j < 8; j++) sums[((i / 16 * OB + c8 / 16) * 64 + ((c8 + j) / 4 & 3) * 16 + i % 16) * 4 + (j & 3)] = s.acc[j];
+                    if (lane == 0) {
+                        wave_m[wave][i] = s.m;
+                        wave_l[wave][i] = s.l;
+                    }
                 }
             }
         }
+        if (open) break;  // the share's last
         sh.x0 += e.u1 - e.u0;
+    }
+    if (!g.n_work) return;
+
+    // Tiles that shares of this workgroup have cut: the first of them takes what the others have added
+    if (lane == 0) wave_end[wave] = ends;
+    __syncthreads();
+    if (ends == CLOSED || (ends == WITHIN && wave > 0)) return;
+    for (int b = 0; b < RB; b++) {
+        f32x4 o[OB];
+        for (int i = 0; i < OB; i++) o[i] = *(const f32x4*)(lds + wave * 2 * TILE + ((b * OB + i) * 64 + lane) * 16);
+        float m = wave_m[wave][b * 16 + r16], l = wave_l[wave][b * 16 + r16];
+        auto add = [&](float pm, float pl, auto sums_of) {
+            const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
+            const float keep = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(pm - base);
+            m = top;
+            l = l * keep + pl * w;
+            for (int i = 0; i < OB; i++) {
+                const f32x4 y = sums_of(i);
+                for (int j = 0; j < 4; j++) o[i][j] = fmaf(y[j], w, o[i][j] * keep);
+            }
+        };
+        int w = wave + 1;
+        for (; w < sh.active && wave_end[w] == WITHIN; w++)
+            add(wave_m[w][b * 16 + r16], wave_l[w][b * 16 + r16],
+                [&](int i) { return *(const f32x4*)(lds + w * 2 * TILE + ((b * OB + i) * 64 + lane) * 16); });
+        const bool ended = w < sh.active;  // its share begins with the tile's end
+        if (ended && b * 16 + r16 < t.count) {
+            const float* part = sh.inner(g, sh.work + w - wave, NC);
+            add(part[NC * 1024 + b * 16 + r16], part[NC * 1024 + 32 + b * 16 + r16],
+                [&](int i) { return *(const f32x4*)(part + part_at(b * 16 + r16, i * 16 + h * 4)); });
+        }
+        if (ends == BEGUN && ended) write_rows(b, o, m, l);
+        else write_part(sh.part(g, ends == BEGUN, NC), b, o, m, l);
+        if (ends == BEGUN && !ended && b == 0 && lane == 0) sh.name(g, t, sh.x0, units);
     }
 }
 
@@ -288,7 +356,7 @@ hipError_t launch(const PagedArgs& g, hipStream_t st) {
     const size_t lds = WAVES * 2 * 32 * CH * 16 + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
     static const hipError_t set = hipFuncSetAttribute((const void*)paged_few_kernel<T, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
     if (set != hipSuccess) return set;
-    const unsigned shares = g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads), blocks = (shares + WAVES - 1) / WAVES + CLEARERS;
+    const unsigned tiles = (unsigned)(g.slots * g.a.n_kv_heads), blocks = (g.n_work ? g.groups : (tiles + WAVES - 1) / WAVES) + CLEARERS;
     paged_few_kernel<T, NC, RB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();
 }

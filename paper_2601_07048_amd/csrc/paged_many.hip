@@ -173,14 +173,14 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
         const Segment e = sh.next<ROWS>(g);
         const Tile& t = e.t;
         if (t.r < 0) return;
-        const int work = sh.work, head = sh.head;
+        const int work = sh.group, head = sh.head;
         const bool whole = e.whole();
         const int key0 = t.lo + e.u0 * KEYS, key1 = min(t.lo + e.u1 * KEYS, t.hi);
 
         // rows of this wavefront
         R x;
         x.begin();
-        const int rows0 = ((wave + work) & (WAVES - 1)) * 32;  // tiles of few rows: the workgroups of a CU keep different SIMDs busy
+        const int rows0 = ((wave + (g.n_work ? work : 0)) & (WAVES - 1)) * 32;  // tiles of few rows: the workgroups of a CU keep different SIMDs busy
         const bool busy = rows0 < t.count;
         auto row_of = [&](int of_lane) {
             const int row = rows0 + (of_lane & 31), rr = t.first + min(row, t.count - 1), token = by_group(g, rr);
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
         float* part = NULL;
         if (!whole) {
             part = sh.part(g, e.u0 == 0, NB) + rows0 / 32 * part_floats(NB);
-            if (e.u0 == 0 && tid == 0) sh.name(g, e);
+            if (e.u0 == 0 && tid == 0) sh.name(g, t, sh.x0, e.units);
         }
         const long long oi = (long long)y.token * a.n_heads + y.head;
         if (busy && !odd_values) {
@@ -364,7 +364,7 @@ hipError_t launch(const PagedArgs& g, hipStream_t st) {
     const size_t lds = 4 * TILE + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
     static const hipError_t set = hipFuncSetAttribute((const void*)paged_many_kernel<T, NB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (set != hipSuccess) return set;
-    const unsigned blocks = (g.n_work ? g.n_work : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
+    const unsigned blocks = (g.n_work ? g.groups : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
     paged_many_kernel<T, NB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();
 }

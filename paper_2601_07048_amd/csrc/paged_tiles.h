@@ -10,7 +10,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
 constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys; of more there are enough without
 
-// A tile that several shares cut: parts 2 work + 1 of the first of them, 2 work of the pieces - 1 that follow.  0 pieces: none
+// A tile whose keys several workgroups share: part 2 group + 1 of the first of them, 2 group of the pieces - 1 that follow.  0 pieces: none
 struct __attribute__((aligned(16))) Join {
     int pieces, head, first, count;  // of the tile: key head, first row and number of rows
     int start, unused[3];            // of the request: its first row of q
@@ -21,11 +21,12 @@ struct PagedArgs {
     int page_shift, group;  // group: query heads of a key head
     uint32_t group_mul, group_shift;  // see by_group
     int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
-    int slots, n_work;      // tiles at most; shares of them, 0 = a share a tile
+    int slots;              // tiles at most
+    int groups, n_work;     // workgroups, and shares of all tiles (1 or FEW_WAVES for each workgroup); 0 = a share a tile
     int part_rows;          // tiles' rows / 32
-    float* part;            // [2 n_work][part_rows]: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
+    float* part;            // [2 groups][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
                             // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
-    Join* joins;            // [n_work]
+    Join* joins;            // [groups]
 };
 
 hipError_t launch_paged_many(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 128, or 256 up to 128 elements
@@ -124,9 +125,9 @@ constexpr int part_floats(int nb) { return nb * 1024 + 64; }
 
 // ---- tiles shared out ---------------------------------------------------------------------------------------------------
 // All tiles of all key heads, UNIT keys of one a unit, are cut into equal shares, whatever the lengths of the requests are, one for each
-// workgroup (many rows) or wavefront (few); where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its share for itself: from the
-// first rows and lengths of all requests (8 bytes each) it counts the units of every slot and adds them up in LDS.  With more than MAX_SLOTS
-// slots there are tiles enough, and each is a workgroup's.
+// workgroup (many rows) or wavefront (few); where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its
+// shares for itself: from the first rows and lengths of all requests (8 bytes each) it counts the units of every slot and adds them up
+// in LDS.  With more than MAX_SLOTS slots there are tiles enough, and each is a share.
 constexpr int UNIT = 64;
 
 struct Segment {  // units u0 .. u1 - 1 of the tile's
@@ -146,14 +147,14 @@ struct Shares {
     // Units x0 .. x1 - 1 are this workgroup's.  The first `rem` shares are `each` + 1 units, the others `each`; the launch has seen to it that
     // there are less than 2^31 in all.
     uint32_t x0, x1, per_head, each, rem;
-    int head, slot, work;
+    int head, slot;
+    int group, per, work, active;  // workgroup in the order of the shares, shares of each, this share, shares that this workgroup has
 
-    // For share `sub` of PER shares of the workgroup, by all of it.  false: nothing to do
+    // For share `sub` of up to PER of the workgroup, by all of it.  false: there is no such share
     template <int ROWS, int PER>
     __device__ __forceinline__ bool begin(const PagedArgs& g, int* lds, int sub) {
-        const int THREADS = (int)blockDim.x;
         const jx_attend_args& a = g.a;
-        const int tid = threadIdx.x, lane = lane_id();
+        const int tid = threadIdx.x, lane = lane_id(), THREADS = (int)blockDim.x;
         x0 = 0;
         x1 = 1;
         if (!g.n_work) {
@@ -199,10 +200,16 @@ struct Shares {
         __syncthreads();
         per_head = __builtin_amdgcn_readfirstlane(cum[g.slots]);
         const uint32_t all = per_head * a.n_kv_heads, shares = min((uint32_t)g.n_work, all);  // none is empty
-        // consecutive shares stay on one XCD's cache; few are spread over all
-        work = all < (uint32_t)g.n_work ? sub * (g.n_work / PER) + (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.n_work / 8) + (int)(blockIdx.x / 8) * PER + sub;
-        if (PER == 1 ? tid == 0 : lane == 0) g.joins[work].pieces = 0;
-        if ((uint32_t)work >= shares) return false;
+        // shares of a workgroup follow each other; consecutive workgroups stay on one XCD's cache, few are spread over all
+        per = PER == 1 ? 1 : (int)((shares + g.groups - 1) / g.groups);
+        group = all < (uint32_t)g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.groups / 8) + (int)(blockIdx.x / 8);
+        work = group * per + sub;
+        active = min(per, (int)shares - group * per);
+        if (tid == 0) g.joins[group].pieces = 0;
+        if (sub >= active) {
+            x1 = 0;
+            return false;
+        }
         each = all / shares;
         rem = all - each * shares;
         x0 = work * each + min((uint32_t)work, rem);
@@ -245,16 +252,21 @@ struct Shares {
         return e;
     }
 
-    // Where this share's part of a tile is left
+    // Where a workgroup leaves its part of a tile that it shares with others: of the tile that it begins and does not end (`first`) or
+    // that it found begun
     __device__ __forceinline__ float* part(const PagedArgs& g, bool first, int nb) const {
-        return g.part + (size_t)(2 * work + first) * g.part_rows * part_floats(nb);
+        return g.part + (size_t)(2 * group + first) * g.part_rows * part_floats(nb);
+    }
+    // ... and a wavefront its part of a tile that others of its workgroup have begun
+    __device__ __forceinline__ float* inner(const PagedArgs& g, int of_work, int nb) const {
+        return g.part + (size_t)(2 * g.groups + of_work) * part_floats(nb);
     }
 
-    // The first of the shares that cut a tile says who they are
-    __device__ __forceinline__ void name(const PagedArgs& g, const Segment& e) const {
-        const uint32_t end = x0 + e.units - 1, large = rem * (each + 1);  // the tile's last unit, and whose it is
+    // The first workgroup of those that share a tile, which began with unit x of all, says who they are
+    __device__ __forceinline__ void name(const PagedArgs& g, const Tile& t, uint32_t x, int units) const {
+        const uint32_t end = x + units - 1, large = rem * (each + 1);  // the tile's last unit, and whose it is
         const int last = (int)(end < large ? end / (each + 1) : rem + (end - large) / each);
-        g.joins[work] = {last - work + 1, head, e.t.first, e.t.count, e.t.start, {0, 0, 0}};
+        g.joins[group] = {last / per - group + 1, head, t.first, t.count, t.start, {0, 0, 0}};
     }
 };
 
