@@ -86,9 +86,17 @@ Plan make_plan(const jx_attend_args& a) {
     const int nb = blocks_of(a.head_dim);
     Plan p = {};
     const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
-    // few rows: those of 16 neighbouring keys have to lie in one page
+    // Few rows: the 16 neighbouring keys that a load takes have to lie in one page.  16 for what is mostly single tokens; 32 where the
+    // cache has little room for each request, since a request of more rows reads its keys once for every tile (32 or 128 rows: 64
+    // requests of up to 8 tokens, 4 heads, up to 300 keys 20 or 31 us; 32 of up to 16 tokens, 4,000 keys 69 or 55).
+    // Many rows: 256 where most tiles are full (256 or 128 rows: a chunk of 4,096 over 16,384 keys 967 or 1,080 us; eight
+    // chunks of up to 512 152 or 131).
     const bool pages = a.cache.page >= 16 && a.cache.token_stride < (1 << 25);
-    p.rows = pages && rows <= 16ll * a.n_req ? 16 : pages && rows <= 32ll * a.n_req ? 32 : nb <= 4 && rows >= (a.n_req == 1 ? 512 : 2048ll * a.n_req) ? 256 : 128;
+    const bool little = (int64_t)a.cache.n_pages * a.cache.page <= 512ll * a.n_req;
+    const long long full = a.n_req == 1 ? 512 : 2048;
+    if (pages && rows <= 16ll * a.n_req) p.rows = 16;
+    else if (pages && little && rows <= 32ll * a.n_req) p.rows = 32;
+    else p.rows = nb <= 4 && rows >= full * a.n_req ? 256 : 128;
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
