@@ -351,6 +351,7 @@ int check_attend(const jx_attend_args* a) {
     if (int rc = check_cache(a->cache)) return rc;
     if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
     if (a->window < 0) return fail(JX_EINVAL, "window < 0");
+    if ((int64_t)a->n_req * a->n_kv_heads > 1 << 28) return fail(JX_EINVAL, "n_req * n_kv_heads out of range");
     return JX_OK;
 }
 

@@ -354,8 +354,8 @@ template <typename T, int NC, int RB>
 hipError_t launch(const PagedArgs& g, hipStream_t st) {
     constexpr int WAVES = FEW_WAVES(NC), CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32;
     const size_t lds = WAVES * 2 * 32 * CH * 16 + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
-    static const hipError_t set = hipFuncSetAttribute((const void*)paged_few_kernel<T, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
-    if (set != hipSuccess) return set;
+    hipError_t e = hipFuncSetAttribute((const void*)paged_few_kernel<T, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
+    if (e != hipSuccess) return e;
     const unsigned tiles = (unsigned)(g.slots * g.a.n_kv_heads), blocks = (g.n_work ? g.groups : (tiles + WAVES - 1) / WAVES) + CLEARERS;
     paged_few_kernel<T, NC, RB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();

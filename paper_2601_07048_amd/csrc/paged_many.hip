@@ -362,8 +362,8 @@ template <typename T, int NB, int WAVES>
 hipError_t launch(const PagedArgs& g, hipStream_t st) {
     constexpr int TILE = UNIT * Rows32<T, NB>::PITCH;
     const size_t lds = 4 * TILE + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
-    static const hipError_t set = hipFuncSetAttribute((const void*)paged_many_kernel<T, NB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (set != hipSuccess) return set;
+    hipError_t e = hipFuncSetAttribute((const void*)paged_many_kernel<T, NB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return e;
     const unsigned blocks = (g.n_work ? g.groups : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
     paged_many_kernel<T, NB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();

@@ -68,7 +68,7 @@ def test_attention_refusals(jx):
 
     call = lambda a: jx._lib.jx_paged_attention(C.byref(a), None, C.c_int64(0), None)  # noqa: E731
     sized = BAD_HEADS + [dict(cache=cache(jx, **c)) for c in BAD_CACHES] + \
-        [dict(table_pages=0), dict(table_pages=1 << 28), dict(n_req=-1), dict(d_table=None), dict(window=-1)]
+        [dict(table_pages=0), dict(table_pages=1 << 28), dict(n_req=-1), dict(n_req=1 << 28), dict(d_table=None), dict(window=-1)]
     for bad in sized:
         refused(jx, call(args(**bad)))
         refused(jx, jx._lib.jx_paged_attention_bytes(C.byref(args(**bad))))

@@ -240,6 +240,41 @@ def test_long_caches(lens, new):
     p.check(window=777, rows=rows)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 72, 96, 128, 192, 256])
+@pytest.mark.parametrize("window", [0, 30])
+def test_a_few_tokens_of_short_requests(dtype, dim, window):
+    rng = np.random.default_rng(dim)
+    lens = rng.integers(1, 140, 24).tolist()
+    new = [min(int(rng.integers(1, 9)), n) for n in lens]
+    Paged(dtype, 8, 2, dim, 16, lens, new, seed=dim).check(window, rows=list(range(0, sum(new), 3)))
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("lens,new", [([700], [600]), ([1500, 1100], [1100, 1100]), ([90, 3000], [1, 2100])], ids=["one", "two", "unlike"])
+def test_long_chunks(dim, lens, new):
+    p = Paged(BF, 8, 2, dim, 32, lens, new, seed=dim)
+    rows = sorted({0, 1, 63, 64, 127, 128, 255, 256, sum(new) // 2, sum(new) - 1})
+    p.check(rows=rows)
+    p.check(window=100, rows=rows)
+
+
+def test_more_tiles_than_are_shared_out():
+    """Many rows: each tile is a workgroup's, none is joined."""
+    rng = np.random.default_rng(3)
+    lens = rng.integers(6, 80, 1100).tolist()
+    p = Paged(BF, 8, 1, 64, 4, lens, [6] * 1100, seed=2)
+    p.check(rows=list(range(0, 6600, 371)))
+    p.check(window=9, rows=list(range(5, 6600, 371)))
+
+
+def test_a_scale_of_zero_gives_the_mean():
+    for new in (1, 40):
+        p = Paged(F16, 4, 2, 64, 16, [100, 41], [new, new], seed=4)
+        p.scale = 0.0
+        p.check()
+
+
 def test_many_requests():
     rng = np.random.default_rng(0)
     lens = rng.integers(0, 90, 1500).tolist()
