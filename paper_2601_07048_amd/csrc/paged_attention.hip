@@ -1,4 +1,5 @@
 // Attention of a step's new tokens over a paged cache: which kernel, and the join of tiles that workgroups shared.
+#include <type_traits>
 #include "paged_tiles.h"
 
 namespace jx {
@@ -26,17 +27,18 @@ __global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(Pag
     float m = -INFINITY, l = 0.0f;
     f32x4 s[K];
     for (int k = 0; k < K; k++) s[k] = (f32x4)0.0f;
-    for (int i0 = lane / wide; i0 < j.pieces; i0 += PIECES * side) {
-        float pm[PIECES], pl[PIECES], top = m;
-        f32x4 y[PIECES][K];
-        for (int u = 0; u < PIECES; u++) {
+    auto take = [&](auto at_once, int i0) {
+        constexpr int N = at_once;
+        float pm[N], pl[N], top = m;
+        f32x4 y[N][K];
+        for (int u = 0; u < N; u++) {
             const int i = min(i0 + u * side, j.pieces - 1);
             const float* p = parts + (size_t)(2 * (blockIdx.x + i) + (i == 0)) * g.part_rows * part_floats(NB);
             pm[u] = p[to_m];
             pl[u] = p[to_m + 32];
             for (int k = 0; k < K; k++) y[u][k] = *(const f32x4*)(p + to_s + k * 256);
         }
-        for (int u = 0; u < PIECES; u++) {
+        for (int u = 0; u < N; u++) {
             if (i0 + u * side >= j.pieces) pm[u] = -INFINITY;
             top = fmaxf(top, pm[u]);
         }
@@ -45,14 +47,19 @@ __global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(Pag
         l *= keep;
         for (int k = 0; k < K; k++)
             for (int e = 0; e < 4; e++) s[k][e] *= keep;
-        for (int u = 0; u < PIECES; u++) {
+        for (int u = 0; u < N; u++) {
             const float w = __builtin_amdgcn_exp2f(pm[u] - base);
             const bool counts = pm[u] != -INFINITY;  // else nothing, or not a piece
             l = counts ? fmaf(pl[u], w, l) : l;
             for (int k = 0; k < K; k++)
                 for (int e = 0; e < 4; e++) s[k][e] = counts ? fmaf(y[u][k][e], w, s[k][e]) : s[k][e];
         }
-    }
+    };
+    const int i0 = lane / wide;
+    if (j.pieces <= 2 * side) take(std::integral_constant<int, 2>(), i0);
+    else if (j.pieces <= 4 * side) take(std::integral_constant<int, 4>(), i0);
+    else
+        for (int i = 0; i < j.pieces; i += PIECES * side) take(std::integral_constant<int, PIECES>(), i0 + i);
     float top = m;
     for (int x = wide; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 64));
     const float keep = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
