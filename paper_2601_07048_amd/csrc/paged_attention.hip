@@ -1,4 +1,5 @@
 // Attention of a step's new tokens over a paged cache: which kernel, and the join of tiles that workgroups shared.
+#include <algorithm>
 #include <type_traits>
 #include "paged_tiles.h"
 
@@ -6,17 +7,17 @@ namespace jx {
 
 namespace {
 
-// Elements of a tile's rows that a wavefront joins: up to eight or sixteen wavefronts for all of them
-constexpr int JOIN_ELEMENTS(int nb) { return nb <= 4 ? 8 : 16; }
+// Workgroups for the elements of a tile's rows, eight a wavefront
+constexpr int JOINERS(int nb) { return nb <= 4 ? 1 : 2; }
 
 // The parts of a tile whose keys several workgroups share, as one: the tile that workgroup blockIdx.x began and did not end;
-// blockIdx.y: which 32 rows.  A wavefront takes 8 or 16 elements, as the lanes held them when the parts were written, and of few rows
+// blockIdx.y: which 32 rows.  A wavefront takes 8 elements, as the lanes held them when the parts were written, and of few rows
 // two or four pieces side by side.  Bound: the time that a chain of reads takes, hence PIECES at once.
 template <typename T, int NB>
-__global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(PagedArgs g) {
-    constexpr int PIECES = 8, K = JOIN_ELEMENTS(NB) / 8;
+__global__ __launch_bounds__(NB * 256 / JOINERS(NB)) void join_kernel(PagedArgs g) {
+    constexpr int PIECES = 8;
     const jx_attend_args& a = g.a;
-    const int lane = lane_id(), e0 = (int)(threadIdx.x >> 6) * JOIN_ELEMENTS(NB), d = a.head_dim;
+    const int lane = lane_id(), e0 = (int)((blockIdx.z * blockDim.x + threadIdx.x) >> 6) * 8, d = a.head_dim;
     const Join j = g.joins[blockIdx.x];
     const int count = j.pieces ? j.count - (int)blockIdx.y * 32 : 0;
     if (count <= 0 || e0 >= d) return;
@@ -25,18 +26,17 @@ __global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(Pag
     const float* parts = g.part + blockIdx.y * part_floats(NB);
     const int to_s = part_at(row, e0 + half * 4), to_m = NB * 1024 + row;
     float m = -INFINITY, l = 0.0f;
-    f32x4 s[K];
-    for (int k = 0; k < K; k++) s[k] = (f32x4)0.0f;
+    f32x4 s = {0, 0, 0, 0};
     auto take = [&](auto at_once, int i0) {
         constexpr int N = at_once;
         float pm[N], pl[N], top = m;
-        f32x4 y[N][K];
+        f32x4 y[N];
         for (int u = 0; u < N; u++) {
             const int i = min(i0 + u * side, j.pieces - 1);
             const float* p = parts + (size_t)(2 * (blockIdx.x + i) + (i == 0)) * g.part_rows * part_floats(NB);
             pm[u] = p[to_m];
             pl[u] = p[to_m + 32];
-            for (int k = 0; k < K; k++) y[u][k] = *(const f32x4*)(p + to_s + k * 256);
+            y[u] = *(const f32x4*)(p + to_s);
         }
         for (int u = 0; u < N; u++) {
             if (i0 + u * side >= j.pieces) pm[u] = -INFINITY;
@@ -45,14 +45,12 @@ __global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(Pag
         const float base = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - base);
         m = top;
         l *= keep;
-        for (int k = 0; k < K; k++)
-            for (int e = 0; e < 4; e++) s[k][e] *= keep;
+        for (int e = 0; e < 4; e++) s[e] *= keep;
         for (int u = 0; u < N; u++) {
             const float w = __builtin_amdgcn_exp2f(pm[u] - base);
             const bool counts = pm[u] != -INFINITY;  // else nothing, or not a piece
             l = counts ? fmaf(pl[u], w, l) : l;
-            for (int k = 0; k < K; k++)
-                for (int e = 0; e < 4; e++) s[k][e] = counts ? fmaf(y[u][k][e], w, s[k][e]) : s[k][e];
+            for (int e = 0; e < 4; e++) s[e] = counts ? fmaf(y[u][e], w, s[e]) : s[e];
         }
     };
     const int i0 = lane / wide;
@@ -64,28 +62,24 @@ __global__ __launch_bounds__(NB * 2048 / JOIN_ELEMENTS(NB)) void join_kernel(Pag
     for (int x = wide; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 64));
     const float keep = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
     l *= keep;
-    for (int k = 0; k < K; k++)
-        for (int e = 0; e < 4; e++) s[k][e] *= keep;
+    for (int e = 0; e < 4; e++) s[e] *= keep;
     for (int x = wide; x < 64; x *= 2) {
         l += __shfl_xor(l, x, 64);
-        for (int k = 0; k < K; k++)
-            for (int e = 0; e < 4; e++) s[k][e] += __shfl_xor(s[k][e], x, 64);
+        for (int e = 0; e < 4; e++) s[e] += __shfl_xor(s[e], x, 64);
     }
     if (lane >= wide || row >= count) return;
     const int rr = j.first + (int)blockIdx.y * 32 + row, token = by_group(g, rr);
     const long long o = (j.start + (long long)token) * a.n_heads + j.head * g.group + rr - token * g.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    for (int k = 0; k < K; k++) {
-        const int e = e0 + k * 8 + half * 4;
-        for (int i = 0; i < 4; i++) s[k][i] *= inv;
-        if (e < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + e) = __builtin_convertvector(s[k], typename Vec<T>::x4);
-    }
+    for (int i = 0; i < 4; i++) s[i] *= inv;
+    const int e = e0 + half * 4;
+    if (e < d) *(typename Vec<T>::x4*)((T*)a.d_out + o * d + e) = __builtin_convertvector(s, typename Vec<T>::x4);
     if (e0 == 0 && half == 0 && a.d_lse) a.d_lse[o] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 struct Plan {
     int rows;  // of a tile: 16, 32: few rows, 128, 256: many
-    int slots, groups, n_work, part_rows;
+    int slots, groups, n_work, part_rows, own;
     int64_t joins, total;  // bytes before the joins, in all
 };
 
@@ -106,9 +100,14 @@ Plan make_plan(const jx_attend_args& a) {
     else p.rows = nb <= 4 && rows >= full * a.n_req ? 256 : 128;
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
+    // Few tiles of few rows and few keys (a table with little room, a short window): a workgroup a tile, which its wavefronts put
+    // together, and no second launch.  128 elements, 8 key heads, 16 requests of up to 256 or 512 keys: 8.9 or 12.7 us, shared out
+    // 11.1 or 12.5; 64 requests 18 or 16.  64 elements, 16 key heads, 16 requests of up to 1,024 keys: 10.9, shared out 18.4.
+    const int64_t room = (int64_t)a.table_pages * a.cache.page, keys = a.window ? std::min<int64_t>(room, (int64_t)a.window + 16) : room;
+    p.own = p.rows < 128 && (int64_t)p.slots * a.n_kv_heads <= 384 && keys <= 1024 / (nb <= 2 ? 1 : nb);
     const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
     // as many shares as the card holds workgroups (many rows) or wavefronts (few) at a time
-    if (p.slots && p.slots <= MAX_SLOTS && units < 2e9) {
+    if (p.slots && !p.own && p.slots <= MAX_SLOTS && units < 2e9) {
         p.groups = 256 * (p.rows >= 128 ? MANY_PER_CU(nb, p.rows) : nb <= 2 ? 2 : 1);
         p.n_work = p.rows >= 128 ? p.groups : p.groups * FEW_WAVES(nb);
     }
@@ -120,7 +119,7 @@ Plan make_plan(const jx_attend_args& a) {
 
 template <typename T, int NB>
 void join(const PagedArgs& g, hipStream_t st) {
-    join_kernel<T, NB><<<dim3(g.groups, g.part_rows), NB * 2048 / JOIN_ELEMENTS(NB), 0, st>>>(g);
+    join_kernel<T, NB><<<dim3(g.groups, g.part_rows, JOINERS(NB)), NB * 256 / JOINERS(NB), 0, st>>>(g);
 }
 
 template <typename T>
@@ -144,7 +143,7 @@ hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStr
     const int near = a.cache.page >= rows && a.cache.token_stride * rows < (1 << 29);
     const int group = a.n_heads / a.n_kv_heads, bits = group == 1 ? 1 : log2_of(group - 1) + 1;
     const uint32_t mul = (uint32_t)(((1ull << (31 + bits)) + group - 1) / group);
-    const PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.part_rows, (float*)work,
+    const PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.part_rows, p.own, (float*)work,
                          (Join*)(work + p.joins)};
     hipError_t e = p.rows >= 128 ? launch_paged_many(g, p.rows, st) : launch_paged_few(g, p.rows, st);
     if (e != hipSuccess || !p.n_work) return e;

@@ -57,13 +57,10 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, h = lane >> 4, d = a.head_dim;
-    const int sharers = (int)gridDim.x - CLEARERS;
-    if ((int)blockIdx.x >= sharers) {
-        clear_rows<T>(a, (int)blockIdx.x - sharers, CLEARERS);
-        return;
-    }
     Shares sh;
-    if (!sh.begin<ROWS, WAVES>(g, (int*)(lds + WAVES * 2 * TILE), wave) && !g.n_work) return;
+    const bool any = sh.begin<ROWS, WAVES>(g, (int*)(lds + WAVES * 2 * TILE), wave);
+    sh.clear_rows<T>(g);
+    if (!any && !g.n_work) return;
 
     const int page_mask = a.cache.page - 1;
     const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
@@ -109,9 +106,10 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         if (h < 2) part[NC * 1024 + h * 32 + b * 16 + r16] = h ? l : m;
     };
     while (sh.x0 < sh.x1) {
-        const Segment e = sh.next<ROWS>(g);
+        const Segment e = sh.next<ROWS, WAVES>(g);
         t = e.t;
         if (t.r < 0) return;
+        if (e.u0 == e.u1) break;  // more wavefronts than units
         head = sh.head;
         units = e.units;
         const int key0 = t.lo + e.u0 * UNIT, key1 = min(t.lo + e.u1 * UNIT, t.hi);
@@ -253,7 +251,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         }
 
         // Results: of a whole tile, of a part that ends one, or of one that is open at the share's end
-        const bool whole = e.whole(), open = e.u1 < e.units;
+        const bool whole = e.whole(), open = !whole && (g.own || e.u1 < e.units);
         if (open) ends = e.u0 == 0 ? BEGUN : WITHIN;
         float* part = whole || open ? NULL : wave == 0 ? sh.part(g, false, NC) : sh.inner(g, sh.work, NC);
         float* sums = (float*)(lds + wave * 2 * TILE);  // [RB][OB][64][4], as the lanes hold them
@@ -314,7 +312,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         if (open) break;  // the share's last
         sh.x0 += e.u1 - e.u0;
     }
-    if (!g.n_work) return;
+    if (!g.n_work && !g.own) return;
 
     // Tiles that shares of this workgroup have cut: the first of them takes what the others have added
     if (lane == 0) wave_end[wave] = ends;
@@ -344,9 +342,9 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             add(part[NC * 1024 + b * 16 + r16], part[NC * 1024 + 32 + b * 16 + r16],
                 [&](int i) { return *(const f32x4*)(part + part_at(b * 16 + r16, i * 16 + h * 4)); });
         }
-        if (ends == BEGUN && ended) write_rows(b, o, m, l);
+        if (ends == BEGUN && (ended || g.own)) write_rows(b, o, m, l);
         else write_part(sh.part(g, ends == BEGUN, NC), b, o, m, l);
-        if (ends == BEGUN && !ended && b == 0 && lane == 0) sh.name(g, t, sh.x0, units);
+        if (ends == BEGUN && !ended && !g.own && b == 0 && lane == 0) sh.name(g, t, sh.x0, units);
     }
 }
 
@@ -356,8 +354,8 @@ hipError_t launch(const PagedArgs& g, hipStream_t st) {
     const size_t lds = WAVES * 2 * 32 * CH * 16 + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
     hipError_t e = hipFuncSetAttribute((const void*)paged_few_kernel<T, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
     if (e != hipSuccess) return e;
-    const unsigned tiles = (unsigned)(g.slots * g.a.n_kv_heads), blocks = (g.n_work ? g.groups : (tiles + WAVES - 1) / WAVES) + CLEARERS;
-    paged_few_kernel<T, NC, RB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
+    const unsigned tiles = (unsigned)(g.slots * g.a.n_kv_heads), blocks = g.n_work ? g.groups : g.own ? tiles : (tiles + WAVES - 1) / WAVES;
+    paged_few_kernel<T, NC, RB, WAVES><<<blocks ? blocks : 256, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();
 }
 

@@ -154,14 +154,11 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
     extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2] keys, [2] values; slots' sums of units, their requests
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int sharers = (int)gridDim.x - CLEARERS;
-    if ((int)blockIdx.x >= sharers) {
-        clear_rows<T>(a, (int)blockIdx.x - sharers, CLEARERS);
-        return;
-    }
     const lds_ptr ring = (lds_ptr)lds;
     Shares sh;
-    if (!sh.begin<ROWS, 1>(g, (int*)(lds + 4 * TILE), 0)) return;
+    const bool any = sh.begin<ROWS, 1>(g, (int*)(lds + 4 * TILE), 0);
+    sh.clear_rows<T>(g);
+    if (!any) return;
 
     const int d = a.head_dim, page_mask = a.cache.page - 1;
     if (d < R::CH * 8)  // what lies behind a head meets zeros of the queries, so it has to be a number
@@ -170,7 +167,7 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
     const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);  // a scale of 0 has to leave -infinity what it is
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
     while (sh.x0 < sh.x1) {
-        const Segment e = sh.next<ROWS>(g);
+        const Segment e = sh.next<ROWS, 1>(g);
         const Tile& t = e.t;
         if (t.r < 0) return;
         const int work = sh.group, head = sh.head;
@@ -364,8 +361,8 @@ hipError_t launch(const PagedArgs& g, hipStream_t st) {
     const size_t lds = 4 * TILE + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
     hipError_t e = hipFuncSetAttribute((const void*)paged_many_kernel<T, NB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return e;
-    const unsigned blocks = (g.n_work ? g.groups : (unsigned)(g.slots * g.a.n_kv_heads)) + CLEARERS;
-    paged_many_kernel<T, NB, WAVES><<<blocks, WAVES * 64, lds, st>>>(g);
+    const unsigned blocks = g.n_work ? g.groups : (unsigned)(g.slots * g.a.n_kv_heads);
+    paged_many_kernel<T, NB, WAVES><<<blocks ? blocks : 256, WAVES * 64, lds, st>>>(g);
     return hipGetLastError();
 }
 

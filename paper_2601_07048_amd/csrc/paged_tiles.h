@@ -7,7 +7,6 @@ namespace jx {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int CLEARERS = 8;      // workgroups that look for rows of no request
 constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys; of more there are enough without
 
 // A tile whose keys several workgroups share: part 2 group + 1 of the first of them, 2 group of the pieces - 1 that follow.  0 pieces: none
@@ -24,6 +23,7 @@ struct PagedArgs {
     int slots;              // tiles at most
     int groups, n_work;     // workgroups, and shares of all tiles (1 or FEW_WAVES for each workgroup); 0 = a share a tile
     int part_rows;          // tiles' rows / 32
+    int own;                // few rows, n_work = 0: whether a workgroup takes a tile, not a wavefront
     float* part;            // [2 groups][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
                             // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
     Join* joins;            // [groups]
@@ -158,7 +158,8 @@ struct Shares {
         x0 = 0;
         x1 = 1;
         if (!g.n_work) {
-            const uint32_t i = blockIdx.x * PER + sub;
+            work = sub;
+            const uint32_t i = g.own ? blockIdx.x : blockIdx.x * PER + sub;
             head = (int)(i % a.n_kv_heads);
             slot = g.slots - 1 - (int)(i / a.n_kv_heads);  // long ones first where there is one request
             return slot >= 0;
@@ -219,8 +220,27 @@ struct Shares {
         return true;
     }
 
+    // Rows that belong to no request: zeros and -infinity, by all workgroups, after begin
+    template <typename T>
+    __device__ __forceinline__ void clear_rows(const PagedArgs& g) const {
+        const jx_attend_args& a = g.a;
+        const int n = (int)a.n_tokens;
+        int b = n, e = n;
+        if (a.n_req) {
+            b = clamp_rows(__builtin_amdgcn_readfirstlane(g.n_work ? starts[0] : a.d_q_start[0]), a);
+            e = clamp_rows(__builtin_amdgcn_readfirstlane(g.n_work ? starts[a.n_req] : a.d_q_start[a.n_req]), a);
+        }
+        const int chunks = a.n_heads * (a.head_dim / 8), outside = b + max(n - max(b, e), 0);
+        for (int i = blockIdx.x; i < outside; i += gridDim.x) {
+            const long long t = i < b ? i : i - b + max(b, e);
+            for (int c = threadIdx.x; c < chunks; c += blockDim.x) ((uint4*)a.d_out)[t * chunks + c] = make_uint4(0, 0, 0, 0);
+            if (a.d_lse)
+                for (int h = threadIdx.x; h < a.n_heads; h += blockDim.x) a.d_lse[t * a.n_heads + h] = -INFINITY;
+        }
+    }
+
     // The segment that begins with unit x0
-    template <int ROWS>
+    template <int ROWS, int PER>
     __device__ __forceinline__ Segment next(const PagedArgs& g) {
         const jx_attend_args& a = g.a;
         Segment e;
@@ -229,7 +249,12 @@ struct Shares {
             e.t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
             e.u0 = 0;
             e.u1 = e.units = e.t.r < 0 ? 1 : units_of(e.t);
-            x1 = x0 + e.units;
+            if (PER > 1 && g.own) {
+                active = min(PER, e.units);
+                e.u0 = (int)((long long)e.units * min(work, active) / active);
+                e.u1 = (int)((long long)e.units * min(work + 1, active) / active);
+            }
+            x1 = x0 + e.u1 - e.u0;
             return e;
         }
         if (x0 >= (head + 1) * per_head) {
@@ -275,19 +300,6 @@ struct RowAt {
     bool mine;
     int head, token, pos;
 };
-
-// Rows that belong to no request: zeros and -infinity, by workgroups `block` of `blocks`
-template <typename T>
-__device__ void clear_rows(const jx_attend_args& a, int block, int blocks) {
-    const int n = (int)a.n_tokens, b = a.n_req ? clamp_rows(a.d_q_start[0], a) : n, e = a.n_req ? clamp_rows(a.d_q_start[a.n_req], a) : n;
-    const int chunks = a.n_heads * (a.head_dim / 8), outside = b + max(n - max(b, e), 0);
-    for (int i = block; i < outside; i += blocks) {
-        const long long t = i < b ? i : i - b + max(b, e);
-        for (int c = threadIdx.x; c < chunks; c += blockDim.x) ((uint4*)a.d_out)[t * chunks + c] = make_uint4(0, 0, 0, 0);
-        if (a.d_lse)
-            for (int h = threadIdx.x; h < a.n_heads; h += blockDim.x) a.d_lse[t * a.n_heads + h] = -INFINITY;
-    }
-}
 
 }  // namespace
 

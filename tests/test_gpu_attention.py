@@ -250,6 +250,26 @@ def test_a_few_tokens_of_short_requests(dtype, dim, window):
     Paged(dtype, 8, 2, dim, 16, lens, new, seed=dim).check(window, rows=list(range(0, sum(new), 3)))
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("bad", [None, math.nan])
+def test_short_requests_in_narrow_and_wide_tables(dtype, dim, bad):
+    """How much a table has room for decides who takes the keys, and nothing else; the same for a window that is short."""
+    lens = [0, 1, 3, 64, 65, 100, 127, 128]
+    p = Paged(dtype, 8, 2, dim, 16, lens, [1, 1, 1, 2, 1, 1, 2, 1], seed=dim, width=8)
+    if bad is not None:  # the first key of the request of 64: its rows 3 and 4 see it, unless the window is short
+        p.v[int(p.table[3, 0]), 0, 1, 3] = bad
+    rows = [t for t in range(10) if bad is None or t not in (3, 4)]
+    narrow, short = p.run(), p.run(window=40)
+    p.table = torch.cat([p.table, torch.full((len(lens), 200), -1, dtype=torch.int32, device="cuda")], 1)
+    for what, got, window in (("narrow", narrow, 0), ("wide", p.run(), 0), ("narrow, window", short, 40), ("wide, window", p.run(window=40), 40)):
+        plain.check(got, p.want(window, None if window else rows), what)
+        for t in range(10):
+            if t not in rows and not window:
+                o = got[0][t].isfinite()
+                assert not o[4:, 3].any() and o[:4].all() and o[4:, :3].all() and o[4:, 4:].all(), what
+
+
 @pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("lens,new", [([700], [600]), ([1500, 1100], [1100, 1100]), ([90, 3000], [1, 2100])], ids=["one", "two", "unlike"])
 def test_long_chunks(dim, lens, new):
