@@ -431,9 +431,10 @@ typedef struct {
  * from the end.  Every request gets the pages that its last one has no room for,
  *   table[r][a_r + i] = free[n_free - 1 - (s_r + i)],  a_r = ceil(len_r / page),
  * s_r = what the requests before r asked for.  There is no room for a request
- * that asks for pages where s_r and its own exceed n_free, whose tokens exceed
- * table_pages pages, or whose rows exceed n_tokens; its tokens get no slots
- * and its row stays as it was.
+ * whose tokens exceed table_pages pages, or whose rows exceed n_tokens: it asks
+ * for no pages.  Nor for one that asks for pages where s_r and its own exceed
+ * n_free, so that what is granted is always the last of the free pages.  A
+ * request without room gets no slots and its row stays as it was.
  * Outputs: d_q_start [n_req + 1], the first row of each request (sums of d_new,
  * at most n_tokens); d_kv_len [n_req] = len + new, or 0 where there was no room;
  * d_pos, d_slot [n_tokens]: position and slot (page * tokens of a page + place

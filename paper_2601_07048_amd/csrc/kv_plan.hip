@@ -58,8 +58,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(KvPlanArgs a) {
         }
         long long all_tokens, all_pages;
         const long long t = tokens + block_before(add, part, &all_tokens);
+        const bool fits = r < a.n_req && end <= a.table_pages && t + add <= a.n_tokens;
+        if (!fits) need = 0;  // asks for nothing: what is granted has to be one piece at the end of the free pages
         const long long p = pages + block_before(need, part, &all_pages);
-        const bool room = r < a.n_req && end <= a.table_pages && t + add <= a.n_tokens && (!need || p + need <= n_free);
+        const bool room = fits && (!need || p + need <= n_free);
         if (r < a.n_req) {
             row[r] = (int32_t)min(t, a.n_tokens);
             before[r] = room ? (int32_t)p : -1;  // p + need <= n_free, or unused
