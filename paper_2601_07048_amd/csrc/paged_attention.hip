@@ -29,6 +29,8 @@ __global__ __launch_bounds__(NB * 256 / JOINERS(NB)) void join_kernel(PagedArgs 
     const int to_s = part_at(row, e0 + half * 4), to_m = NB * 1024 + row;
     float m = -INFINITY, l = 0.0f;
     f32x4 s = {0, 0, 0, 0};
+    // A piece is one by its number, not by its largest score: that of scores which are not numbers is -infinity, and they have to
+    // reach the result.  One without keys adds zeros.
     auto take = [&](auto at_once, int i0) {
         constexpr int N = at_once;
         float pm[N], pl[N], top = m;
@@ -50,7 +52,7 @@ __global__ __launch_bounds__(NB * 256 / JOINERS(NB)) void join_kernel(PagedArgs 
         for (int e = 0; e < 4; e++) s[e] *= keep;
         for (int u = 0; u < N; u++) {
             const float w = __builtin_amdgcn_exp2f(pm[u] - base);
-            const bool counts = pm[u] != -INFINITY;  // else nothing, or not a piece
+            const bool counts = i0 + u * side < j.pieces;
             l = counts ? fmaf(pl[u], w, l) : l;
             for (int e = 0; e < 4; e++) s[e] = counts ? fmaf(y[u][e], w, s[e]) : s[e];
         }
