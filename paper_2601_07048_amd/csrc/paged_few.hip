@@ -202,8 +202,8 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                 for (int i = 0; i < 8; i += 2) top = fmaxf(fmaxf(top, s[b][i >> 2][i & 3]), s[b][i >> 2][(i & 3) + 1]);
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64)) * c;
-                if (ballot(top > m[b] + 8.0f)) {  // the running maximum moves only for a rise by more than 2^8, as for many rows
-                    const float to = fmaxf(top, m[b]), keep = __builtin_amdgcn_exp2f(m[b] - (to == -INFINITY ? 0.0f : to));
+                if (ballot(top > m[b] + BELOW<T> + 8.0f)) {  // the running maximum moves only for a rise by more than 2^8, as for many rows
+                    const float to = fmaxf(top - BELOW<T>, m[b]), keep = __builtin_amdgcn_exp2f(m[b] - (to == -INFINITY ? 0.0f : to));
                     m[b] = to;
                     l[b] *= keep;
                     for (int i = 0; i < OB; i++)

@@ -43,7 +43,7 @@ struct Rows32 {
     static constexpr int CH = NB <= 2 ? 8 : NB <= 4 ? 16 : 32, PITCH = CH * 16;
     s16x8 q[2 * NB];
     f32x16 o[NB];        // sums
-    float m, l, top;     // running maximum and sum of weights, the scores' largest
+    float m, l, top;     // running maximum less BELOW and sum of weights, the scores' largest
     int k_at, v_at;  // a lane's first place in a row of keys, of values
 
     __device__ __forceinline__ void begin() {
@@ -89,8 +89,8 @@ struct Rows32 {
     // Moves the running maximum if these scores rise far over it; c = scale * log2 e
     __device__ __forceinline__ void raise(float c) {
         const float t = both_halves_max(top) * c;
-        if (ballot(t > m + 8.0f)) {
-            const float to = fmaxf(t, m), keep = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
+        if (ballot(t > m + BELOW<T> + 8.0f)) {
+            const float to = fmaxf(t - BELOW<T>, m), keep = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
             m = to;
             l *= keep;
             for (int b = 0; b < NB; b++)

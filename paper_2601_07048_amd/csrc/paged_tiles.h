@@ -51,6 +51,14 @@ __device__ __forceinline__ int by_group(const PagedArgs& g, int n) {
     return g.group == 1 ? n : (int)(__umulhi((uint32_t)n, g.group_mul) >> g.group_shift);
 }
 
+// Weights are 2^(score - m), m = the running maximum less BELOW, and rounded to the element type for their product with the values
+// (half the matrix instructions that two parts would take).  binary16 has nothing under 2^-25: with weights of up to 1, 2^8 after a
+// rise that leaves m alone, the values of keys 18 and more nats under the largest vanish from the sum while their weights stay in
+// the divisor (of 60,000 such keys beside one that has the maximum 98 % of what they add).  So they go up to 2^7, 2^15 after a rise, and what is lost
+// of a key is at most 2^-32 of the largest weight.  bfloat16 has the exponents of 32 bits.
+template <typename T>
+constexpr float BELOW = __is_same(T, _Float16) ? 7.0f : 0.0f;
+
 // ---- a tile: ROWS consecutive rows (token, head of the group) of one request -------------------------------------------
 // Request r has rows (q_start[r + 1] - q_start[r]) * group for each key head.  Its tiles are the slots from
 // q_start[r] * group / ROWS + r on: that leaves room for each request's last, partly filled one without a sum over the requests,
