@@ -76,13 +76,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(jx_rope_args a, int p
         if (a.interleaved) {
             for (int j = 0; j < 4; j++) {
                 const float p = x[2 * j], q = x[2 * j + 1];
-                x[2 * j] = fmaf(p, co[j], -(q * si[j]));
-                x[2 * j + 1] = fmaf(q, co[j], p * si[j]);
+                x[2 * j] = turns ? fmaf(p, co[j], -(q * si[j])) : p;  // not by an angle of 0: 0 times an infinity is NaN
+                x[2 * j + 1] = turns ? fmaf(q, co[j], p * si[j]) : q;
             }
         } else {
             f32x8 y;
             for (int j = 0; j < 8; j++) y[j] = __shfl(x[j], other, 64);
-            for (int j = 0; j < 8; j++) x[j] = fmaf(x[j], co[j], y[j] * si[j]);
+            for (int j = 0; j < 8; j++) x[j] = turns ? fmaf(x[j], co[j], y[j] * si[j]) : x[j];
         }
         T* to = kv < 0 ? (T*)a.d_q_out + ((int64_t)t * a.n_heads + row) * a.head_dim : (T*)a.cache.d_k + place + kv * a.cache.head_stride;
         if (inside && (kv < 0 || stored)) store8(to + c8, placed ? x : (f32x8)0.0f);
