@@ -56,7 +56,8 @@ class Server:
         q, key, value = self.project(tokens)
         new = torch.full((1,), tokens, dtype=torch.int32, device="cuda")
         plan = jx.kv_plan(self.len, new, self.table, self.free, self.n_free, PAGE, tokens)
-        self.n_free, self.len = plan.n_free, plan.kv_len
+        # kv_len is 0 where there was no room: such a step leaves the request as it was (its results are zeros)
+        self.n_free, self.len = plan.n_free, torch.where(plan.kv_len > 0, plan.kv_len, self.len)
         ready = jx.qk_norm_rope(q, key, value, self.k_cache, self.v_cache, plan.pos, plan.slot, self.cos, self.sin, self.weight, self.weight)
         part = jx.paged_attention(ready, self.k_cache, self.v_cache, self.table, plan.q_start, plan.kv_len, self.scale)
         if not self.moved:
