@@ -111,6 +111,7 @@ extern "C" {
 #define JX_MAX_BF_K 128 /* largest k of jx_bruteforce */
 #define JX_MAX_REQUESTS 8192 /* requests of one jx_kv_plan / jx_kv_release call */
 #define JX_MAX_HEAD_DIM 256 /* elements of an attention head */
+#define JX_MAX_POSITIONS 0x7FFFFC00 /* table_pages * page: the kernels look ahead of the last key, in 32 bits */
 #define JX_STATIC_SCRATCH_BYTES (16 << 20) /* device scratch of jx_bruteforce_static, held per GPU for the life of the process */
 
 typedef struct jx_index jx_index; /* opaque, host side */

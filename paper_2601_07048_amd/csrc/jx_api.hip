@@ -340,7 +340,7 @@ int check_cache(const jx_kv_cache& c) {
 
 int check_table(const int32_t* table, int table_pages, int page, int n_req) {
     if (n_req < 0) return fail(JX_EINVAL, "n_req < 0");
-    if (table_pages < 1 || (int64_t)table_pages * page > 0x7FFFFFFFll) return fail(JX_EINVAL, "table_pages out of range");
+    if (table_pages < 1 || (int64_t)table_pages * page > JX_MAX_POSITIONS) return fail(JX_EINVAL, "table_pages out of range");
     if (!table && n_req) return fail(JX_EINVAL, "d_table is NULL");
     return JX_OK;
 }

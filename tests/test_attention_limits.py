@@ -1,0 +1,27 @@
+"""Sizes and arguments that the attention entry points refuse, without a GPU: no kernel is launched."""
+import ctypes as C
+
+import pytest
+
+from test_attention_abi import HEX, cache, jx, refused  # noqa: F401  (jx is the fixture)
+
+
+def attend(jx, **kw):
+    base = dict(dtype=jx.BF16, n_heads=4, n_kv_heads=2, head_dim=64, n_tokens=3, d_q=HEX, q_token_stride=256, q_head_stride=64,
+                cache=cache(jx), d_table=HEX, table_pages=8, n_req=2, d_q_start=HEX, d_kv_len=HEX, scale=0.1, window=0, d_out=HEX, d_lse=None)
+    base.update(kw)
+    return jx.AttendArgs(**base)
+
+
+@pytest.mark.parametrize("page,table_pages", [(1, 0x7FFFFFFF), (16, (1 << 27) - 1), (4096, (1 << 19) - 1), (1, 0x7FFFFC01)])
+def test_tables_that_end_beside_2_to_31(jx, page, table_pages):
+    """The kernels look a few tiles ahead of the last key, in 32 bits."""
+    c = cache(jx, page=page)
+    if page * table_pages > 0x7FFFFC00:
+        refused(jx, jx._lib.jx_paged_attention_bytes(C.byref(attend(jx, cache=c, table_pages=table_pages))))
+        refused(jx, jx._lib.jx_paged_attention(C.byref(attend(jx, cache=c, table_pages=table_pages)), None, C.c_int64(0), None))
+        refused(jx, jx._lib.jx_kv_plan(HEX, HEX, 2, page, HEX, table_pages, HEX, HEX, 9, 2 * HEX, HEX, 3 * HEX, HEX, HEX, 5, None))
+        if page == 1:
+            refused(jx, jx._lib.jx_kv_release(HEX, HEX, 1, HEX, table_pages, HEX, HEX, 9, None))
+    largest = 0x7FFFFC00 // page
+    assert jx._lib.jx_paged_attention_bytes(C.byref(attend(jx, cache=c, table_pages=largest))) >= 0
