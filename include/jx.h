@@ -522,7 +522,7 @@ int jx_paged_attention(const jx_attend_args* args, void* d_work, int64_t work_by
  * returns them for the queries [n_tokens * n_heads]: d_ids [n_tokens][n_heads][k],
  * ids outside [0, n_rows) (JX_NONE among them) are passed over, an id that
  * occurs twice counts twice.  Row i, key head h of d_keys and d_values at
- * i * row_stride + h * head_stride.  With d_part_out [n_tokens][n_heads][head_dim]
+ * i * row_stride + h * head_stride, row_stride not negative.  With d_part_out [n_tokens][n_heads][head_dim]
  * and d_part_lse the result is that over both sets of keys, the list's and
  * those that the part came from (the part's weight is exp(lse); a part of
  * -infinity has none); both NULL: the list alone.  d_out may be d_part_out, d_lse

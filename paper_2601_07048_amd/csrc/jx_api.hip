@@ -1327,6 +1327,7 @@ int jx_found_attention(const jx_found_args* a, void* stream) {
     if (int rc = check_rows("d_out", a->d_out, 0, 0)) return rc;
     if (a->k && !a->d_ids) return fail(JX_EINVAL, "d_ids is NULL");
     if (a->k && a->n_rows) {
+        if (a->row_stride < 0) return fail(JX_EINVAL, "row_stride must not be negative");
         if (int rc = check_rows("d_keys", a->d_keys, a->row_stride, a->head_stride)) return rc;
         if (int rc = check_rows("d_values", a->d_values, 0, 0)) return rc;
     }

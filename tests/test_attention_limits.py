@@ -25,3 +25,17 @@ def test_tables_that_end_beside_2_to_31(jx, page, table_pages):
             refused(jx, jx._lib.jx_kv_release(HEX, HEX, 1, HEX, table_pages, HEX, HEX, 9, None))
     largest = 0x7FFFFC00 // page
     assert jx._lib.jx_paged_attention_bytes(C.byref(attend(jx, cache=c, table_pages=largest))) >= 0
+
+
+def found(jx, **kw):
+    base = dict(dtype=jx.F16, n_heads=4, n_kv_heads=2, head_dim=64, n_tokens=3, d_q=HEX, q_token_stride=256, q_head_stride=64, d_keys=HEX,
+                d_values=HEX, row_stride=128, head_stride=64, n_rows=5, d_ids=HEX, k=4, scale=0.1, d_part_out=None, d_part_lse=None, d_out=HEX,
+                d_lse=None)
+    base.update(kw)
+    return jx.FoundArgs(**base)
+
+
+@pytest.mark.parametrize("stride", [-128, -8, -(1 << 40)])
+def test_found_rows_that_lie_backwards(jx, stride):
+    """A negative offset stands for a row that is passed over."""
+    refused(jx, jx._lib.jx_found_attention(C.byref(found(jx, row_stride=stride)), None))
