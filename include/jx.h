@@ -413,8 +413,8 @@ int jx_encode_rotated(jx_index* idx, const float* d_rot, int64_t n, uint8_t* d_c
  * and may be anything that keeps each head's row on a 16-byte boundary (head
  * dimensions are multiples of 8, at most JX_MAX_HEAD_DIM).  Outputs are
  * contiguous [n_tokens][n_heads][head_dim].  Query head h reads key head
- * h / (n_heads / n_kv_heads).  Outputs may not overlap inputs where nothing
- * else is said.
+ * h / (n_heads / n_kv_heads).  Scales are finite, of any sign or 0.  Outputs may
+ * not overlap inputs where nothing else is said.
  */
 typedef struct {
     void* d_k;            /* keys:   page p, token i, head h at d_k + p * page_stride + i * token_stride + h * head_stride */

@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
+#include <cmath>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -345,12 +346,18 @@ int check_table(const int32_t* table, int table_pages, int page, int n_req) {
     return JX_OK;
 }
 
+int check_scale(float scale) {
+    if (!std::isfinite(scale)) return fail(JX_EINVAL, "scale must be finite");
+    return JX_OK;
+}
+
 int check_attend(const jx_attend_args* a) {
     if (!a) return fail(JX_EINVAL, "args is NULL");
     if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
     if (int rc = check_cache(a->cache)) return rc;
     if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
     if (a->window < 0) return fail(JX_EINVAL, "window < 0");
+    if (int rc = check_scale(a->scale)) return rc;
     if ((int64_t)a->n_req * a->n_kv_heads > 1 << 28) return fail(JX_EINVAL, "n_req * n_kv_heads out of range");
     return JX_OK;
 }
@@ -1321,6 +1328,7 @@ int jx_found_attention(const jx_found_args* a, void* stream) {
     if (!a) return fail(JX_EINVAL, "args is NULL");
     if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
     if (a->k < 0 || (a->k && (a->n_rows < 0 || a->n_rows > 0xFFFFFFFFll))) return fail(JX_EINVAL, "k or n_rows out of range");
+    if (int rc = check_scale(a->scale)) return rc;
     if (!a->d_part_out != !a->d_part_lse) return fail(JX_EINVAL, "d_part_out and d_part_lse belong together");
     if (a->n_tokens == 0) return JX_OK;
     if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;

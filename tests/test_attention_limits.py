@@ -39,3 +39,10 @@ def found(jx, **kw):
 def test_found_rows_that_lie_backwards(jx, stride):
     """A negative offset stands for a row that is passed over."""
     refused(jx, jx._lib.jx_found_attention(C.byref(found(jx, row_stride=stride)), None))
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf")])
+def test_scales_that_are_not_finite(jx, scale):
+    refused(jx, jx._lib.jx_paged_attention_bytes(C.byref(attend(jx, scale=scale))))
+    refused(jx, jx._lib.jx_paged_attention(C.byref(attend(jx, scale=scale)), None, C.c_int64(0), None))
+    refused(jx, jx._lib.jx_found_attention(C.byref(found(jx, scale=scale)), None))
