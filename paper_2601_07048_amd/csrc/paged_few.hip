@@ -65,7 +65,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
 
     const int page_mask = a.cache.page - 1;
     const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
-    const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);  // a scale of 0 has to leave -infinity what it is
+    const float c = fmaxf(fabsf(a.scale) * LOG2E, __FLT_MIN__);  // a scale of 0 has to leave -infinity what it is
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
     const lds_ptr mine = (lds_ptr)lds + wave * 2 * TILE;
     // a lane's place in 16 keys; of a head that ends inside a block the last chunk is read once more, against zeros of the queries

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
     if (d < R::CH * 8)  // what lies behind a head meets zeros of the queries, so it has to be a number
         for (int i = tid; i < 4 * TILE / 16; i += THREADS) *(uint4*)(lds + i * 16) = make_uint4(0, 0, 0, 0);
     const uint32_t page_chunks = (uint32_t)(a.cache.page_stride / 8), token_chunks = (uint32_t)(a.cache.token_stride / 8);
-    const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);  // a scale of 0 has to leave -infinity what it is
+    const float c = fmaxf(fabsf(a.scale) * LOG2E, __FLT_MIN__);  // a scale of 0 has to leave -infinity what it is
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
     while (sh.x0 < sh.x1) {
         const Segment e = sh.next<ROWS, 1>(g);
