@@ -441,7 +441,8 @@ typedef struct {
  * d_pos, d_slot [n_tokens]: position and slot (page * tokens of a page + place
  * in it) of every row, -1 where there was no room, in rows beyond the last
  * request, and (d_slot alone) where the table names no page; *d_n_free_out, how
- * many pages are left (not the same address as d_n_free).
+ * many pages are left.  d_kv_len may not be d_len or d_new, d_n_free_out not
+ * d_n_free.
  * n_req <= JX_MAX_REQUESTS.  The call only enqueues; nothing is read back.
  */
 int jx_kv_plan(const int32_t* d_len, const int32_t* d_new, int32_t n_req, int32_t page, int32_t* d_table, int32_t table_pages,

@@ -1268,6 +1268,7 @@ int jx_kv_plan(const int32_t* d_len, const int32_t* d_new, int32_t n_req, int32_
     if ((n_req && (!d_len || !d_new || !d_kv_len)) || !d_free || !d_n_free || !d_n_free_out || !d_q_start || (n_tokens && (!d_pos || !d_slot)))
         return fail(JX_EINVAL, "NULL argument");
     if (d_n_free_out == d_n_free) return fail(JX_EINVAL, "d_n_free_out must not be d_n_free");
+    if (n_req && (d_kv_len == d_len || d_kv_len == d_new)) return fail(JX_EINVAL, "d_kv_len must not be d_len or d_new");
     jx::KvPlanArgs a = {d_len, d_new, n_req, jx::log2_of(page), d_table, table_pages, d_free, d_n_free, n_pages,
                         d_n_free_out, d_q_start, d_kv_len, d_pos, d_slot, n_tokens};
     JX_HIP(jx::launch_kv_plan(a, as_stream(stream)));

@@ -46,3 +46,12 @@ def test_scales_that_are_not_finite(jx, scale):
     refused(jx, jx._lib.jx_paged_attention_bytes(C.byref(attend(jx, scale=scale))))
     refused(jx, jx._lib.jx_paged_attention(C.byref(attend(jx, scale=scale)), None, C.c_int64(0), None))
     refused(jx, jx._lib.jx_found_attention(C.byref(found(jx, scale=scale)), None))
+
+
+@pytest.mark.parametrize("same", [dict(d_kv_len=HEX), dict(d_kv_len=5 * HEX)])
+def test_plans_that_would_write_what_they_read(jx, same):
+    """Every workgroup reads the lengths and the new tokens, and the first one writes the new lengths."""
+    a = dict(d_len=HEX, d_new=5 * HEX, d_kv_len=3 * HEX)
+    a.update(same)
+    refused(jx, jx._lib.jx_kv_plan(a["d_len"], a["d_new"], 2, 16, HEX, 4, HEX, HEX, 9, 2 * HEX, HEX, a["d_kv_len"], HEX, HEX, 5, None))
+    assert b"d_kv_len" in jx._lib.jx_last_error()
