@@ -414,7 +414,10 @@ int jx_encode_rotated(jx_index* idx, const float* d_rot, int64_t n, uint8_t* d_c
  * dimensions are multiples of 8, at most JX_MAX_HEAD_DIM).  Outputs are
  * contiguous [n_tokens][n_heads][head_dim].  Query head h reads key head
  * h / (n_heads / n_kv_heads).  Scales are finite, of any sign or 0.  Outputs may
- * not overlap inputs where nothing else is said.
+ * not overlap inputs where nothing else is said.  A call is one or two launches, of less
+ * than 2^32 threads: n_tokens * n_heads <= 2^26 - 4 for jx_found_attention, and
+ * n_tokens * ceil((n_heads + 2 n_kv_heads) / 4) * 32 < 2^32 is enough for
+ * jx_qk_norm_rope; n_req * n_kv_heads <= 2^23 for jx_paged_attention.
  */
 typedef struct {
     void* d_k;            /* keys:   page p, token i, head h at d_k + p * page_stride + i * token_stride + h * head_stride */

@@ -30,6 +30,15 @@ hipError_t launch_found_attention(const jx_found_args& a, hipStream_t st);
 inline int row_lanes(int head_dim) { return head_dim <= 64 ? 8 : head_dim <= 128 ? 16 : 32; }
 inline int log2_of(int power) { return 31 - __builtin_clz((unsigned)power); }
 
+// Threads of a launch, in all; it has to be less than 2^32.  Norm and rotation: a group of lanes takes a head of a token, or four from as
+// many heads on as the card holds lanes at a time
+inline bool rope_many(const jx_rope_args& a) { return a.n_tokens * (a.n_heads + 2ll * a.n_kv_heads) * row_lanes(a.head_dim) > 256 * 2048; }
+inline int64_t rope_threads(const jx_rope_args& a) {
+    const int64_t rows = a.n_heads + 2ll * a.n_kv_heads;
+    return (a.n_tokens * (rope_many(a) ? (rows + 3) / 4 : rows) * row_lanes(a.head_dim) + 255) / 256 * 256;
+}
+inline int64_t found_threads(const jx_found_args& a) { return (a.n_tokens * a.n_heads + 3) / 4 * 256; }
+
 // ---- device ----------------------------------------------------------------------------------------------------------
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));

@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void found_attention_kernel(jx_found_args a) {
 
 template <typename T>
 hipError_t launch(const jx_found_args& a, hipStream_t st) {
-    const unsigned blocks = (unsigned)((a.n_tokens * a.n_heads + 3) / 4);
+    const unsigned blocks = (unsigned)(found_threads(a) / 256);
     const int lpr = row_lanes(a.head_dim);
     if (lpr == 8) found_attention_kernel<T, 8><<<blocks, 256, 0, st>>>(a);
     else if (lpr == 16) found_attention_kernel<T, 16><<<blocks, 256, 0, st>>>(a);

@@ -358,7 +358,8 @@ int check_attend(const jx_attend_args* a) {
     if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
     if (a->window < 0) return fail(JX_EINVAL, "window < 0");
     if (int rc = check_scale(a->scale)) return rc;
-    if ((int64_t)a->n_req * a->n_kv_heads > 1 << 28) return fail(JX_EINVAL, "n_req * n_kv_heads out of range");
+    // 256 threads for each tile, of which there are at most n_tokens * n_heads / 128 < 2^22, and one for each request and key head
+    if ((int64_t)a->n_req * a->n_kv_heads > 1 << 23) return fail(JX_EINVAL, "n_req * n_kv_heads out of range");
     return JX_OK;
 }
 
@@ -1293,6 +1294,7 @@ int jx_qk_norm_rope(const jx_rope_args* a, void* stream) {
         return fail(JX_EINVAL, "rot_dim must be a multiple of 16, at most head_dim");
     if (a->n_pos < 0 || a->n_pos > 0x7FFFFFFFll) return fail(JX_EINVAL, "n_pos out of range");
     if (!(a->eps >= 0.0f)) return fail(JX_EINVAL, "eps must be non-negative");
+    if (jx::rope_threads(*a) >= 1ll << 32) return fail(JX_EINVAL, "n_tokens out of range: 2^32 threads and more");
     if (int rc = check_cache(a->cache)) return rc;
     if (a->n_tokens == 0) return JX_OK;
     if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
@@ -1329,6 +1331,7 @@ int jx_found_attention(const jx_found_args* a, void* stream) {
     if (!a) return fail(JX_EINVAL, "args is NULL");
     if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
     if (a->k < 0 || (a->k && (a->n_rows < 0 || a->n_rows > 0xFFFFFFFFll))) return fail(JX_EINVAL, "k or n_rows out of range");
+    if (jx::found_threads(*a) >= 1ll << 32) return fail(JX_EINVAL, "n_tokens * n_heads out of range: 2^32 threads and more");
     if (int rc = check_scale(a->scale)) return rc;
     if (!a->d_part_out != !a->d_part_lse) return fail(JX_EINVAL, "d_part_out and d_part_lse belong together");
     if (a->n_tokens == 0) return JX_OK;

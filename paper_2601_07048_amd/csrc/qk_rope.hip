@@ -91,13 +91,9 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(jx_rope_args a, int p
 
 template <typename T, int LPR>
 hipError_t launch(const jx_rope_args& a, hipStream_t st) {
-    // from as many rows on as the card holds lanes at a time, a group takes four
-    const long long rows = a.n_heads + 2 * a.n_kv_heads;
-    const bool many = a.n_tokens * rows * LPR > 256 * 2048;
-    const long long groups = a.n_tokens * (many ? (rows + 3) / 4 : rows);
-    const unsigned blocks = (unsigned)((groups * LPR + 255) / 256);
+    const unsigned blocks = (unsigned)(rope_threads(a) / 256);
     const int shift = log2_of(a.cache.page);
-    if (many) qk_norm_rope_kernel<T, LPR, 4><<<blocks, 256, 0, st>>>(a, shift);
+    if (rope_many(a)) qk_norm_rope_kernel<T, LPR, 4><<<blocks, 256, 0, st>>>(a, shift);
     else qk_norm_rope_kernel<T, LPR, 1><<<blocks, 256, 0, st>>>(a, shift);
     return hipGetLastError();
 }

@@ -55,3 +55,27 @@ def test_plans_that_would_write_what_they_read(jx, same):
     a.update(same)
     refused(jx, jx._lib.jx_kv_plan(a["d_len"], a["d_new"], 2, 16, HEX, 4, HEX, HEX, 9, 2 * HEX, HEX, a["d_kv_len"], HEX, HEX, 5, None))
     assert b"d_kv_len" in jx._lib.jx_last_error()
+
+
+def rope(jx, **kw):
+    base = dict(dtype=jx.BF16, n_heads=4, n_kv_heads=2, head_dim=64, rot_dim=32, interleaved=0, n_tokens=3, n_pos=10, d_q=HEX, d_k=HEX, d_v=HEX,
+                q_token_stride=512, q_head_stride=64, k_token_stride=512, k_head_stride=64, v_token_stride=512, v_head_stride=64, d_q_weight=HEX,
+                d_k_weight=None, eps=1e-6, d_cos=HEX, d_sin=HEX, d_pos=HEX, d_slot=HEX, d_q_out=HEX, cache=cache(jx))
+    base.update(kw)
+    return jx.RopeArgs(**base)
+
+
+def test_calls_of_more_threads_than_a_launch_has(jx):
+    """A launch has less than 2^32 threads: 64 for a list of found rows, 8 to 32 for a head (or four) of a token, 256 for a tile."""
+    for heads, tokens in ((32, 1 << 21), (1, (1 << 26) - 3), (4096, 1 << 14)):
+        refused(jx, jx._lib.jx_found_attention(C.byref(found(jx, n_heads=heads, n_kv_heads=1, n_tokens=tokens)), None))
+        assert b"n_tokens" in jx._lib.jx_last_error()
+    for heads, kv, dim, tokens in ((1, 1, 256, 1 << 27), (32, 32, 256, 1 << 24), (8, 8, 64, 1 << 27 >> 1), (64, 64, 128, (1 << 32) // (48 * 16) + 1)):
+        refused(jx, jx._lib.jx_qk_norm_rope(C.byref(rope(jx, n_heads=heads, n_kv_heads=kv, head_dim=dim, n_tokens=tokens)), None))
+        assert b"n_tokens" in jx._lib.jx_last_error()
+    for n_req, kv in ((1 << 23, 2), ((1 << 23) + 1, 1), (1 << 20, 16)):
+        a = attend(jx, n_req=n_req, n_heads=16, n_kv_heads=kv)
+        refused(jx, jx._lib.jx_paged_attention_bytes(C.byref(a)))
+        refused(jx, jx._lib.jx_paged_attention(C.byref(a), None, C.c_int64(0), None))
+        assert b"n_req" in jx._lib.jx_last_error()
+    assert jx._lib.jx_paged_attention_bytes(C.byref(attend(jx, n_req=1 << 22, n_kv_heads=2))) >= 0
