@@ -378,9 +378,8 @@ _HEAD_TYPES = {torch.float16: F16, torch.bfloat16: BF16}
 _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
 
 
-def _run(fn, device, *args):
-    """Calls an entry point with the device's current stream as its last argument."""
-    i = device.index
+def _run(fn, i, *args):
+    """Calls an entry point with the current stream of GPU i as its last argument."""
     if torch.cuda.current_device() == i:
         rc = fn(*args, _raw_stream(i))
     else:
@@ -390,28 +389,36 @@ def _run(fn, device, *args):
         _check(rc)
 
 
-def _rows(t, dtype):
+def _gpu(t):
+    """The GPU of a call's first tensor; all the others have to be there too."""
+    i = t.get_device()
+    assert i >= 0, "not on a GPU"
+    return i
+
+
+def _rows(t, i, dtype):
     """A tensor of any strides whose last dimension holds a head's elements."""
-    assert t.is_cuda and t.dtype is dtype and (t.stride(-1) == 1 or t.shape[-1] == 1)
+    assert t.get_device() == i and t.dtype is dtype and (t.stride(-1) == 1 or t.shape[-1] == 1), (t.device, i, t.dtype)
     return t.data_ptr()
 
 
-def _array(t, dtype, *shape):
-    assert t.is_cuda and t.is_contiguous() and t.dtype is dtype and t.shape == shape, (t.dtype, tuple(t.shape), shape)
+def _array(t, i, dtype, *shape):
+    assert t.get_device() == i and t.is_contiguous() and t.dtype is dtype and t.shape == shape, (t.device, i, t.dtype, tuple(t.shape), shape)
     return t.data_ptr()
 
 
-def _kv_cache(k_cache, v_cache, dtype, head_dim):
+def _kv_cache(k_cache, v_cache, i, dtype, head_dim):
     pages, page, _, d = k_cache.shape
     strides = k_cache.stride()
     assert d == head_dim and v_cache.shape == k_cache.shape and v_cache.stride() == strides
-    return KvCache(_rows(k_cache, dtype), _rows(v_cache, dtype), strides[0], strides[1], strides[2], page, pages)
+    return KvCache(_rows(k_cache, i, dtype), _rows(v_cache, i, dtype), strides[0], strides[1], strides[2], page, pages)
 
 
 def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
     """jx_kv_plan: `table` gets the new pages in place; `n_free` stays, the number left is in the result.  n_tokens: rows of the
     step (the host's bound on the sum of `new`).  `out`: a KvPlan to write into."""
     n, w, f = lens.shape[0], table.shape[1], free.shape[0]
+    i = _gpu(lens)
     if out is None:
         # the 64-bit slots first, then the 32-bit arrays, in one allocation
         block = torch.empty(3 * n_tokens + 2 * n + 2, dtype=_I32, device=lens.device)
@@ -423,18 +430,19 @@ def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
         p_len = p_start + 4 * (n + 1)
         p_left = p_len + 4 * n
     else:
-        p_left, p_start, p_len = _array(out.n_free, _I32, 1), _array(out.q_start, _I32, n + 1), _array(out.kv_len, _I32, n)
-        p_pos, p_slot = _array(out.pos, _I32, n_tokens), _array(out.slot, _I64, n_tokens)
-    _run(_lib.jx_kv_plan, lens.device, _array(lens, _I32, n), _array(new, _I32, n), n, page, _array(table, _I32, n, w), w,
-         _array(free, _I32, f), _array(n_free, _I32, 1), f, p_left, p_start, p_len, p_pos, p_slot, n_tokens)
+        p_left, p_start, p_len = _array(out.n_free, i, _I32, 1), _array(out.q_start, i, _I32, n + 1), _array(out.kv_len, i, _I32, n)
+        p_pos, p_slot = _array(out.pos, i, _I32, n_tokens), _array(out.slot, i, _I64, n_tokens)
+    _run(_lib.jx_kv_plan, i, _array(lens, i, _I32, n), _array(new, i, _I32, n), n, page, _array(table, i, _I32, n, w), w,
+         _array(free, i, _I32, f), _array(n_free, i, _I32, 1), f, p_left, p_start, p_len, p_pos, p_slot, n_tokens)
     return out
 
 
 def kv_release(first, end, table, free, n_free):
     """jx_kv_release: pages first[r] .. end[r] - 1 of row r go back; `table`, `free` and `n_free` are updated in place."""
     n, w, f = first.shape[0], table.shape[1], free.shape[0]
-    _run(_lib.jx_kv_release, table.device, _array(first, _I32, n), _array(end, _I32, n), n, _array(table, _I32, n, w), w,
-         _array(free, _I32, f), _array(n_free, _I32, 1), f)
+    i = _gpu(table)
+    _run(_lib.jx_kv_release, i, _array(first, i, _I32, n), _array(end, i, _I32, n), n, _array(table, i, _I32, n, w), w,
+         _array(free, i, _I32, f), _array(n_free, i, _I32, 1), f)
 
 
 def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
@@ -443,30 +451,30 @@ def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_wei
     go to their slots of the caches [pages][page][kv_heads][head_dim] (any strides, alike in both)."""
     t, h, d = q.shape
     kv = k_cache.shape[2]
-    dt = q.dtype
+    dt, i = q.dtype, _gpu(q)
     if out is None:
         out = torch.empty((t, h, d), dtype=dt, device=q.device)
     else:
-        _array(out, dt, t, h, d)
+        _array(out, i, dt, t, h, d)
     n_pos, half = cos.shape if cos is not None else (0x7FFFFFFF, 0)
     assert k.shape == v.shape == (t, kv, d)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
-    a = RopeArgs(_HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, dt), _rows(k, dt), _rows(v, dt), qs[0], qs[1], ks[0],
-                 ks[1], vs[0], vs[1], _array(q_weight, dt, d) if q_weight is not None else None,
-                 _array(k_weight, dt, d) if k_weight is not None else None, eps, _array(cos, _F32, n_pos, half) if half else None,
-                 _array(sin, _F32, n_pos, half) if half else None, _array(pos, _I32, t), _array(slot, _I64, t), out.data_ptr(),
-                 _kv_cache(k_cache, v_cache, dt, d))
-    _run(_lib.jx_qk_norm_rope, q.device, C.byref(a))
+    a = RopeArgs(_HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt), _rows(k, i, dt), _rows(v, i, dt), qs[0], qs[1], ks[0],
+                 ks[1], vs[0], vs[1], _array(q_weight, i, dt, d) if q_weight is not None else None,
+                 _array(k_weight, i, dt, d) if k_weight is not None else None, eps, _array(cos, i, _F32, n_pos, half) if half else None,
+                 _array(sin, i, _F32, n_pos, half) if half else None, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
+                 _kv_cache(k_cache, v_cache, i, dt, d))
+    _run(_lib.jx_qk_norm_rope, i, C.byref(a))
     return out
 
 
-def _outputs(out, q, t, h, d):
+def _outputs(out, q, i, t, h, d):
     """The pair to write into, made here if there is none, and its pointers."""
     if out is None:
         o, lse = torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device)
         return o, lse, o.data_ptr(), lse.data_ptr()
     o, lse = out
-    return o, lse, _array(o, q.dtype, t, h, d), _array(lse, _F32, t, h) if lse is not None else None
+    return o, lse, _array(o, i, q.dtype, t, h, d), _array(lse, i, _F32, t, h) if lse is not None else None
 
 
 def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
@@ -474,11 +482,11 @@ def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0
     `work`: a uint8 tensor as large as the call needs (made here where it is None)."""
     t, h, d = q.shape
     n, w = table.shape
-    dt = q.dtype
-    o, lse, p_out, p_lse = _outputs(out, q, t, h, d)
+    dt, i = q.dtype, _gpu(q)
+    o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
     qs = q.stride()
-    a = AttendArgs(_HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, dt, d),
-                   _array(table, _I32, n, w), w, n, _array(q_start, _I32, n + 1), _array(kv_len, _I32, n), scale, window, p_out, p_lse)
+    a = AttendArgs(_HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, i, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, i, dt, d),
+                   _array(table, i, _I32, n, w), w, n, _array(q_start, i, _I32, n + 1), _array(kv_len, i, _I32, n), scale, window, p_out, p_lse)
     ref = C.byref(a)
     if work is None:
         nbytes = _lib.jx_paged_attention_bytes(ref)
@@ -487,8 +495,8 @@ def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0
         work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
     else:
         nbytes = work.shape[0]
-        _array(work, torch.uint8, nbytes)
-    _run(_lib.jx_paged_attention, q.device, ref, work.data_ptr(), nbytes)
+        _array(work, i, torch.uint8, nbytes)
+    _run(_lib.jx_paged_attention, i, ref, work.data_ptr(), nbytes)
     return o, lse
 
 
@@ -498,14 +506,14 @@ def found_attention(q, keys, values, ids, scale, part=None, out=None):
     t, h, d = q.shape
     n, kv, kd = keys.shape
     k = ids.shape[2]
-    dt = q.dtype
-    o, lse, p_out, p_lse = _outputs(out, q, t, h, d)
+    dt, i = q.dtype, _gpu(q)
+    o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
     qs, ks = q.stride(), keys.stride()
     assert kd == d and values.shape == keys.shape and values.stride() == ks
-    a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, dt), qs[0], qs[1], _rows(keys, dt), _rows(values, dt), ks[0], ks[1], n,
-                  _array(ids, _I32, t, h, k), k, scale, _array(part[0], dt, t, h, d) if part else None,
-                  _array(part[1], _F32, t, h) if part else None, p_out, p_lse)
-    _run(_lib.jx_found_attention, q.device, C.byref(a))
+    a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt), qs[0], qs[1], _rows(keys, i, dt), _rows(values, i, dt), ks[0], ks[1], n,
+                  _array(ids, i, _I32, t, h, k), k, scale, _array(part[0], i, dt, t, h, d) if part else None,
+                  _array(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
+    _run(_lib.jx_found_attention, i, C.byref(a))
     return o, lse
 
 
