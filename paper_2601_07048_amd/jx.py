@@ -372,7 +372,8 @@ def probe_gather(table: torch.Tensor, rec_bytes: int, ids: torch.Tensor, blocks:
 
 
 # -- attention beside the index: jx_kv_plan .. jx_found_attention.  These are called many times in each step of a model, over
-# operands of a few microseconds' work: their checks are written to be quick.
+# operands of a few microseconds' work: their checks are written to be quick.  They are a serving program's: inputs that require a gradient
+# are refused unless gradients are switched off.
 
 _HEAD_TYPES = {torch.float16: F16, torch.bfloat16: BF16}
 _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
@@ -396,8 +397,13 @@ def _gpu(t):
     return i
 
 
+def _no_gradient(t):
+    assert not (t.requires_grad and torch.is_grad_enabled()), "no gradient goes through the attention calls: make them under torch.no_grad()"
+
+
 def _rows(t, i, dtype):
     """A tensor of any strides whose last dimension holds a head's elements."""
+    _no_gradient(t)
     assert t.get_device() == i and t.dtype is dtype and (t.stride(-1) == 1 or t.shape[-1] == 1), (t.device, i, t.dtype)
     return t.data_ptr()
 
@@ -405,6 +411,12 @@ def _rows(t, i, dtype):
 def _array(t, i, dtype, *shape):
     assert t.get_device() == i and t.is_contiguous() and t.dtype is dtype and t.shape == shape, (t.device, i, t.dtype, tuple(t.shape), shape)
     return t.data_ptr()
+
+
+def _real(t, i, dtype, *shape):
+    """An array that a model may have learnt or made."""
+    _no_gradient(t)
+    return _array(t, i, dtype, *shape)
 
 
 def _kv_cache(k_cache, v_cache, i, dtype, head_dim):
@@ -460,9 +472,9 @@ def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_wei
     assert k.shape == v.shape == (t, kv, d)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     a = RopeArgs(_HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt), _rows(k, i, dt), _rows(v, i, dt), qs[0], qs[1], ks[0],
-                 ks[1], vs[0], vs[1], _array(q_weight, i, dt, d) if q_weight is not None else None,
-                 _array(k_weight, i, dt, d) if k_weight is not None else None, eps, _array(cos, i, _F32, n_pos, half) if half else None,
-                 _array(sin, i, _F32, n_pos, half) if half else None, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
+                 ks[1], vs[0], vs[1], _real(q_weight, i, dt, d) if q_weight is not None else None,
+                 _real(k_weight, i, dt, d) if k_weight is not None else None, eps, _real(cos, i, _F32, n_pos, half) if half else None,
+                 _real(sin, i, _F32, n_pos, half) if half else None, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
                  _kv_cache(k_cache, v_cache, i, dt, d))
     _run(_lib.jx_qk_norm_rope, i, C.byref(a))
     return out
@@ -511,8 +523,8 @@ def found_attention(q, keys, values, ids, scale, part=None, out=None):
     qs, ks = q.stride(), keys.stride()
     assert kd == d and values.shape == keys.shape and values.stride() == ks
     a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt), qs[0], qs[1], _rows(keys, i, dt), _rows(values, i, dt), ks[0], ks[1], n,
-                  _array(ids, i, _I32, t, h, k), k, scale, _array(part[0], i, dt, t, h, d) if part else None,
-                  _array(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
+                  _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else None,
+                  _real(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
     _run(_lib.jx_found_attention, i, C.byref(a))
     return o, lse
 

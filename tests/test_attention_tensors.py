@@ -102,3 +102,21 @@ def test_a_tensor_that_is_elsewhere(noted, call, name, device):
     with pytest.raises(AssertionError):
         run(jx, tensors)
     assert not lib.made
+
+
+LEARNT = [(call, name) for call, name in NAMES if name in
+          ("q", "k", "v", "k_cache", "v_cache", "keys", "values", "q_weight", "k_weight", "cos", "sin", "part", "part_lse")]
+
+
+@pytest.mark.parametrize("call,name", LEARNT)
+def test_a_gradient_that_would_be_lost(noted, call, name):
+    jx, lib = noted
+    run, tensors = calls()[call]
+    tensors[name].requires_grad = True
+    with pytest.raises(AssertionError, match="gradient"):
+        run(jx, tensors)
+    assert not lib.made
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            run(jx, tensors)
+    assert lib.made == ["jx_" + call] * 2
