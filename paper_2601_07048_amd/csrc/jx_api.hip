@@ -319,9 +319,10 @@ int check_heads(int dtype, int heads, int kv_heads, int dim, int64_t tokens) {
     return JX_OK;
 }
 
-int check_rows(const char* what, const void* p, int64_t s0, int64_t s1) {
+// Rows n0 x n1 at strides s0 and s1; the stride of a dimension of one has no meaning
+int check_rows(const char* what, const void* p, int64_t n0 = 1, int64_t s0 = 0, int64_t n1 = 1, int64_t s1 = 0) {
     if (!p) return fail(JX_EINVAL, "%s is NULL", what);
-    if (off16(p) || s0 % 8 || s1 % 8) return fail(JX_EINVAL, "%s: rows must lie on 16-byte boundaries", what);
+    if (off16(p) || (n0 > 1 && s0 % 8) || (n1 > 1 && s1 % 8)) return fail(JX_EINVAL, "%s: rows must lie on 16-byte boundaries", what);
     return JX_OK;
 }
 
@@ -331,12 +332,12 @@ int check_page(int page, int n_pages) {
     return JX_OK;
 }
 
-int check_cache(const jx_kv_cache& c) {
+int check_cache(const jx_kv_cache& c, int kv_heads) {
     if (int rc = check_page(c.page, c.n_pages)) return rc;
     if (c.page_stride < 0 || c.token_stride < 0 || c.head_stride < 0 || c.page_stride >> 34 || c.token_stride >> 34)
         return fail(JX_EINVAL, "cache strides must be below 2^34 and not negative");
-    if (int rc = check_rows("cache.d_k", c.d_k, c.page_stride, c.token_stride)) return rc;
-    return check_rows("cache.d_v", c.d_v, c.head_stride, 0);
+    if (int rc = check_rows("cache.d_k", c.d_k, c.n_pages, c.page_stride, c.page, c.token_stride)) return rc;
+    return check_rows("cache.d_v", c.d_v, kv_heads, c.head_stride);
 }
 
 int check_table(const int32_t* table, int table_pages, int page, int n_req) {
@@ -354,7 +355,7 @@ int check_scale(float scale) {
 int check_attend(const jx_attend_args* a) {
     if (!a) return fail(JX_EINVAL, "args is NULL");
     if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
-    if (int rc = check_cache(a->cache)) return rc;
+    if (int rc = check_cache(a->cache, a->n_kv_heads)) return rc;
     if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
     if (a->window < 0) return fail(JX_EINVAL, "window < 0");
     if (int rc = check_scale(a->scale)) return rc;
@@ -1295,12 +1296,12 @@ int jx_qk_norm_rope(const jx_rope_args* a, void* stream) {
     if (a->n_pos < 0 || a->n_pos > 0x7FFFFFFFll) return fail(JX_EINVAL, "n_pos out of range");
     if (!(a->eps >= 0.0f)) return fail(JX_EINVAL, "eps must be non-negative");
     if (jx::rope_threads(*a) >= 1ll << 32) return fail(JX_EINVAL, "n_tokens out of range: 2^32 threads and more");
-    if (int rc = check_cache(a->cache)) return rc;
+    if (int rc = check_cache(a->cache, a->n_kv_heads)) return rc;
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
-    if (int rc = check_rows("d_k", a->d_k, a->k_token_stride, a->k_head_stride)) return rc;
-    if (int rc = check_rows("d_v", a->d_v, a->v_token_stride, a->v_head_stride)) return rc;
-    if (int rc = check_rows("d_q_out", a->d_q_out, 0, 0)) return rc;
+    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_k", a->d_k, a->n_tokens, a->k_token_stride, a->n_kv_heads, a->k_head_stride)) return rc;
+    if (int rc = check_rows("d_v", a->d_v, a->n_tokens, a->v_token_stride, a->n_kv_heads, a->v_head_stride)) return rc;
+    if (int rc = check_rows("d_q_out", a->d_q_out)) return rc;
     if (off16(a->d_q_weight) || off16(a->d_k_weight)) return fail(JX_EINVAL, "weights must lie on 16-byte boundaries");
     if (a->rot_dim && (!a->d_cos || !a->d_sin || off16(a->d_cos) || off16(a->d_sin)))
         return fail(JX_EINVAL, "d_cos and d_sin must lie on 16-byte boundaries");
@@ -1317,8 +1318,8 @@ int64_t jx_paged_attention_bytes(const jx_attend_args* a) {
 int jx_paged_attention(const jx_attend_args* a, void* d_work, int64_t work_bytes, void* stream) {
     if (int rc = check_attend(a)) return rc;
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
-    if (int rc = check_rows("d_out", a->d_out, 0, 0)) return rc;
+    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_out", a->d_out)) return rc;
     if (a->n_req && (!a->d_q_start || !a->d_kv_len)) return fail(JX_EINVAL, "NULL argument");
     const int64_t need = jx::paged_attention_bytes(*a);
     if (need && (!d_work || ((uintptr_t)d_work & 255))) return fail(JX_EINVAL, "d_work must be 256-byte aligned");
@@ -1335,13 +1336,13 @@ int jx_found_attention(const jx_found_args* a, void* stream) {
     if (int rc = check_scale(a->scale)) return rc;
     if (!a->d_part_out != !a->d_part_lse) return fail(JX_EINVAL, "d_part_out and d_part_lse belong together");
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_rows("d_q", a->d_q, a->q_token_stride, a->q_head_stride)) return rc;
-    if (int rc = check_rows("d_out", a->d_out, 0, 0)) return rc;
+    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_out", a->d_out)) return rc;
     if (a->k && !a->d_ids) return fail(JX_EINVAL, "d_ids is NULL");
     if (a->k && a->n_rows) {
         if (a->row_stride < 0) return fail(JX_EINVAL, "row_stride must not be negative");
-        if (int rc = check_rows("d_keys", a->d_keys, a->row_stride, a->head_stride)) return rc;
-        if (int rc = check_rows("d_values", a->d_values, 0, 0)) return rc;
+        if (int rc = check_rows("d_keys", a->d_keys, a->n_rows, a->row_stride, a->n_kv_heads, a->head_stride)) return rc;
+        if (int rc = check_rows("d_values", a->d_values)) return rc;
     }
     if (off16(a->d_part_out)) return fail(JX_EINVAL, "d_part_out: rows must lie on 16-byte boundaries");
     JX_HIP(jx::launch_found_attention(*a, as_stream(stream)));

@@ -419,10 +419,18 @@ def _real(t, i, dtype, *shape):
     return _array(t, i, dtype, *shape)
 
 
+def _alike(a, b):
+    """Whether two tensors are laid out alike; the stride of a dimension of one has no meaning."""
+    if a.shape != b.shape:
+        return False
+    sa, sb = a.stride(), b.stride()
+    return sa == sb or all(n <= 1 or x == y for n, x, y in zip(a.shape, sa, sb))
+
+
 def _kv_cache(k_cache, v_cache, i, dtype, head_dim):
     pages, page, _, d = k_cache.shape
     strides = k_cache.stride()
-    assert d == head_dim and v_cache.shape == k_cache.shape and v_cache.stride() == strides
+    assert d == head_dim and _alike(k_cache, v_cache)
     return KvCache(_rows(k_cache, i, dtype), _rows(v_cache, i, dtype), strides[0], strides[1], strides[2], page, pages)
 
 
@@ -521,7 +529,7 @@ def found_attention(q, keys, values, ids, scale, part=None, out=None):
     dt, i = q.dtype, _gpu(q)
     o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
     qs, ks = q.stride(), keys.stride()
-    assert kd == d and values.shape == keys.shape and values.stride() == ks
+    assert kd == d and _alike(keys, values)
     a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt), qs[0], qs[1], _rows(keys, i, dt), _rows(values, i, dt), ks[0], ks[1], n,
                   _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else None,
                   _real(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
