@@ -36,7 +36,7 @@ __device__ __forceinline__ long long block_before(long long v, long long* part, 
 // enough; the first one also writes what there is once per request.  A page's entry in the table is written by the token
 // at its first position, which knows the page's place among the free ones; only tokens that go on in a page begun earlier read
 // the table, and those entries nobody writes.
-// Bound: a chain of dependent reads (lengths, sums, table or free page), not bytes: 5.8 us for 64 requests of a token, 8.0 for 1,000
+// Bound: a chain of dependent reads (lengths, sums, table or free page), not bytes: 6 us for 64 requests of a token, 8 for 1,000
 // requests of up to 512.
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(KvPlanArgs a) {
     extern __shared__ int32_t places[];  // [n_req + 1] first row, [n_req] pages asked for before this request, -1 = no room
@@ -116,8 +116,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(KvPlanArgs a) {
     a.slot[t] = slot;
 }
 
-// Bound: latency, as for the plan.  One workgroup: a wavefront counts the pages that a request gives back, the counts become places, and a second walk writes
-// them, in the order of requests and pages whatever the timing.
+// One workgroup: a wavefront counts the pages that a request gives back, the counts become places, and a second walk writes them, in
+// the order of requests and pages whatever the timing.  Bound: for a few requests latency, as for the plan (7 us for a row of 640
+// entries), for many what one CU reads, the table twice (26 us for 64 such rows, 1.5 ms for 1,000 of 2,000 entries).
 __global__ __launch_bounds__(PLAN_THREADS) void kv_release_kernel(const int32_t* first, const int32_t* end, int n_req, int32_t* table,
                                                                  int table_pages, int32_t* free_pages, int32_t* n_free, int n_pages) {
     extern __shared__ int32_t places[];  // [n_req] pages given back, then their place

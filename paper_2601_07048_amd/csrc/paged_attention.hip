@@ -13,8 +13,8 @@ constexpr int JOINERS(int nb) { return nb <= 4 ? 1 : 2; }
 // The parts of a tile whose keys several workgroups share, as one: the tile that workgroup blockIdx.x began and did not end;
 // blockIdx.y: which 32 rows.  A wavefront takes 8 elements, as the lanes held them when the parts were written, and of few rows
 // two or four pieces side by side.  Bound: the time that a chain of reads takes, hence PIECES at once, but two or four where there
-// are no more (8 always: 27 and not 16 us for a chunk of 4,096 tokens): single tokens of 64 requests 4.9 us, 40 MB of parts of
-// 256 elements 15.5.
+// are no more (8 always: 27 and not 16 us for a chunk of 4,096 tokens): single tokens of 64 requests 4.8 us, 40 MB of parts of
+// 256 elements 15.2.
 template <typename T, int NB>
 __global__ __launch_bounds__(NB * 256 / JOINERS(NB)) void join_kernel(PagedArgs g) {
     constexpr int PIECES = 8;
@@ -95,7 +95,8 @@ Plan make_plan(const jx_attend_args& a) {
     // cache has little room for each request, since a request of more rows reads its keys once for every tile (32 or 128 rows: 64
     // requests of up to 8 tokens, 4 heads, up to 300 keys 20 or 31 us; 32 of up to 16 tokens, 4,000 keys 69 or 55).
     // Many rows: 256 where most tiles are full (256 or 128 rows: a chunk of 4,096 over 16,384 keys 967 or 1,080 us; eight
-    // chunks of up to 512 152 or 131).
+    // chunks of up to 512 152 or 131).  One height for all requests, by their mean: 256 single tokens of 4,000 keys and a chunk of 512
+    // are all taken 16 rows at a time, in 877 us; 735 and 68 apart.
     const bool pages = a.cache.page >= 16 && a.cache.token_stride < (1 << 25);
     const bool little = (int64_t)a.cache.n_pages * a.cache.page <= 512ll * a.n_req;
     const long long full = a.n_req == 1 ? 512 : 2048;
@@ -105,7 +106,8 @@ Plan make_plan(const jx_attend_args& a) {
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     // Few tiles of few rows and few keys (a table with little room, a short window): a workgroup a tile, which its wavefronts put
-    // together, and no second launch.  128 elements, 8 key heads, 16 requests of up to 256 or 512 keys: 8.9 or 12.7 us, shared out
+    // together, and no second launch.  The host has the room, not the lengths: neither this nor 32 rows is taken where pool and table
+    // are sized for more than the step's requests hold.  128 elements, 8 key heads, 16 requests of up to 256 or 512 keys: 8.9 or 12.7 us, shared out
     // 11.1 or 12.5; 64 requests 18 or 16.  64 elements, 16 key heads, 16 requests of up to 1,024 keys: 10.9, shared out 18.4.
     const int64_t room = (int64_t)a.table_pages * a.cache.page, keys = a.window ? std::min<int64_t>(room, (int64_t)a.window + 16) : room;
     p.own = p.rows < 128 && (int64_t)p.slots * a.n_kv_heads <= 384 && keys <= 1024 / (nb <= 2 ? 1 : nb);

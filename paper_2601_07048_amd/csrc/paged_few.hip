@@ -46,7 +46,7 @@ __device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {
 // only when its share is done.  Wavefronts that took a tile's keys in turn lost a fifth of the time where they met at its end.
 // The shares of a workgroup follow each other, so that tiles which they cut are put together in LDS, and only those which the
 // workgroup itself found begun or leaves open are left for join_kernel.  Few short tiles are a workgroup's own (g.own) and joined by it.
-// 64 requests of up to 8,192 keys, 8 key heads of 128 elements: 138 us, 5.0 TB/s; 4 of up to 131,072: 254 us, 5.5 TB/s; one of 777: 7.4.
+// 64 requests of up to 8,192 keys, 8 key heads of 128 elements: 138 us, 5.0 TB/s; 4 of up to 131,072: 255 us, 5.5 TB/s; one of 777: 8.
 template <typename T, int NC, int RB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     constexpr int ROWS = RB * 16, KEYS = 32, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32, PITCH = CH * 16, TILE = KEYS * PITCH;

@@ -35,7 +35,7 @@ __device__ __forceinline__ float both_halves_sum(float x) {
 // of the first are taken in the same order.  The running maximum moves only when a row's scores rise by more than 2^8 over it:
 // weights of up to 2^8 round no worse, and most tiles leave the sums alone.
 // Bound: the matrix instructions, and with them the card's power: a chunk of 4,096 tokens over 16,384 keys, 32 heads of 128 elements,
-// 965 us or 1.0 PFLOP/s of the products at a clock that falls to 1.7 GHz.  32 rows a wavefront, since 64 need more registers than there are
+// 952 us a call with the join's 15, or 1.0 PFLOP/s of the products, at a clock that falls to 1.7 GHz.  32 rows a wavefront, since 64 need more registers than there are
 // (slower by the spills); 8 wavefronts over the same keys halve what is read again.  256 elements have one wavefront on a SIMD:
 // 0.5 to 0.6 PFLOP/s; two there, with 32 of the 64 keys each, were not faster (their registers spill).
 template <typename T, int NB>

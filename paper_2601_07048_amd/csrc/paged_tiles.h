@@ -7,7 +7,7 @@ namespace jx {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys; of more there are enough without
+constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys, see Shares
 
 // A tile whose keys several workgroups share: part 2 group + 1 of the first of them, 2 group of the pieces - 1 that follow.  0 pieces: none
 struct __attribute__((aligned(16))) Join {
@@ -24,8 +24,9 @@ struct PagedArgs {
     int groups, n_work;     // workgroups, and shares of all tiles (1 or FEW_WAVES for each workgroup); 0 = a share a tile
     int part_rows;          // tiles' rows / 32
     int own;                // few rows, n_work = 0: whether a workgroup takes a tile, not a wavefront
-    float* part;            // [2 groups][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's keys, sums [NB][4][64][4], largest scores and
-                            // weights' sums [2][32]; the sums as a wavefront holds them, see part_at
+    float* part;            // [2 groups][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's
+                            // keys, sums [NB][4][64][4], largest scores and weights' sums [2][32]; the sums as a wavefront holds
+                            // them, see part_at
     Join* joins;            // [groups]
 };
 
@@ -51,11 +52,13 @@ __device__ __forceinline__ int by_group(const PagedArgs& g, int n) {
     return g.group == 1 ? n : (int)(__umulhi((uint32_t)n, g.group_mul) >> g.group_shift);
 }
 
-// Weights are 2^(score - m), m = the running maximum less BELOW, and rounded to the element type for their product with the values
-// (half the matrix instructions that two parts would take).  binary16 has nothing under 2^-25: with weights of up to 1, 2^8 after a
-// rise that leaves m alone, the values of keys 18 and more nats under the largest vanish from the sum while their weights stay in
-// the divisor (of 60,000 such keys beside one that has the maximum 98 % of what they add).  So they go up to 2^7, 2^15 after a rise, and what is lost
-// of a key is at most 2^-32 of the largest weight.  bfloat16 has the exponents of 32 bits.
+// Weights are 2^(score - m), m = the running maximum less BELOW, and rounded to the element type for their product with the values:
+// two parts of a weight would take half as many matrix instructions again, which bound chunks.  What that costs, against 64 bits: 0.0023
+// of the result's size in bfloat16 and 0.00029 in binary16, where 32-bit weights and the rounding of the result have 0.0017 and 0.00021.
+// binary16 has nothing under 2^-25: with weights of up to 1, 2^8 after a rise that leaves m alone, the values of keys 18 and
+// more nats under the largest vanish from the sum while their weights stay in the divisor (of 60,000 such keys beside one that has
+// the maximum 98 % of what they add).  So they go up to 2^7, 2^15 after a rise, and what is lost of a key is at most 2^-32 of the
+// largest weight.  bfloat16 has the exponents of 32 bits.
 template <typename T>
 constexpr float BELOW = __is_same(T, _Float16) ? 7.0f : 0.0f;
 
@@ -135,7 +138,9 @@ constexpr int part_floats(int nb) { return nb * 1024 + 64; }
 // All tiles of all key heads, UNIT keys of one a unit, are cut into equal shares, whatever the lengths of the requests are, one for each
 // workgroup (many rows) or wavefront (few); where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its
 // shares for itself: from the first rows and lengths of all requests (8 bytes each) it counts the units of every slot and adds them up
-// in LDS.  With more than MAX_SLOTS slots there are tiles enough, and each is a share.
+// in LDS.  With more than MAX_SLOTS slots there are tiles enough to fill the card, and each is a share: that holds for like lengths (1,000
+// single tokens of up to 512 keys, 4 heads a group: 251 us), while one long request among so many is read by a wavefront alone (one
+// of 131,072 keys: 10.6 ms).
 constexpr int UNIT = 64;
 
 struct Segment {  // units u0 .. u1 - 1 of the tile's

@@ -11,8 +11,9 @@ namespace {
 // Bound: bytes.  A group of LPR lanes holds one head's row, eight elements (16 bytes) a lane, so a row is read and written
 // once and the norm is a sum over the group; the other half of a rotated pair is in the lane rot_dim / 16 further on (or in
 // the same lane where neighbours are paired).  Sums, norm and rotation are in 32 bits, rounded once when stored.  With many
-// tokens a group takes ROWS heads of one: as many reads on their way, and the angles once.  8,191 tokens of 48 heads of 128
-// elements: 38 us, 5.3 TB/s read and written (one head a group: 44); 64 tokens: 4.0 us.
+// tokens a group takes ROWS heads of one: as many reads on their way, and the angles once (8,191 tokens of 48 heads of 128
+// elements, a call: 46.6 us, with one head a group 52).  The kernel then takes 45 us on inputs that no cache holds, 4.5 TB/s read
+// and written; 64 tokens 3.8.
 template <typename T, int LPR, int ROWS>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(jx_rope_args a, int page_shift) {
     typedef typename Vec<T>::x8 X8;
