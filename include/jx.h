@@ -549,6 +549,51 @@ typedef struct {
 } jx_found_args;
 int jx_found_attention(const jx_found_args* args, void* stream);
 
+/*
+ * ---- The same over keys and values of 8 bits --------------------------------
+ *
+ * Half the memory, and half the bytes of a decode step.  A value is
+ *   code * 2^(byte - 127),
+ * the code an e4m3 number (sign, 4 bits of exponent, 3 of mantissa, no
+ * infinities, 0x7F and 0xFF not a number), the byte one for each block of tokens
+ * and key head, keys and values apart (e8m0; 255: what the block holds is not a
+ * number).  A record of arguments is the one of the call without the 8, with
+ * d_k, d_v (d_keys, d_values) at codes, strides in codes, every row of codes on
+ * a 16-byte boundary, head dimensions multiples of 16.  dtype is that of the queries and outputs.
+ * Codes times their scale enter products as they are where that type has the
+ * number: bfloat16 from 2^-133 on, binary16 from 2^-24 up to 65504.
+ */
+typedef struct {
+    uint8_t *d_k, *d_v; /* paged: [n_pages][page / block][n_kv_heads]; found rows: [ceil(n_rows / block)][n_kv_heads] */
+    int32_t block;      /* tokens of a block: a power of two, at most 64 and (paged) at most a page */
+} jx_kv_scales;
+
+/*
+ * jx_qk_norm_rope into such a cache.  Keys and values of the step's rows that
+ * lie in one block, E the largest exponent among their sizes |y| (floor(log2)):
+ *   scale = 2^(E - 7), or the block's present one if that is larger and tokens
+ *           stand in front of the first new one,  at least 2^-126
+ *   codes = y / scale, rounded once (largest ones: 128 up to 256)
+ * and, where the scale has grown, the codes in front of the first new one are
+ * brought to the new scale (rounded again only under 2^-6 scales).  So tokens are
+ * appended one at a time or many at once; what stands behind the last new
+ * one is left as it is and does not count.  Sizes over 15 * 2^12 (JX_F16), 15 * 2^124
+ * (JX_BF16) are held as those; infinities and what is not a number are held as
+ * not a number and take no part in E.
+ * Rows of one block follow one another, in the order of their slots, as jx_kv_plan
+ * gives them; rows that are not stored stand elsewhere.
+ * n_tokens * n_kv_heads * 512 + n_tokens * n_heads * 32 < 2^32 is enough.
+ */
+int jx_qk_norm_rope8(const jx_rope_args* args, const jx_kv_scales* scales, void* stream);
+
+/* jx_paged_attention over such a cache; work_bytes as jx_paged_attention8_bytes says. */
+int64_t jx_paged_attention8_bytes(const jx_attend_args* args, const jx_kv_scales* scales);
+int jx_paged_attention8(const jx_attend_args* args, const jx_kv_scales* scales, void* d_work, int64_t work_bytes, void* stream);
+
+/* jx_found_attention over rows of codes, row i in block i / block: whole blocks
+ * of a paged cache, one after the other, are such rows.  The part and the outputs are of `dtype`. */
+int jx_found_attention8(const jx_found_args* args, const jx_kv_scales* scales, void* stream);
+
 const char* jx_strerror(int code);
 const char* jx_last_error(void);
 

@@ -25,6 +25,11 @@ hipError_t launch_qk_norm_rope(const jx_rope_args& a, hipStream_t st);
 int64_t paged_attention_bytes(const jx_attend_args& a);
 hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStream_t st);
 hipError_t launch_found_attention(const jx_found_args& a, hipStream_t st);
+// the same over keys and values of 8 bits
+hipError_t launch_qk_norm_rope8(const jx_rope_args& a, const jx_kv_scales& s, hipStream_t st);
+int64_t paged_attention8_bytes(const jx_attend_args& a, const jx_kv_scales& s);
+hipError_t launch_paged_attention8(const jx_attend_args& a, const jx_kv_scales& s, uint8_t* work, hipStream_t st);
+hipError_t launch_found_attention8(const jx_found_args& a, const jx_kv_scales& s, hipStream_t st);
 
 // the smallest power of two of 8-element chunks that holds a row, 8..32
 inline int row_lanes(int head_dim) { return head_dim <= 64 ? 8 : head_dim <= 128 ? 16 : 32; }
@@ -36,6 +41,21 @@ inline bool rope_many(const jx_rope_args& a) { return a.n_tokens * (a.n_heads + 
 inline int64_t rope_threads(const jx_rope_args& a) {
     const int64_t rows = a.n_heads + 2ll * a.n_kv_heads;
     return (a.n_tokens * (rope_many(a) ? (rows + 3) / 4 : rows) * row_lanes(a.head_dim) + 255) / 256 * 256;
+}
+// Into a cache of 8 bits: 256 / lanes of a row heads, or four times as many, for each workgroup of the queries; a workgroup for each
+// key head's keys or values of `rows` tokens
+struct Rope8Grid {
+    int q_rows, rows;
+    int64_t q_blocks, kv_blocks;
+};
+inline Rope8Grid rope8_grid(const jx_rope_args& a, int block) {
+    Rope8Grid g;
+    const int lpr = row_lanes(a.head_dim);
+    g.q_rows = a.n_tokens * a.n_heads * lpr > 256 * 2048 ? 4 : 1;
+    g.q_blocks = (a.n_tokens * ((a.n_heads + g.q_rows - 1) / g.q_rows) * lpr + 255) / 256;
+    g.rows = a.n_tokens * 2 * a.n_kv_heads <= 16384 ? 1 : block;
+    g.kv_blocks = (a.n_tokens + g.rows - 1) / g.rows * 2 * a.n_kv_heads;
+    return g;
 }
 inline int64_t found_threads(const jx_found_args& a) { return (a.n_tokens * a.n_heads + 3) / 4 * 256; }
 

@@ -319,10 +319,10 @@ int check_heads(int dtype, int heads, int kv_heads, int dim, int64_t tokens) {
     return JX_OK;
 }
 
-// Rows n0 x n1 at strides s0 and s1; the stride of a dimension of one has no meaning
-int check_rows(const char* what, const void* p, int64_t n0 = 1, int64_t s0 = 0, int64_t n1 = 1, int64_t s1 = 0) {
+// Rows n0 x n1 at strides s0 and s1; the stride of a dimension of one has no meaning.  chunk: elements of 16 bytes
+int check_rows(const char* what, const void* p, int64_t n0 = 1, int64_t s0 = 0, int64_t n1 = 1, int64_t s1 = 0, int chunk = 8) {
     if (!p) return fail(JX_EINVAL, "%s is NULL", what);
-    if (off16(p) || (n0 > 1 && s0 % 8) || (n1 > 1 && s1 % 8)) return fail(JX_EINVAL, "%s: rows must lie on 16-byte boundaries", what);
+    if (off16(p) || (n0 > 1 && s0 % chunk) || (n1 > 1 && s1 % chunk)) return fail(JX_EINVAL, "%s: rows must lie on 16-byte boundaries", what);
     return JX_OK;
 }
 
@@ -332,12 +332,25 @@ int check_page(int page, int n_pages) {
     return JX_OK;
 }
 
-int check_cache(const jx_kv_cache& c, int kv_heads) {
+int check_cache(const jx_kv_cache& c, int kv_heads, int chunk = 8) {
     if (int rc = check_page(c.page, c.n_pages)) return rc;
     if (c.page_stride < 0 || c.token_stride < 0 || c.head_stride < 0 || c.page_stride >> 34 || c.token_stride >> 34)
         return fail(JX_EINVAL, "cache strides must be below 2^34 and not negative");
-    if (int rc = check_rows("cache.d_k", c.d_k, c.n_pages, c.page_stride, c.page, c.token_stride)) return rc;
-    return check_rows("cache.d_v", c.d_v, kv_heads, c.head_stride);
+    if (int rc = check_rows("cache.d_k", c.d_k, c.n_pages, c.page_stride, c.page, c.token_stride, chunk)) return rc;
+    return check_rows("cache.d_v", c.d_v, kv_heads, c.head_stride, 1, 0, chunk);
+}
+
+// Of keys and values in 8 bits; most: tokens that a block may have
+int check_scales(const jx_kv_scales* s, int dim, int most) {
+    if (!s) return fail(JX_EINVAL, "scales is NULL");
+    if (s->block < 1 || s->block > most || (s->block & (s->block - 1)))
+        return fail(JX_EINVAL, "scales.block must be a power of two, at most 64 and at most a page");
+    if (dim % 16) return fail(JX_EINVAL, "head_dim must be a multiple of 16");
+    return JX_OK;
+}
+int check_scales_there(const jx_kv_scales* s) {
+    if (!s->d_k || !s->d_v) return fail(JX_EINVAL, "scales: d_k or d_v is NULL");
+    return JX_OK;
 }
 
 int check_table(const int32_t* table, int table_pages, int page, int n_req) {
@@ -352,15 +365,74 @@ int check_scale(float scale) {
     return JX_OK;
 }
 
-int check_attend(const jx_attend_args* a) {
+int check_rope(const jx_rope_args* a) {
     if (!a) return fail(JX_EINVAL, "args is NULL");
     if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
-    if (int rc = check_cache(a->cache, a->n_kv_heads)) return rc;
+    if (a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16)
+        return fail(JX_EINVAL, "rot_dim must be a multiple of 16, at most head_dim");
+    if (a->n_pos < 0 || a->n_pos > 0x7FFFFFFFll) return fail(JX_EINVAL, "n_pos out of range");
+    if (!(a->eps >= 0.0f)) return fail(JX_EINVAL, "eps must be non-negative");
+    return JX_OK;
+}
+
+int check_rope_rows(const jx_rope_args* a) {
+    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_k", a->d_k, a->n_tokens, a->k_token_stride, a->n_kv_heads, a->k_head_stride)) return rc;
+    if (int rc = check_rows("d_v", a->d_v, a->n_tokens, a->v_token_stride, a->n_kv_heads, a->v_head_stride)) return rc;
+    if (int rc = check_rows("d_q_out", a->d_q_out)) return rc;
+    if (off16(a->d_q_weight) || off16(a->d_k_weight)) return fail(JX_EINVAL, "weights must lie on 16-byte boundaries");
+    if (a->rot_dim && (!a->d_cos || !a->d_sin || off16(a->d_cos) || off16(a->d_sin)))
+        return fail(JX_EINVAL, "d_cos and d_sin must lie on 16-byte boundaries");
+    if (!a->d_pos || !a->d_slot) return fail(JX_EINVAL, "NULL argument");
+    return JX_OK;
+}
+
+int check_attend(const jx_attend_args* a, int chunk = 8) {
+    if (!a) return fail(JX_EINVAL, "args is NULL");
+    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
+    if (int rc = check_cache(a->cache, a->n_kv_heads, chunk)) return rc;
     if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
     if (a->window < 0) return fail(JX_EINVAL, "window < 0");
     if (int rc = check_scale(a->scale)) return rc;
     // 256 threads for each tile, of which there are at most n_tokens * n_heads / 128 < 2^22, and one for each request and key head
     if ((int64_t)a->n_req * a->n_kv_heads > 1 << 23) return fail(JX_EINVAL, "n_req * n_kv_heads out of range");
+    return JX_OK;
+}
+
+int check_attend8(const jx_attend_args* a, const jx_kv_scales* s) {
+    if (int rc = check_attend(a, 16)) return rc;
+    return check_scales(s, a->head_dim, std::min(64, a->cache.page));
+}
+
+int check_attend_rows(const jx_attend_args* a, int64_t need, const void* d_work, int64_t work_bytes) {
+    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_out", a->d_out)) return rc;
+    if (a->n_req && (!a->d_q_start || !a->d_kv_len)) return fail(JX_EINVAL, "NULL argument");
+    if (need && (!d_work || ((uintptr_t)d_work & 255))) return fail(JX_EINVAL, "d_work must be 256-byte aligned");
+    if (work_bytes < need) return fail(JX_ECAPACITY, "work_bytes: %lld needed", (long long)need);
+    return JX_OK;
+}
+
+int check_found(const jx_found_args* a) {
+    if (!a) return fail(JX_EINVAL, "args is NULL");
+    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
+    if (a->k < 0 || (a->k && (a->n_rows < 0 || a->n_rows > 0xFFFFFFFFll))) return fail(JX_EINVAL, "k or n_rows out of range");
+    if (jx::found_threads(*a) >= 1ll << 32) return fail(JX_EINVAL, "n_tokens * n_heads out of range: 2^32 threads and more");
+    if (int rc = check_scale(a->scale)) return rc;
+    if (!a->d_part_out != !a->d_part_lse) return fail(JX_EINVAL, "d_part_out and d_part_lse belong together");
+    return JX_OK;
+}
+
+int check_found_rows(const jx_found_args* a, int chunk) {
+    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
+    if (int rc = check_rows("d_out", a->d_out)) return rc;
+    if (a->k && !a->d_ids) return fail(JX_EINVAL, "d_ids is NULL");
+    if (a->k && a->n_rows) {
+        if (a->row_stride < 0) return fail(JX_EINVAL, "row_stride must not be negative");
+        if (int rc = check_rows("d_keys", a->d_keys, a->n_rows, a->row_stride, a->n_kv_heads, a->head_stride, chunk)) return rc;
+        if (int rc = check_rows("d_values", a->d_values)) return rc;
+    }
+    if (off16(a->d_part_out)) return fail(JX_EINVAL, "d_part_out: rows must lie on 16-byte boundaries");
     return JX_OK;
 }
 
@@ -1289,24 +1361,25 @@ int jx_kv_release(const int32_t* d_first, const int32_t* d_end, int32_t n_req, i
 }
 
 int jx_qk_norm_rope(const jx_rope_args* a, void* stream) {
-    if (!a) return fail(JX_EINVAL, "args is NULL");
-    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
-    if (a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16)
-        return fail(JX_EINVAL, "rot_dim must be a multiple of 16, at most head_dim");
-    if (a->n_pos < 0 || a->n_pos > 0x7FFFFFFFll) return fail(JX_EINVAL, "n_pos out of range");
-    if (!(a->eps >= 0.0f)) return fail(JX_EINVAL, "eps must be non-negative");
+    if (int rc = check_rope(a)) return rc;
     if (jx::rope_threads(*a) >= 1ll << 32) return fail(JX_EINVAL, "n_tokens out of range: 2^32 threads and more");
     if (int rc = check_cache(a->cache, a->n_kv_heads)) return rc;
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
-    if (int rc = check_rows("d_k", a->d_k, a->n_tokens, a->k_token_stride, a->n_kv_heads, a->k_head_stride)) return rc;
-    if (int rc = check_rows("d_v", a->d_v, a->n_tokens, a->v_token_stride, a->n_kv_heads, a->v_head_stride)) return rc;
-    if (int rc = check_rows("d_q_out", a->d_q_out)) return rc;
-    if (off16(a->d_q_weight) || off16(a->d_k_weight)) return fail(JX_EINVAL, "weights must lie on 16-byte boundaries");
-    if (a->rot_dim && (!a->d_cos || !a->d_sin || off16(a->d_cos) || off16(a->d_sin)))
-        return fail(JX_EINVAL, "d_cos and d_sin must lie on 16-byte boundaries");
-    if (!a->d_pos || !a->d_slot) return fail(JX_EINVAL, "NULL argument");
+    if (int rc = check_rope_rows(a)) return rc;
     JX_HIP(jx::launch_qk_norm_rope(*a, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_qk_norm_rope8(const jx_rope_args* a, const jx_kv_scales* scales, void* stream) {
+    if (int rc = check_rope(a)) return rc;
+    if (int rc = check_cache(a->cache, a->n_kv_heads, 16)) return rc;
+    if (int rc = check_scales(scales, a->head_dim, std::min(64, a->cache.page))) return rc;
+    const jx::Rope8Grid n = jx::rope8_grid(*a, scales->block);
+    if (n.q_blocks + n.kv_blocks >= 1 << 24) return fail(JX_EINVAL, "n_tokens out of range: 2^32 threads and more");
+    if (a->n_tokens == 0) return JX_OK;
+    if (int rc = check_rope_rows(a)) return rc;
+    if (int rc = check_scales_there(scales)) return rc;
+    JX_HIP(jx::launch_qk_norm_rope8(*a, *scales, as_stream(stream)));
     return JX_OK;
 }
 
@@ -1318,34 +1391,41 @@ int64_t jx_paged_attention_bytes(const jx_attend_args* a) {
 int jx_paged_attention(const jx_attend_args* a, void* d_work, int64_t work_bytes, void* stream) {
     if (int rc = check_attend(a)) return rc;
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
-    if (int rc = check_rows("d_out", a->d_out)) return rc;
-    if (a->n_req && (!a->d_q_start || !a->d_kv_len)) return fail(JX_EINVAL, "NULL argument");
-    const int64_t need = jx::paged_attention_bytes(*a);
-    if (need && (!d_work || ((uintptr_t)d_work & 255))) return fail(JX_EINVAL, "d_work must be 256-byte aligned");
-    if (work_bytes < need) return fail(JX_ECAPACITY, "work_bytes: %lld needed", (long long)need);
+    if (int rc = check_attend_rows(a, jx::paged_attention_bytes(*a), d_work, work_bytes)) return rc;
     JX_HIP(jx::launch_paged_attention(*a, (uint8_t*)d_work, as_stream(stream)));
     return JX_OK;
 }
 
-int jx_found_attention(const jx_found_args* a, void* stream) {
-    if (!a) return fail(JX_EINVAL, "args is NULL");
-    if (int rc = check_heads(a->dtype, a->n_heads, a->n_kv_heads, a->head_dim, a->n_tokens)) return rc;
-    if (a->k < 0 || (a->k && (a->n_rows < 0 || a->n_rows > 0xFFFFFFFFll))) return fail(JX_EINVAL, "k or n_rows out of range");
-    if (jx::found_threads(*a) >= 1ll << 32) return fail(JX_EINVAL, "n_tokens * n_heads out of range: 2^32 threads and more");
-    if (int rc = check_scale(a->scale)) return rc;
-    if (!a->d_part_out != !a->d_part_lse) return fail(JX_EINVAL, "d_part_out and d_part_lse belong together");
+int64_t jx_paged_attention8_bytes(const jx_attend_args* a, const jx_kv_scales* scales) {
+    if (int rc = check_attend8(a, scales)) return rc;
+    return jx::paged_attention8_bytes(*a, *scales);
+}
+
+int jx_paged_attention8(const jx_attend_args* a, const jx_kv_scales* scales, void* d_work, int64_t work_bytes, void* stream) {
+    if (int rc = check_attend8(a, scales)) return rc;
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_rows("d_q", a->d_q, a->n_tokens, a->q_token_stride, a->n_heads, a->q_head_stride)) return rc;
-    if (int rc = check_rows("d_out", a->d_out)) return rc;
-    if (a->k && !a->d_ids) return fail(JX_EINVAL, "d_ids is NULL");
-    if (a->k && a->n_rows) {
-        if (a->row_stride < 0) return fail(JX_EINVAL, "row_stride must not be negative");
-        if (int rc = check_rows("d_keys", a->d_keys, a->n_rows, a->row_stride, a->n_kv_heads, a->head_stride)) return rc;
-        if (int rc = check_rows("d_values", a->d_values)) return rc;
-    }
-    if (off16(a->d_part_out)) return fail(JX_EINVAL, "d_part_out: rows must lie on 16-byte boundaries");
+    if (int rc = check_attend_rows(a, jx::paged_attention8_bytes(*a, *scales), d_work, work_bytes)) return rc;
+    if (int rc = check_scales_there(scales)) return rc;
+    JX_HIP(jx::launch_paged_attention8(*a, *scales, (uint8_t*)d_work, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_found_attention(const jx_found_args* a, void* stream) {
+    if (int rc = check_found(a)) return rc;
+    if (a->n_tokens == 0) return JX_OK;
+    if (int rc = check_found_rows(a, 8)) return rc;
     JX_HIP(jx::launch_found_attention(*a, as_stream(stream)));
+    return JX_OK;
+}
+
+int jx_found_attention8(const jx_found_args* a, const jx_kv_scales* scales, void* stream) {
+    if (int rc = check_found(a)) return rc;
+    if (int rc = check_scales(scales, a->head_dim, 64)) return rc;
+    if (a->n_tokens == 0) return JX_OK;
+    if (int rc = check_found_rows(a, 16)) return rc;
+    if (a->k && a->n_rows)
+        if (int rc = check_scales_there(scales)) return rc;
+    JX_HIP(jx::launch_found_attention8(*a, *scales, as_stream(stream)));
     return JX_OK;
 }
 

@@ -1,7 +1,6 @@
 // Queries and keys of a step made ready for attention: RMS norm per head, rotation by position, keys and values stored in the
 // paged cache, in one pass over the projection's output.
-#include "attend.h"
-#include "jx_device.h"
+#include "rope_row.h"
 
 namespace jx {
 
@@ -37,25 +36,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(jx_rope_args a, int p
                                 : (const T*)a.d_v + t * a.v_token_stride + v * a.v_head_stride;
         raw[r] = inside && row < rows && (kv < 0 ? placed : stored) ? *(const X8*)(from + c8) : (X8)(T)0.0f;
     }
-    // the angles: of four pairs, or of the eight elements beside those of the other half
-    const int half = a.rot_dim / 2, step = half / 8;
-    const bool low = c < step, turns = placed && c8 < a.rot_dim;
-    f32x8 co = {1, 1, 1, 1, 1, 1, 1, 1}, si = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (turns) {
-        const float *cs = a.d_cos + (size_t)pos * half, *sn = a.d_sin + (size_t)pos * half;
-        if (a.interleaved) {
-            for (int j = 0; j < 4; j++) {
-                co[j] = cs[c * 4 + j];
-                si[j] = sn[c * 4 + j];
-            }
-        } else {
-            co = *(const f32x8*)(cs + (low ? c : c - step) * 8);
-            si = *(const f32x8*)(sn + (low ? c : c - step) * 8);
-            if (low)
-                for (int j = 0; j < 8; j++) si[j] = -si[j];
-        }
-    }
-    const int other = lane_id() + (low ? step : c8 < a.rot_dim ? -step : 0);
+    const Angles angles = angles_at(a, pos, placed, c);
 #pragma unroll
     for (int r = 0; r < ROWS; r++) {
         const int row = row0 + r, kv = row - a.n_heads, v = kv - a.n_kv_heads;
@@ -63,28 +44,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(jx_rope_args a, int p
             if (row < rows && stored && inside) *(X8*)((T*)a.cache.d_v + place + v * a.cache.head_stride + c8) = raw[r];
             continue;
         }
-        f32x8 x = __builtin_convertvector(raw[r], f32x8);
-        const T* w = (const T*)(kv < 0 ? a.d_q_weight : a.d_k_weight);
-        if (w) {
-            float s = 0.0f;
-            for (int j = 0; j < 8; j++) s = fmaf(x[j], x[j], s);
-            s = group_sum<LPR>(s);
-            const float n = 1.0f / sqrtf(s / (float)a.head_dim + a.eps);
-            f32x8 g = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (inside) g = load8(w + c8);
-            for (int j = 0; j < 8; j++) x[j] = x[j] * n * g[j];
-        }
-        if (a.interleaved) {
-            for (int j = 0; j < 4; j++) {
-                const float p = x[2 * j], q = x[2 * j + 1];
-                x[2 * j] = turns ? fmaf(p, co[j], -(q * si[j])) : p;  // not by an angle of 0: 0 times an infinity is NaN
-                x[2 * j + 1] = turns ? fmaf(q, co[j], p * si[j]) : q;
-            }
-        } else {
-            f32x8 y;
-            for (int j = 0; j < 8; j++) y[j] = __shfl(x[j], other, 64);
-            for (int j = 0; j < 8; j++) x[j] = turns ? fmaf(x[j], co[j], y[j] * si[j]) : x[j];
-        }
+        const f32x8 x = norm_and_turn<T, LPR>(a, __builtin_convertvector(raw[r], f32x8), (const T*)(kv < 0 ? a.d_q_weight : a.d_k_weight), inside, c8, angles);
         T* to = kv < 0 ? (T*)a.d_q_out + ((int64_t)t * a.n_heads + row) * a.head_dim : (T*)a.cache.d_k + place + kv * a.cache.head_stride;
         if (inside && (kv < 0 || stored)) store8(to + c8, placed ? x : (f32x8)0.0f);
     }

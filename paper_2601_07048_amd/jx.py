@@ -36,6 +36,7 @@ EXPORTS = [
     "jx_rotate_points", "jx_encode_rotated", "jx_delete", "jx_consolidate", "jx_compact", "jx_deleted_count", "jx_probe_gather", "jx_mips_augment", "jx_strerror", "jx_last_error",
     "jx_bruteforce_static", "jx_bruteforce_kernel", "jx_set_flags",
     "jx_kv_plan", "jx_kv_release", "jx_qk_norm_rope", "jx_paged_attention_bytes", "jx_paged_attention", "jx_found_attention",
+    "jx_qk_norm_rope8", "jx_paged_attention8_bytes", "jx_paged_attention8", "jx_found_attention8",
 ]
 
 
@@ -89,6 +90,10 @@ class FoundArgs(C.Structure):
                 ("d_part_out", C.c_void_p), ("d_part_lse", C.c_void_p), ("d_out", C.c_void_p), ("d_lse", C.c_void_p)]
 
 
+class KvScales(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("block", C.c_int32)]
+
+
 class KvPlan(NamedTuple):
     """What jx_kv_plan writes beside the table."""
     q_start: torch.Tensor
@@ -113,13 +118,16 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.jx_strerror.restype = C.c_char_p
     lib.jx_last_error.restype = C.c_char_p
     lib.jx_bruteforce_kernel.restype = C.c_char_p
-    lib.jx_paged_attention_bytes.restype = C.c_int64
+    lib.jx_paged_attention_bytes.restype = lib.jx_paged_attention8_bytes.restype = C.c_int64
     p, i, n = C.c_void_p, C.c_int32, C.c_int64
     lib.jx_kv_plan.argtypes = [p, p, i, i, p, i, p, p, i, p, p, p, p, p, n, p]
     lib.jx_kv_release.argtypes = [p, p, i, p, i, p, p, i, p]
     lib.jx_qk_norm_rope.argtypes = lib.jx_found_attention.argtypes = [p, p]
+    lib.jx_qk_norm_rope8.argtypes = lib.jx_found_attention8.argtypes = [p, p, p]
     lib.jx_paged_attention_bytes.argtypes = [p]
     lib.jx_paged_attention.argtypes = [p, p, n, p]
+    lib.jx_paged_attention8_bytes.argtypes = [p, p]
+    lib.jx_paged_attention8.argtypes = [p, p, p, n, p]
     for name in EXPORTS:
         getattr(lib, name)  # fail loudly on a missing symbol
     return lib
@@ -377,6 +385,7 @@ def probe_gather(table: torch.Tensor, rec_bytes: int, ids: torch.Tensor, blocks:
 
 _HEAD_TYPES = {torch.float16: F16, torch.bfloat16: BF16}
 _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
 def _run(fn, i, *args):
@@ -434,6 +443,14 @@ def _kv_cache(k_cache, v_cache, i, dtype, head_dim):
     return KvCache(_rows(k_cache, i, dtype), _rows(v_cache, i, dtype), strides[0], strides[1], strides[2], page, pages)
 
 
+def _kv_scales(k_cache, k_scale, v_scale, i):
+    """Scales of a paged cache of codes; the block follows from their shape."""
+    pages, page, kv, _ = k_cache.shape
+    blocks = k_scale.shape[1]
+    assert blocks >= 1 and page % blocks == 0, (page, blocks)
+    return KvScales(_real(k_scale, i, _E8M0, pages, blocks, kv), _real(v_scale, i, _E8M0, pages, blocks, kv), page // blocks)
+
+
 def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
     """jx_kv_plan: `table` gets the new pages in place; `n_free` stays, the number left is in the result.  n_tokens: rows of the
     step (the host's bound on the sum of `new`).  `out`: a KvPlan to write into."""
@@ -465,10 +482,8 @@ def kv_release(first, end, table, free, n_free):
          _array(free, i, _I32, f), _array(n_free, i, _I32, 1), f)
 
 
-def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
-                 out=None):
-    """jx_qk_norm_rope: the queries [tokens][heads][head_dim] made ready (in `out`, which may be a contiguous q); keys and values
-    go to their slots of the caches [pages][page][kv_heads][head_dim] (any strides, alike in both)."""
+def _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, eps, interleaved, out, of_cache):
+    """(queries made ready, the GPU, the record) of a call; of_cache: type of the cache, None: the queries'."""
     t, h, d = q.shape
     kv = k_cache.shape[2]
     dt, i = q.dtype, _gpu(q)
@@ -479,12 +494,29 @@ def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_wei
     n_pos, half = cos.shape if cos is not None else (0x7FFFFFFF, 0)
     assert k.shape == v.shape == (t, kv, d)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
-    a = RopeArgs(_HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt), _rows(k, i, dt), _rows(v, i, dt), qs[0], qs[1], ks[0],
-                 ks[1], vs[0], vs[1], _real(q_weight, i, dt, d) if q_weight is not None else None,
-                 _real(k_weight, i, dt, d) if k_weight is not None else None, eps, _real(cos, i, _F32, n_pos, half) if half else None,
-                 _real(sin, i, _F32, n_pos, half) if half else None, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
-                 _kv_cache(k_cache, v_cache, i, dt, d))
+    return out, i, RopeArgs(
+        _HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt), _rows(k, i, dt), _rows(v, i, dt), qs[0], qs[1], ks[0],
+        ks[1], vs[0], vs[1], _real(q_weight, i, dt, d) if q_weight is not None else None,
+        _real(k_weight, i, dt, d) if k_weight is not None else None, eps, _real(cos, i, _F32, n_pos, half) if half else None,
+        _real(sin, i, _F32, n_pos, half) if half else None, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
+        _kv_cache(k_cache, v_cache, i, of_cache or dt, d))
+
+
+def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                 out=None):
+    """jx_qk_norm_rope: the queries [tokens][heads][head_dim] made ready (in `out`, which may be a contiguous q); keys and values
+    go to their slots of the caches [pages][page][kv_heads][head_dim] (any strides, alike in both)."""
+    out, i, a = _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, eps, interleaved, out, None)
     _run(_lib.jx_qk_norm_rope, i, C.byref(a))
+    return out
+
+
+def qk_norm_rope8(q, k, v, k_cache, v_cache, k_scale, v_scale, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6,
+                  interleaved=False, out=None):
+    """jx_qk_norm_rope8: as qk_norm_rope, into caches of torch.float8_e4m3fn with scales [pages][blocks of a page][kv_heads] of
+    torch.float8_e8m0fnu, both of which it updates."""
+    out, i, a = _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, eps, interleaved, out, _E4M3)
+    _run(_lib.jx_qk_norm_rope8, i, C.byref(a), C.byref(_kv_scales(k_cache, k_scale, v_scale, i)))
     return out
 
 
@@ -497,43 +529,79 @@ def _outputs(out, q, i, t, h, d):
     return o, lse, _array(o, i, q.dtype, t, h, d), _array(lse, i, _F32, t, h) if lse is not None else None
 
 
-def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
-    """jx_paged_attention: (out [tokens][heads][head_dim], lse [tokens][heads]).  `out`: those two, to write into (lse may be None);
-    `work`: a uint8 tensor as large as the call needs (made here where it is None)."""
+def _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, of_cache):
+    """(out, lse, the GPU, the record) of a call; of_cache: type of the cache."""
     t, h, d = q.shape
     n, w = table.shape
     dt, i = q.dtype, _gpu(q)
     o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
     qs = q.stride()
-    a = AttendArgs(_HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, i, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, i, dt, d),
-                   _array(table, i, _I32, n, w), w, n, _array(q_start, i, _I32, n + 1), _array(kv_len, i, _I32, n), scale, window, p_out, p_lse)
-    ref = C.byref(a)
+    return o, lse, i, AttendArgs(
+        _HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, i, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, i, of_cache or dt, d),
+        _array(table, i, _I32, n, w), w, n, _array(q_start, i, _I32, n + 1), _array(kv_len, i, _I32, n), scale, window, p_out, p_lse)
+
+
+def _with_work(work, q, i, size, fn, *refs):
+    """Calls fn with `work`, or with as many bytes as `size` asks for."""
     if work is None:
-        nbytes = _lib.jx_paged_attention_bytes(ref)
+        nbytes = size(*refs)
         if nbytes < 0:
             _check(int(nbytes))
         work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
     else:
         nbytes = work.shape[0]
         _array(work, i, torch.uint8, nbytes)
-    _run(_lib.jx_paged_attention, i, ref, work.data_ptr(), nbytes)
+    _run(fn, i, *refs, work.data_ptr(), nbytes)
+
+
+def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
+    """jx_paged_attention: (out [tokens][heads][head_dim], lse [tokens][heads]).  `out`: those two, to write into (lse may be None);
+    `work`: a uint8 tensor as large as the call needs (made here where it is None)."""
+    o, lse, i, a = _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, None)
+    _with_work(work, q, i, _lib.jx_paged_attention_bytes, _lib.jx_paged_attention, C.byref(a))
     return o, lse
+
+
+def paged_attention8(q, k_cache, v_cache, k_scale, v_scale, table, q_start, kv_len, scale, window=0, out=None, work=None):
+    """jx_paged_attention8: as paged_attention, over caches and scales as qk_norm_rope8 fills them."""
+    o, lse, i, a = _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, _E4M3)
+    _with_work(work, q, i, _lib.jx_paged_attention8_bytes, _lib.jx_paged_attention8, C.byref(a), C.byref(_kv_scales(k_cache, k_scale, v_scale, i)))
+    return o, lse
+
+
+def _found(q, keys, values, ids, scale, part, out, of_rows):
+    """(out, lse, the GPU, the record) of a call; of_rows: type of keys and values."""
+    t, h, d = q.shape
+    n, kv, kd = keys.shape
+    k = ids.shape[2]
+    dt, i = q.dtype, _gpu(q)
+    of_rows = of_rows or dt
+    o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
+    qs, ks = q.stride(), keys.stride()
+    assert kd == d and _alike(keys, values)
+    return o, lse, i, FoundArgs(
+        _HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt), qs[0], qs[1], _rows(keys, i, of_rows), _rows(values, i, of_rows), ks[0], ks[1], n,
+        _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else None,
+        _real(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
 
 
 def found_attention(q, keys, values, ids, scale, part=None, out=None):
     """jx_found_attention: (out, lse) over the rows ids [tokens][heads][k] of keys and values [rows][kv_heads][head_dim] (any
     strides, alike in both), joined with part = (out, lse) of other keys if given.  `out`: two tensors to write into (may be `part`)."""
-    t, h, d = q.shape
-    n, kv, kd = keys.shape
-    k = ids.shape[2]
-    dt, i = q.dtype, _gpu(q)
-    o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
-    qs, ks = q.stride(), keys.stride()
-    assert kd == d and _alike(keys, values)
-    a = FoundArgs(_HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt), qs[0], qs[1], _rows(keys, i, dt), _rows(values, i, dt), ks[0], ks[1], n,
-                  _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else None,
-                  _real(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
+    o, lse, i, a = _found(q, keys, values, ids, scale, part, out, None)
     _run(_lib.jx_found_attention, i, C.byref(a))
+    return o, lse
+
+
+def found_attention8(q, keys, values, k_scale, v_scale, ids, scale, block, part=None, out=None):
+    """jx_found_attention8: as found_attention, over rows of torch.float8_e4m3fn; scales [ceil(rows / block)][kv_heads] of
+    torch.float8_e8m0fnu, row i in block i // block."""
+    o, lse, i, a = _found(q, keys, values, ids, scale, part, out, _E4M3)
+    n, kv, _ = keys.shape
+    assert block >= 1, block
+    blocks = -(-n // block)
+    sc = KvScales(_real(k_scale, i, _E8M0, blocks, kv), _real(v_scale, i, _E8M0, blocks, kv), block)
+    _run(_lib.jx_found_attention8, i, C.byref(a), C.byref(sc))
     return o, lse
 
 

@@ -1,0 +1,696 @@
+"""Attention over keys and values of 8 bits against its definitions in 64 bits: the store into blocks with a common scale, paged
+attention over all that a table, a window and a chunk can leave of the keys, found rows and their join.  Bounds: attention8_plain."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2601_07048_amd import jx  # noqa: E402
+
+import attention8_plain as plain8  # noqa: E402
+import attention_plain as plain  # noqa: E402
+from test_gpu_attention import BF, F16, TYPES, found_case, i32, normal, rope_plain  # noqa: E402
+
+CODE, SCALE = plain8.CODE, plain8.SCALE
+NAN_CODE, NAN_SCALE = 0x7F, 255
+
+
+def cache8(pages, page, kv, dim, block, seed, layout="thd"):
+    """Codes and scales of normal values whose size differs from block to block, on the GPU."""
+    g = torch.Generator().manual_seed(seed)
+    size = torch.exp(0.7 * torch.randn((pages * page // block, 1, kv, 1), generator=g))
+    x = torch.randn((pages * page // block, block, kv, dim), generator=g) * size
+    codes, scale = plain8.quantised(x.view(-1, kv, dim), block)
+    codes = codes.view(pages, page, kv, dim)
+    if layout == "htd":
+        codes = codes.view(torch.uint8).transpose(1, 2).contiguous().view(CODE).cuda().transpose(1, 2)
+    return codes.cuda(), scale.view(pages, page // block, kv).cuda()
+
+
+class Paged8:
+    """Requests with lengths `lens` (new tokens included) of which the last `new` ask; pages scattered; codes and scales that no
+    request owns are not numbers."""
+
+    def __init__(self, dtype, heads, kv, dim, page, block, lens, new, seed=0, layout="thd", spare=3, width=None, pad=0):
+        rng = np.random.default_rng(seed)
+        held = [-(-max(n, 0) // page) for n in lens]
+        pages = sum(held) + spare
+        order = rng.permutation(pages)
+        width = width or max(1, max(held) + 1)
+        table = np.full((len(lens), width), -1, np.int32)
+        at = 0
+        for r, n in enumerate(held):
+            m = min(n, width)
+            table[r, :m] = order[at:at + m]
+            at += n
+        (self.k, self.k_scale), (self.v, self.v_scale) = (cache8(pages, page, kv, dim, block, seed + i, layout) for i in (1, 2))
+        free = torch.ones((pages, page), dtype=torch.bool)
+        for r, n in enumerate(lens):
+            for p in range(min(held[r], width)):
+                free[int(table[r, p]), :min(page, n - p * page)] = False
+        none = free.view(pages, page // block, block).all(2).cuda()
+        free = free.cuda()
+        for codes, scale in ((self.k, self.k_scale), (self.v, self.v_scale)):
+            codes.view(torch.uint8)[free] = NAN_CODE
+            scale.view(torch.uint8)[none] = NAN_SCALE
+        self.table, self.page, self.block = i32(table), page, block
+        self.q_start = i32(np.cumsum([0] + list(new)).tolist())
+        self.kv_len = i32(list(lens))
+        self.q = normal((sum(new) + pad, heads, dim), dtype, seed + 3, 1.5)
+        self.scale = dim ** -0.5
+
+    def place(self, r, position):
+        return int(self.table[r, position // self.page]), position % self.page
+
+    def run(self, window=0, **kw):
+        got = jx.paged_attention8(self.q, self.k, self.v, self.k_scale, self.v_scale, self.table, self.q_start, self.kv_len, self.scale,
+                                  window=window, **kw)
+        torch.cuda.synchronize()
+        return got
+
+    def want(self, window=0, rows=None):
+        return plain.paged(self.q, plain8.stands_for(self.k, self.k_scale), plain8.stands_for(self.v, self.v_scale), self.table, self.q_start,
+                           self.kv_len, self.scale, window, rows)
+
+    def check(self, window=0, rows=None, what=""):
+        got = self.run(window)
+        assert torch.isfinite(got[0]).all(), what
+        plain.check(got, self.want(window, rows), what)
+        return got
+
+
+# ---- the store ---------------------------------------------------------------------------------------------------------
+
+def store_case(dtype, spans, heads, kv, dim, rot, page, block, pairs, normed, seed, layout="thd", size=3.0):
+    """A step of requests with (first position, tokens); pages in a random order."""
+    rng = np.random.default_rng(seed)
+    held = [(a + n - 1) // page - a // page + 1 if n else 0 for a, n in spans]
+    pages = sum(held) + 2
+    order, at, pos, slot = rng.permutation(pages), 0, [], []
+    for (a, n), h in zip(spans, held):
+        for p in range(a, a + n):
+            pos.append(p)
+            slot.append(int(order[at + p // page - a // page]) * page + p % page)
+        at += h
+    t = len(pos)
+    n_pos = max(pos) + 1
+    g = torch.Generator().manual_seed(seed)
+    (kc, ks), (vc, vs) = (cache8(pages, page, kv, dim, block, seed + i, layout) for i in (1, 2))
+    angle = torch.rand((n_pos, rot // 2), generator=g) * 6.3
+    return dict(q=normal((t, heads, dim), dtype, seed, 3.0), k=normal((t, kv, dim), dtype, seed + 5, size), v=normal((t, kv, dim), dtype, seed + 6, size),
+                k_cache=kc, v_cache=vc, k_scale=ks, v_scale=vs, pos=pos, slot=slot, n_pos=n_pos, block=block, page=page, pairs=pairs,
+                cos=angle.cos().cuda() if rot else None, sin=angle.sin().cuda() if rot else None, eps=1e-5,
+                wq=normal((dim,), dtype, 6) if normed else None, wk=normal((dim,), dtype, 7) if normed else None)
+
+
+def flat(codes, scale):
+    """[slots][kv][dim] and [blocks][kv] on the CPU."""
+    return codes.view(torch.uint8).cpu().contiguous().flatten(0, 1).view(CODE).clone(), scale.view(torch.uint8).cpu().flatten(0, 1).clone()
+
+
+def run_store(c, **kw):
+    return jx.qk_norm_rope8(c["q"], c["k"], c["v"], c["k_cache"], c["v_cache"], c["k_scale"], c["v_scale"], i32(c["pos"]),
+                            torch.tensor(c["slot"], dtype=torch.int64, device="cuda"), c["cos"], c["sin"], c["wq"], c["wk"], eps=c["eps"],
+                            interleaved=c["pairs"], **kw)
+
+
+def check_store(c, what=""):
+    before = flat(c["k_cache"], c["k_scale"]), flat(c["v_cache"], c["v_scale"])
+    got = run_store(c)
+    torch.cuda.synchronize()
+    dtype = c["q"].dtype
+    pos = torch.tensor(c["pos"])
+    here = (pos >= 0) & (pos < c["n_pos"])
+    at = pos.clamp(0, c["n_pos"] - 1)
+    turn = (c["cos"].cpu()[at], c["sin"].cpu()[at]) if c["cos"] is not None else (None, None)
+    n_slots = c["k_cache"].shape[0] * c["page"]
+    found = plain8.runs(c["pos"], c["slot"], c["n_pos"], n_slots, c["block"])
+    y, d = rope_plain(c["q"].cpu(), c["wq"].cpu() if c["wq"] is not None else None, c["eps"], *turn, c["pairs"])
+    u, tiny = plain.UNIT[dtype], plain.TINY[dtype]
+    assert bool(((got.cpu().double() - y).abs()[here] <= (d + u * y.abs())[here] * 1.01 + tiny / 2).all()), what
+    assert not got.cpu()[~here].any(), what
+    plain_k = c["wk"] is None and c["cos"] is None
+    y, d = rope_plain(c["k"].cpu(), c["wk"].cpu() if c["wk"] is not None else None, c["eps"], *turn, c["pairs"])
+    plain8.check_store(y, torch.zeros_like(d) if plain_k else d, c["slot"], found, before[0], flat(c["k_cache"], c["k_scale"]), c["block"], dtype,
+                       plain_k, (what, "keys"))
+    y = c["v"].cpu().double()
+    plain8.check_store(y, torch.zeros_like(y), c["slot"], found, before[1], flat(c["v_cache"], c["v_scale"]), c["block"], dtype, True, (what, "values"))
+    return got
+
+
+SHAPES = [(8, 2, 128, 128, 16, 16), (6, 3, 64, 32, 64, 64), (4, 1, 96, 96, 32, 8), (2, 2, 256, 64, 64, 64), (1, 1, 16, 0, 1, 1), (3, 1, 192, 16, 16, 4),
+          (5, 5, 80, 80, 4, 2), (40, 8, 128, 64, 128, 32), (2, 1, 256, 128, 16, 1), (4, 2, 64, 0, 128, 64)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,dim,rot,page,block", SHAPES)
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("normed", [False, True])
+def test_store(dtype, heads, kv, dim, rot, page, block, pairs, normed):
+    """Single tokens at the first, a middle and the last place of a block, chunks inside a block, over its end and over many."""
+    spans = [(0, 1), (1, 1), (page * 3 - 1, 1), (block // 2, 1), (7, 5), (page - 2 if page > 1 else 0, 3), (block, block), (3, 2 * page + block + 1),
+             (0, page), (5 * page + 1, 40)]
+    check_store(store_case(dtype, spans, heads, kv, dim, rot, page, block, pairs, normed, seed=dim + page))
+
+
+@pytest.mark.parametrize("heads,kv,dim,rot,page,block", SHAPES)
+@pytest.mark.parametrize("size", [1e-3, 1.0, 30.0])
+def test_store_where_scales_grow_or_stay(heads, kv, dim, rot, page, block, size):
+    spans = [(r % (4 * page), 1 + r % 3) for r in range(70)]
+    check_store(store_case(BF, spans, heads, kv, dim, rot, page, block, False, False, seed=3, size=size))
+
+
+def test_store_of_many_tokens():
+    """So many that a workgroup takes several tokens."""
+    c = store_case(BF, [(5, 700), (16, 1), (33, 1), (1, 900)] + [(r, 1) for r in range(300)], 8, 8, 64, 64, 16, 16, False, True, seed=1)
+    check_store(c)
+    c = store_case(F16, [(5, 700), (64, 1), (33, 1), (1, 64)] + [(r, 1) for r in range(600)], 16, 16, 64, 32, 64, 64, True, True, seed=2, layout="htd")
+    check_store(c)
+
+
+def test_rows_that_are_not_stored():
+    c = store_case(BF, [(0, 3), (4, 2), (9, 30), (7, 1), (2, 1)], 4, 2, 64, 64, 16, 8, False, True, seed=5)
+    n_slots = c["k_cache"].shape[0] * 16
+    c["n_pos"] -= 3  # the last positions of the long request, and then some
+    c["cos"], c["sin"] = c["cos"][:c["n_pos"]].contiguous(), c["sin"][:c["n_pos"]].contiguous()
+    c["pos"][2], c["slot"][4] = -1, -1
+    c["slot"][35], c["slot"][36] = n_slots, -5
+    check_store(c)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+def test_store_of_extreme_values(dtype):
+    """The type's largest and smallest, infinities and what is not a number, blocks of zeros."""
+    c = store_case(dtype, [(0, 4), (8, 4), (16, 4), (24, 4), (36, 4), (44, 1), (48, 8)], 1, 1, 32, 0, 8, 4, False, False, seed=7)
+    most = torch.finfo(dtype).max
+    for name in ("k", "v"):
+        x = c[name]
+        x[0] = most
+        x[1, 0, 0], x[2, 0, 1], x[3, 0, 2] = -most, math.nan, math.inf
+        x[4:8] = torch.finfo(dtype).smallest_normal * 2.0 ** -5  # subnormal
+        x[8:12] = 0
+        x[9, 0, 3] = -math.inf
+        x[12:16] = math.nan
+        x[16, 0, 5] = 1e-4
+        x[17, 0, :16] = -0.0
+        x[20, 0, 3] = 15 * 2.0 ** 12
+        x[21:25] *= 2.0 ** -100 if dtype is BF else 2.0 ** -14
+    check_store(c)
+
+
+def test_tokens_one_by_one_and_at_once():
+    """The same tokens in chunks of different lengths: values that the codes stand for agree to their roundings, and a scale is that of
+    the largest so far."""
+    t, kv, dim, page, block = 96, 2, 64, 32, 16
+    k, v, q = normal((t, kv, dim), BF, 1), normal((t, kv, dim), BF, 2), normal((t, 4, dim), BF, 3)
+    v *= torch.exp(torch.randn((t, kv, 1), generator=torch.Generator().manual_seed(4))).cuda().to(BF)
+    end = []
+    for step in (1, 3, 16, 96):
+        kc, vc = (torch.full((3, page, kv, dim), NAN_CODE, dtype=torch.uint8, device="cuda").view(CODE) for _ in range(2))
+        ks, vs = (torch.full((3, page // block, kv), NAN_SCALE, dtype=torch.uint8, device="cuda").view(SCALE) for _ in range(2))
+        for a in range(0, t, step):
+            b = slice(a, min(a + step, t))
+            at = torch.arange(a, b.stop, device="cuda")
+            jx.qk_norm_rope8(q[b], k[b], v[b], kc, vc, ks, vs, at.int(), at)
+        end.append((plain8.stands_for(kc, ks).flatten(0, 1), plain8.stands_for(vc, vs).flatten(0, 1), ks.view(torch.uint8).cpu(), vs.view(torch.uint8).cpu()))
+    for e in end:
+        assert torch.equal(e[2], end[-1][2]) and torch.equal(e[3], end[-1][3])
+        for x, y, scale in ((e[0], k, e[2]), (e[1], v, e[3])):
+            power = torch.exp2(scale.flatten(0, 1).double() - 127).repeat_interleave(block, 0)[..., None].expand(-1, -1, dim)
+            y = y.cpu().double()
+            # rounded once; numbers that came under 2^-6 scales as a scale grew, once more for each of the at most 4 times it did
+            half = plain8.half_step(y.abs(), power)
+            assert bool(((x - y).abs() <= half + torch.where(y.abs() < power * 2.0 ** -5, 2.0 ** -9 * power, torch.zeros_like(y))).all())
+
+
+def test_store_in_place_of_queries_and_strides():
+    c = store_case(BF, [(3, 20), (0, 7), (15, 1)], 8, 2, 64, 64, 16, 8, False, True, seed=11)
+    d = {x: (y.clone() if torch.is_tensor(y) else y) for x, y in c.items()}
+    want = run_store(c)
+    pages = d["k_cache"].shape[0]
+    both = torch.full((pages, 16, 3, 2, 80), 7, dtype=torch.uint8, device="cuda")
+    both[:, :, 1:, 0, :64], both[:, :, 1:, 1, :64] = d["k_cache"].view(torch.uint8), d["v_cache"].view(torch.uint8)
+    was = both.clone()
+    d["k_cache"], d["v_cache"] = both[:, :, 1:, 0, :64].view(CODE), both[:, :, 1:, 1, :64].view(CODE)
+    fused = torch.full((28, 13, 72), math.nan, dtype=BF, device="cuda")
+    fused[:, 8:10, :64], fused[:, 10:12, :64] = d["k"], d["v"]
+    d["k"], d["v"] = fused[:, 8:10, :64], fused[:, 10:12, :64]
+    q = d["q"]
+    assert run_store(d, out=q) is q and torch.equal(q, want)
+    for x in ("k", "v"):
+        assert torch.equal(d[x + "_cache"].view(torch.uint8), c[x + "_cache"].view(torch.uint8))
+        assert torch.equal(d[x + "_scale"].view(torch.uint8), c[x + "_scale"].view(torch.uint8))
+    was[:, :, 1:, :, :64] = both[:, :, 1:, :, :64]
+    assert torch.equal(was, both)
+
+
+def test_store_offsets_beyond_32_bits():
+    c = store_case(BF, [(3, 5), (40, 1), (70, 30)], 4, 2, 64, 64, 64, 16, False, True, seed=2)
+    d = {x: (y.clone() if torch.is_tensor(y) else y) for x, y in c.items()}
+    want = run_store(c)
+    pages, stride = d["k_cache"].shape[0], 2 ** 31 + 2 ** 20
+    pool = torch.empty((pages - 1) * stride + 2 * 64 * 2 * 64, dtype=torch.uint8, device="cuda").view(CODE)
+    for i, x in enumerate(("k_cache", "v_cache")):
+        far = pool.as_strided((pages, 64, 2, 64), (stride, 128, 64, 1), i * 64 * 128)
+        far.view(torch.uint8).copy_(d[x].view(torch.uint8))
+        d[x] = far
+    assert torch.equal(run_store(d), want)
+    for x in ("k", "v"):
+        assert torch.equal(d[x + "_cache"].view(torch.uint8), c[x + "_cache"].view(torch.uint8))
+        assert torch.equal(d[x + "_scale"].view(torch.uint8), c[x + "_scale"].view(torch.uint8))
+
+
+def test_no_tokens():
+    c = store_case(BF, [(0, 1)], 4, 2, 64, 64, 16, 8, False, True, seed=11)
+    before = flat(c["k_cache"], c["k_scale"])
+    for x in "qkv":
+        c[x] = c[x][:0]
+    c["pos"], c["slot"] = [], []
+    assert run_store(c).shape[0] == 0
+    after = flat(c["k_cache"], c["k_scale"])
+    assert torch.equal(before[0].view(torch.uint8), after[0].view(torch.uint8)) and torch.equal(before[1], after[1])
+
+
+# ---- paged attention ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,dim,page,block", [(8, 1, 128, 16, 16), (6, 2, 64, 8, 1), (4, 4, 96, 32, 4), (5, 1, 256, 64, 64), (3, 3, 16, 1, 1),
+                                                     (16, 1, 80, 4, 2), (40, 2, 128, 128, 32), (2, 1, 192, 16, 8), (33, 1, 64, 2, 2), (8, 2, 128, 16, 1)])
+def test_one_token_per_request(dtype, heads, kv, dim, page, block):
+    lens = [1, 2, 15, 16, 17, 63, 64, 65, 127, 130, 257]
+    Paged8(dtype, heads, kv, dim, page, block, lens, [1] * len(lens), seed=dim + heads).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,dim,page,block", [(8, 2, 128, 16, 8), (4, 4, 64, 64, 16), (7, 1, 128, 8, 1), (4, 2, 256, 32, 32), (2, 2, 48, 16, 4), (12, 2, 96, 1, 1)])
+@pytest.mark.parametrize("window", [0, 1, 5, 64, 1000])
+def test_chunks_of_unlike_lengths(dtype, heads, kv, dim, page, block, window):
+    lens, new = [70, 1, 33, 129, 5, 64, 200], [70, 1, 17, 3, 0, 64, 65]
+    Paged8(dtype, heads, kv, dim, page, block, lens, new, seed=window).check(window)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("new", [[1], [2], [16], [17], [100], [300]], ids=lambda n: str(n[0]))
+def test_one_request(dtype, new):
+    Paged8(dtype, 4, 1, 128, 16, 16, [333], new, seed=new[0]).check()
+
+
+def test_no_keys_no_requests_and_rows_of_none():
+    p = Paged8(BF, 4, 2, 64, 16, 8, [0, 3, 40, 0], [2, 5, 0, 0], seed=5, pad=3)
+    got = p.check()
+    assert (got[1][:4] == -math.inf).all() and (got[1][4:7] > -math.inf).all() and (got[1][7:] == -math.inf).all()
+    p.q_start += 2
+    p.check()
+    p.q_start = i32([0])
+    p.kv_len, p.table = i32([]), p.table[:0].contiguous()
+    out, lse = p.run()
+    assert not out.any() and (lse == -math.inf).all()
+    p.q = p.q[:0]
+    assert p.run()[0].shape[0] == 0
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_pages_that_the_table_does_not_name(new):
+    p = Paged8(F16, 8, 2, 128, 16, 16, [150, 150, 150, 150], [new] * 4, seed=9)
+    pages = p.k.shape[0]
+    p.table[0, 2] = -1
+    p.table[1, :5] = -1
+    p.table[2, 9] = pages        # names no page
+    p.table[2, 3] = 2 ** 31 - 1
+    p.table[3] = -7              # nothing is left
+    got = p.check()
+    assert (got[1][3 * new:] == -math.inf).all()
+    p.check(window=40)
+    p.table = p.table[:, :6].contiguous()  # a table narrower than the lengths
+    p.check()
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 128), (2, 2, 64), (4, 1, 256)])
+@pytest.mark.parametrize("block", [1, 16])
+@pytest.mark.parametrize("what", ["code", "scale"])
+def test_what_a_row_does_not_see_has_no_part_in_it(heads, kv, dim, block, what):
+    """A key or value that is not a number, at every place of a chunk in turn, or a block whose scale is none: the rows before it, and
+    those that their window has taken past it, are what they are without it."""
+    for at in (10, 11, 40, 63, 64, 88, 89):
+        p = Paged8(BF, heads, kv, dim, 16, block, [90], [80], seed=at)
+        first, last = (at, at) if what == "code" else (at // block * block, at // block * block + block - 1)
+        row, behind = max(first - 10, 0), last - 10 + 7  # the first row that sees it, the first whose window has left it
+        before = list(range(max(0, row - 3), row))
+        past = [r for r in range(behind, min(80, behind + 3))]
+        want, want_window = p.want(rows=before), p.want(window=7, rows=before + past)
+        page, place = p.place(0, at)
+        for codes, scale in ((p.k, p.k_scale), (p.v, p.v_scale)):
+            bad = codes.view(torch.uint8)[page, place] if what == "code" else scale.view(torch.uint8)[page, place // block]
+            keep = bad.clone()
+            bad.fill_(NAN_CODE if what == "code" else NAN_SCALE)
+            got = p.run()
+            assert torch.isfinite(got[0][:row]).all() and torch.isfinite(got[1][:row]).all()
+            plain.check(got, want, (at, "chunk"))
+            assert not torch.isfinite(got[0][row:]).any()
+            if codes is p.k:
+                assert torch.isnan(got[1][row:]).all()
+            got = p.run(window=7)
+            assert torch.isfinite(got[0][:row]).all() and torch.isfinite(got[0][behind:]).all()
+            plain.check(got, want_window, (at, "window"))
+            bad.copy_(keep)
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (8, 2), (40, 2)])
+@pytest.mark.parametrize("dim", [64, 128, 208])
+def test_single_tokens_do_not_see_what_has_left_their_window(heads, kv, dim):
+    """Before the window, behind the length and in pages that the table does not name there may be anything."""
+    lens = (150, 75, 33, 16)
+    p = Paged8(BF, heads, kv, dim, 16, 4, lens, [1] * 4, seed=dim)
+    want = p.want(window=20)
+    for r, n in enumerate(lens):
+        for j in range(n - 20):
+            page, place = p.place(r, j)
+            p.k.view(torch.uint8)[page, place] = NAN_CODE
+            p.v.view(torch.uint8)[page, place] = 0xFF
+            if j // 4 * 4 + 4 <= n - 20 and j % 3:
+                p.v_scale.view(torch.uint8)[page, place // 4] = NAN_SCALE
+                p.k_scale.view(torch.uint8)[page, place // 4] = NAN_SCALE
+    plain.check(p.run(window=20), want)
+
+
+@pytest.mark.parametrize("lens,new", [([50], [20]), ([50, 7], [1, 1])])
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+def test_values_that_are_not_numbers_reach_the_rows_that_see_them(dtype, lens, new):
+    p = Paged8(dtype, 4, 2, 64, 16, 8, lens, new, seed=4)
+    page, place = p.place(0, 40)
+    p.v.view(torch.uint8)[page, place, 1, 3] = NAN_CODE  # key head 1
+    got = p.run()
+    row = 10 if new[0] == 20 else 0
+    seen = got[0][row:new[0]]
+    assert seen[:, 2:, 3].isnan().all() and torch.isfinite(got[0][:row]).all() and torch.isfinite(got[0][:, :2]).all()
+    assert torch.isfinite(seen[:, 2:, :3]).all() and torch.isfinite(seen[:, 2:, 4:]).all() and torch.isfinite(got[0][new[0]:]).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+def test_scales_of_every_size(dtype, new):
+    """Blocks whose values are very large or very small beside one another, up to the ends of the type's numbers."""
+    p = Paged8(dtype, 8, 2, 128, 16, 8, [300], [new], seed=3)
+    rows = sorted({0, new // 2, new - 1})
+    low, high = (40, 127 + 24) if dtype is BF else (127 - 15, 127 + 7)  # codes of up to 448 times 2^7: 57,344
+    g = torch.Generator().manual_seed(1)
+    for scale, codes in ((p.v_scale, p.v), (p.k_scale, p.k)):
+        codes.view(torch.uint8)[(codes.float().abs() > 448) | codes.float().isnan()] = 0
+        byte = torch.randint(low, high, scale.shape, generator=g).to(torch.uint8).cuda()
+        keep = scale.view(torch.uint8).clone()
+        scale.view(torch.uint8).copy_(byte if scale is p.v_scale else byte.clamp(127 - 20, 127))
+        p.check(rows=rows)
+        if scale is p.v_scale:
+            scale.view(torch.uint8).copy_(keep)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+def test_scores_of_every_size(dtype):
+    """The largest score decides, nothing overflows; and equal scores, where the mean is the result; a negative scale."""
+    p = Paged8(dtype, 8, 2, 128, 16, 16, [777, 400], [1, 130], seed=3)
+    p.q *= 100
+    p.scale = 2.0
+    p.check(rows=[0, 1, 50, 130])
+    p.q.zero_()
+    p.check(rows=[0, 1, 130])
+    p.scale = -0.1
+    p.q = normal(p.q.shape, dtype, 1)
+    p.check(rows=[0, 1, 130])
+    p.scale = 0.0
+    p.check(rows=[0, 1, 130])
+
+
+@pytest.mark.parametrize("layout", ["thd", "htd"])
+def test_strides(layout):
+    p = Paged8(BF, 8, 2, 64, 16, 8, [100, 37], [1, 20], seed=8, layout=layout)
+    want = p.run()
+    p.check()
+    fused = torch.full((21, 12, 80), math.nan, dtype=BF, device="cuda")
+    fused[:, 2:10, :64] = p.q
+    q = p.q
+    p.q = fused[:, 2:10, :64]
+    assert torch.equal(p.run()[0], want[0])
+    p.q = q
+    pages = p.k.shape[0]  # keys and values of a page together, one block for both
+    both = torch.full((pages, 2, 16, 3, 80), NAN_CODE, dtype=torch.uint8, device="cuda")
+    both[:, 0, :, 1:, :64], both[:, 1, :, 1:, :64] = p.k.view(torch.uint8), p.v.view(torch.uint8)
+    p.k, p.v = both[:, 0, :, 1:, :64].view(CODE), both[:, 1, :, 1:, :64].view(CODE)
+    assert torch.equal(p.run()[0], want[0])
+    p.check()
+    assert torch.equal(p.run(out=(torch.empty_like(want[0]), None))[0], want[0])
+
+
+def test_offsets_beyond_32_bits():
+    stride = 2 ** 31 + 2 ** 20  # codes between pages
+    pool = torch.empty(2 * stride + 2 * 64 * 2 * 64, dtype=torch.uint8, device="cuda")
+    far = [pool.as_strided((3, 64, 2, 64), (stride, 128, 64, 1), i * 64 * 128) for i in (0, 1)]
+    for new in (1, 30):
+        p = Paged8(BF, 4, 2, 64, 64, 16, [170], [new], seed=2, spare=0)
+        want = p.run()
+        for x, y in zip(far, (p.k, p.v)):
+            x.copy_(y.view(torch.uint8))
+        p.k, p.v = (x.view(CODE) for x in far)
+        assert torch.equal(p.run()[0], want[0])
+        p.check(rows=[0])
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("lens", [[20011], [5, 9000, 1, 700, 4096], [2000] * 40], ids=["one", "unlike", "many"])
+def test_long_caches(lens, new):
+    p = Paged8(BF, 16, 2, 128, 16, 16, lens, [min(new, n) for n in lens], seed=len(lens))
+    rows = sorted({0, p.q.shape[0] // 2, p.q.shape[0] - 1})
+    p.check(rows=rows)
+    p.check(window=777, rows=rows)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 80, 96, 128, 192, 256])
+@pytest.mark.parametrize("window", [0, 30])
+def test_a_few_tokens_of_short_requests(dtype, dim, window):
+    rng = np.random.default_rng(dim)
+    lens = rng.integers(1, 140, 24).tolist()
+    new = [min(int(rng.integers(1, 9)), n) for n in lens]
+    Paged8(dtype, 8, 2, dim, 16, 4, lens, new, seed=dim).check(window, rows=list(range(0, sum(new), 3)))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("bad", [False, True])
+def test_short_requests_in_narrow_and_wide_tables(dtype, dim, bad):
+    """How much a table has room for decides who takes the keys, and nothing else; the same for a window that is short."""
+    lens = [0, 1, 3, 64, 65, 100, 127, 128]
+    p = Paged8(dtype, 8, 2, dim, 16, 16, lens, [1, 1, 1, 2, 1, 1, 2, 1], seed=dim, width=8)
+    if bad:  # the first key of the request of 64: its rows 3 and 4 see it, unless the window is short
+        p.v.view(torch.uint8)[int(p.table[3, 0]), 0, 1, 3] = NAN_CODE
+    rows = [t for t in range(10) if not bad or t not in (3, 4)]
+    narrow, short = p.run(), p.run(window=40)
+    p.table = torch.cat([p.table, torch.full((len(lens), 200), -1, dtype=torch.int32, device="cuda")], 1)
+    for what, got, window in (("narrow", narrow, 0), ("wide", p.run(), 0), ("narrow, window", short, 40), ("wide, window", p.run(window=40), 40)):
+        plain.check(got, p.want(window, None if window else rows), what)
+        for t in range(10):
+            if t not in rows and not window:
+                o = got[0][t].isfinite()
+                assert not o[4:, 3].any() and o[:4].all() and o[4:, :3].all() and o[4:, 4:].all(), what
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("lens,new", [([700], [600]), ([1500, 1100], [1100, 1100]), ([90, 3000], [1, 2100])], ids=["one", "two", "unlike"])
+def test_long_chunks(dim, lens, new):
+    p = Paged8(BF, 8, 2, dim, 32, 16, lens, new, seed=dim)
+    rows = sorted({0, 1, 63, 64, 127, 128, 255, 256, sum(new) // 2, sum(new) - 1})
+    p.check(rows=rows)
+    p.check(window=100, rows=rows)
+
+
+def test_more_tiles_than_are_shared_out():
+    rng = np.random.default_rng(3)
+    lens = rng.integers(6, 80, 1100).tolist()
+    p = Paged8(BF, 8, 1, 64, 4, 2, lens, [6] * 1100, seed=2)
+    p.check(rows=list(range(0, 6600, 371)))
+    p.check(window=9, rows=list(range(5, 6600, 371)))
+
+
+def test_many_requests():
+    rng = np.random.default_rng(0)
+    lens = rng.integers(0, 90, 1500).tolist()
+    new = [int(rng.integers(0, 3)) for _ in lens]
+    p = Paged8(F16, 4, 1, 64, 16, 16, lens, new, seed=1)
+    p.check(rows=list(range(0, sum(new), 37)))
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    p = Paged8(BF, 8, 1, 128, 16, 16, [3000, 17, 900], [1, 1, 33], seed=6)
+    want = p.run()
+    for _ in range(3):
+        got = p.run()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = jx.paged_attention8(p.q, p.k, p.v, p.k_scale, p.v_scale, p.table, p.q_start, p.kv_len, p.scale)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# ---- attention over found rows -----------------------------------------------------------------------------------------
+
+def found8_case(dtype, t, heads, kv, dim, k, rows, block, seed, holes=0.2):
+    q, _, _, ids = found_case(dtype, t, heads, kv, dim, k, rows, seed, holes)
+    blocks = -(-rows // block)
+    (keys, ks), (values, vs) = (cache8(blocks, block, kv, dim, block, seed + i) for i in (2, 3))
+    return q, keys.flatten(0, 1)[:rows], values.flatten(0, 1)[:rows], ks.flatten(0, 1), vs.flatten(0, 1), ids
+
+
+def found8_want(q, keys, values, ks, vs, ids, scale, block, part=None):
+    return plain.found(q, plain8.rows_stand_for(keys, ks, block), plain8.rows_stand_for(values, vs, block), ids, scale, part)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("t,heads,kv,dim,k,block", [(1, 1, 1, 128, 1, 1), (3, 8, 2, 128, 10, 16), (5, 6, 3, 64, 33, 64), (2, 4, 1, 256, 100, 8),
+                                                    (2, 2, 2, 80, 7, 4), (1, 4, 4, 16, 130, 2), (2, 3, 1, 192, 64, 32), (7, 2, 1, 128, 513, 1)])
+@pytest.mark.parametrize("joined", [False, True])
+def test_found_rows(dtype, t, heads, kv, dim, k, block, joined):
+    q, keys, values, ks, vs, ids = found8_case(dtype, t, heads, kv, dim, k, 50, block, seed=k)
+    ids[0, 0, 0] = 50              # outside
+    ids[-1, -1] = -1               # nothing found
+    ids[0, -1, :2] = 3             # the same row twice
+    part = None
+    if joined:
+        part = normal((t, heads, dim), dtype, 9), torch.randn((t, heads), generator=torch.Generator().manual_seed(1)).cuda() * 3
+        part[1][0, 0] = -math.inf  # a part of no keys, whatever its rows hold
+        part[0][0, 0] = math.nan
+    scale = dim ** -0.5
+    got = jx.found_attention8(q, keys, values, ks, vs, ids, scale, block, part=part)
+    torch.cuda.synchronize()
+    plain.check(got, found8_want(q, keys, values, ks, vs, ids, scale, block, part))
+    if joined:  # in place
+        same = jx.found_attention8(q, keys, values, ks, vs, ids, scale, block, part=part, out=part)
+        assert torch.equal(same[0], got[0]) and torch.equal(same[1], got[1])
+
+
+def test_found_rows_of_no_list_and_rows_that_are_passed_over():
+    q, keys, values, ks, vs, ids = found8_case(BF, 3, 4, 2, 64, 8, 20, 4, seed=3, holes=0.0)
+    out, lse = jx.found_attention8(q, keys, values, ks, vs, ids[:, :, :0].contiguous(), 0.1, 4)
+    assert not out.any() and (lse == -math.inf).all()
+    out, lse = jx.found_attention8(q, keys[:0], values[:0], ks[:0], vs[:0], ids, 0.1, 4)
+    assert not out.any() and (lse == -math.inf).all()
+    ids[(ids >= 4) & (ids < 8)] = 8
+    ids[:, :, 3] = -1
+    for x in (keys, values):
+        x.view(torch.uint8)[7] = NAN_CODE
+    for x in (ks, vs):
+        x.view(torch.uint8)[1] = NAN_SCALE
+    clean = jx.found_attention8(q, keys, values, ks, vs, ids, 0.1, 4)
+    assert torch.isfinite(clean[0]).all()
+    plain.check(clean, found8_want(q, keys, values, ks, vs, ids, 0.1, 4))
+    # strided rows: only some of a larger table, keys and values of a row together
+    both = torch.full((20, 2, 3, 80), NAN_CODE, dtype=torch.uint8, device="cuda")
+    both[:, 0, :2, :64], both[:, 1, :2, :64] = keys.view(torch.uint8), values.view(torch.uint8)
+    got = jx.found_attention8(q, both[:, 0, :2, :64].view(CODE), both[:, 1, :2, :64].view(CODE), ks, vs, ids, 0.1, 4)
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+    # what is not a number and is listed reaches the result
+    ids[0, 0, 0] = 5  # its scale is none
+    got = jx.found_attention8(q, keys, values, ks, vs, ids, 0.1, 4)
+    assert got[0][0, 0].isnan().all() and torch.equal(got[0][1:], clean[0][1:]) and torch.equal(got[0][0, 1:], clean[0][0, 1:])
+
+
+def test_found_rows_far_apart_and_scales_of_every_size():
+    stride = 2 ** 31 + 2 ** 20
+    pool = torch.empty(3 * stride + 4 * 2 * 64, dtype=torch.uint8, device="cuda")
+    q, keys, values, ks, vs, ids = found8_case(F16, 2, 4, 2, 64, 6, 4, 1, seed=5)
+    far = [pool.as_strided((4, 2, 64), (stride, 64, 1), i * 128) for i in (0, 1)]
+    for x, y in zip(far, (keys, values)):
+        x.copy_(y.view(torch.uint8))
+    want = jx.found_attention8(q, keys, values, ks, vs, ids, 0.125, 1)
+    got = jx.found_attention8(q, far[0].view(CODE), far[1].view(CODE), ks, vs, ids, 0.125, 1)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    vs.view(torch.uint8).copy_(torch.tensor([[0, 100], [1, 127], [90, 133], [127, 120]], dtype=torch.uint8))
+    ks.view(torch.uint8).copy_(torch.tensor([[0, 120], [1, 127], [100, 110], [127, 1]], dtype=torch.uint8))
+    got = jx.found_attention8(q, keys, values, ks, vs, ids, 0.125, 1)
+    plain.check(got, found8_want(q, keys, values, ks, vs, ids, 0.125, 1))
+
+
+def test_parts_join_to_the_whole():
+    """Paged attention over one half of the keys and found attention over the other = attention over all; whole blocks of the cache
+    are the rows."""
+    p = Paged8(F16, 8, 2, 128, 16, 8, [64], [4], seed=11)
+    whole = p.want()
+    pages = p.table[0, :4].long()
+    rows = [x.view(torch.uint8)[pages].flatten(0, 1)[:32].contiguous().view(x.dtype) for x in (p.k, p.v)]
+    scales = [x.view(torch.uint8)[pages].flatten(0, 1)[:4].contiguous().view(x.dtype) for x in (p.k_scale, p.v_scale)]
+    most = plain8.stands_for(p.v, p.v_scale)[pages.cpu()].abs().max()
+    p.table[0, :2] = -1
+    part = p.run()
+    ids = torch.arange(32, device="cuda", dtype=torch.int32).expand(4, 8, 32).contiguous()
+    got = jx.found_attention8(p.q, *rows, *scales, ids, p.scale, 8, part=part)
+    out = got[0].cpu().double()
+    for (t, h), (o, l, bo, bl) in whole.items():
+        # the part was rounded to the element type once more
+        assert bool(((out[t, h] - o).abs() <= bo + 2 * plain.UNIT[F16] * most).all())
+        assert abs(float(got[1][t, h]) - l) <= 4 * bl
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------
+
+def test_steps_of_a_served_request_in_a_graph():
+    """Plan, norm, rotation and store in 8 bits, attention over the cache, search results joined, captured once and replayed with new
+    inputs: every replay equals the eager calls, and is attention over what the cache then holds."""
+    heads, kv, dim, page, block, n_req = 8, 2, 64, 16, 8, 5
+    lens, new = i32([30, 1, 7, 100, 47]), i32([1, 1, 1, 1, 1])
+    qkv = normal((n_req, heads + 2 * kv, dim), BF, 0)
+    q, k, v = qkv.split([heads, kv, kv], 1)
+    pages = 64
+    caches = [x for i in (1, 2) for x in cache8(pages, page, kv, dim, block, i)]
+    kc, ks, vc, vs = caches
+    first = [x.view(torch.uint8).clone() for x in caches]
+    perm = torch.randperm(pages, generator=torch.Generator().manual_seed(2)).int().cuda()
+    table = torch.full((n_req, 10), -1, dtype=torch.int32, device="cuda")
+    for r, n in enumerate([2, 1, 1, 7, 3]):
+        table[r, :n] = perm[r * 10:r * 10 + n]
+    first_table = table.clone()
+    free = torch.cat([perm[50:], torch.full((50,), -1, dtype=torch.int32, device="cuda")])
+    n_free = i32([14])
+    angle = torch.rand((200, 32), generator=torch.Generator().manual_seed(3)) * 6
+    cos, sin = angle.cos().cuda(), angle.sin().cuda()
+    w = normal((dim,), BF, 4)
+    (keys, krow), (values, vrow) = (cache8(5, 8, kv, dim, block, i) for i in (5, 6))
+    keys, values, krow, vrow = (x.flatten(0, 1) for x in (keys, values, krow, vrow))
+    ids = torch.randint(-1, 40, (n_req, heads, 10), generator=torch.Generator().manual_seed(7), dtype=torch.int32).cuda()
+
+    def reset():
+        for x, y in zip(caches, first):
+            x.view(torch.uint8).copy_(y)
+        table.copy_(first_table)  # no page belongs to two requests
+
+    def step():
+        plan = jx.kv_plan(lens, new, table, free, n_free, page, n_req)
+        ready = jx.qk_norm_rope8(q, k, v, kc, vc, ks, vs, plan.pos, plan.slot, cos, sin, w, w)
+        part = jx.paged_attention8(ready, kc, vc, ks, vs, table, plan.q_start, plan.kv_len, 0.125)
+        out, lse = jx.found_attention8(ready, keys, values, krow, vrow, ids, 0.125, block, part=part)
+        return out, lse, plan.kv_len, part[0], part[1], ready, plan.q_start
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    reset()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(3):
+        qkv.copy_(normal(qkv.shape, BF, 20 + i, 3.0 ** i))
+        lens.copy_(i32([30 + i, 1, 7, 95 + i, 47]))
+        reset()
+        want = [x.clone() for x in step()]
+        cache = [x.view(torch.uint8).clone() for x in caches]
+        torch.cuda.synchronize()
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)
+        for a, b in zip(caches, cache):
+            assert torch.equal(a.view(torch.uint8), b)
+        plain.check((held[3], held[4]), plain.paged(held[5], plain8.stands_for(kc, ks), plain8.stands_for(vc, vs), table, held[6], held[2], 0.125, 0))
+        plain.check((held[0], held[1]), found8_want(held[5], keys, values, krow, vrow, ids, 0.125, block, part=(held[3], held[4])))
