@@ -27,7 +27,7 @@ hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStr
 hipError_t launch_found_attention(const jx_found_args& a, hipStream_t st);
 // the same over keys and values of 8 bits
 hipError_t launch_qk_norm_rope8(const jx_rope_args& a, const jx_kv_scales& s, hipStream_t st);
-int64_t paged_attention8_bytes(const jx_attend_args& a, const jx_kv_scales& s);
+int64_t paged_attention8_bytes(const jx_attend_args& a);
 hipError_t launch_paged_attention8(const jx_attend_args& a, const jx_kv_scales& s, uint8_t* work, hipStream_t st);
 hipError_t launch_found_attention8(const jx_found_args& a, const jx_kv_scales& s, hipStream_t st);
 

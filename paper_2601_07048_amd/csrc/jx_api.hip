@@ -1398,13 +1398,13 @@ int jx_paged_attention(const jx_attend_args* a, void* d_work, int64_t work_bytes
 
 int64_t jx_paged_attention8_bytes(const jx_attend_args* a, const jx_kv_scales* scales) {
     if (int rc = check_attend8(a, scales)) return rc;
-    return jx::paged_attention8_bytes(*a, *scales);
+    return jx::paged_attention8_bytes(*a);
 }
 
 int jx_paged_attention8(const jx_attend_args* a, const jx_kv_scales* scales, void* d_work, int64_t work_bytes, void* stream) {
     if (int rc = check_attend8(a, scales)) return rc;
     if (a->n_tokens == 0) return JX_OK;
-    if (int rc = check_attend_rows(a, jx::paged_attention8_bytes(*a, *scales), d_work, work_bytes)) return rc;
+    if (int rc = check_attend_rows(a, jx::paged_attention8_bytes(*a), d_work, work_bytes)) return rc;
     if (int rc = check_scales_there(scales)) return rc;
     JX_HIP(jx::launch_paged_attention8(*a, *scales, (uint8_t*)d_work, as_stream(stream)));
     return JX_OK;

@@ -87,7 +87,7 @@ struct Plan {
     int64_t joins, total;  // bytes before the joins, in all
 };
 
-Plan make_plan(const jx_attend_args& a) {
+Plan make_plan(const jx_attend_args& a, bool coded) {
     const int nb = blocks_of(a.head_dim);
     Plan p = {};
     const long long rows = a.n_tokens * (a.n_heads / a.n_kv_heads);
@@ -141,21 +141,30 @@ void join_dim(const PagedArgs& g, hipStream_t st) {
 
 }  // namespace
 
-int64_t paged_attention_bytes(const jx_attend_args& a) { return make_plan(a).total; }
+namespace {
 
-hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStream_t st) {
-    const Plan p = make_plan(a);
-    const int rows = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 4 : 2;
+hipError_t launch(const jx_attend_args& a, const jx_kv_scales* s, uint8_t* work, hipStream_t st) {
+    const Plan p = make_plan(a, s != NULL);
+    const int rows = (a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 4 : 2) * (s ? 2 : 1);  // that a load of a wavefront takes
     const int near = a.cache.page >= rows && a.cache.token_stride * rows < (1 << 29);
     const int group = a.n_heads / a.n_kv_heads, bits = group == 1 ? 1 : log2_of(group - 1) + 1;
     const uint32_t mul = (uint32_t)(((1ull << (31 + bits)) + group - 1) / group);
-    const PagedArgs g = {a, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.part_rows, p.own, (float*)work,
-                         (Join*)(work + p.joins)};
-    hipError_t e = p.rows >= 128 ? launch_paged_many(g, p.rows, st) : launch_paged_few(g, p.rows, st);
+    const Scales scales = s ? Scales{s->d_k, s->d_v, log2_of(s->block), a.cache.page / s->block} : Scales{};
+    const PagedArgs g = {a, scales, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.part_rows, p.own,
+                         (float*)work, (Join*)(work + p.joins)};
+    hipError_t e = p.rows >= 128 ? (s ? launch_paged_many8 : launch_paged_many)(g, p.rows, st) : (s ? launch_paged_few8 : launch_paged_few)(g, p.rows, st);
     if (e != hipSuccess || !p.n_work) return e;
     if (a.dtype == JX_BF16) join_dim<__bf16>(g, st);
     else join_dim<_Float16>(g, st);
     return hipGetLastError();
 }
+
+}  // namespace
+
+int64_t paged_attention_bytes(const jx_attend_args& a) { return make_plan(a, false).total; }
+int64_t paged_attention8_bytes(const jx_attend_args& a) { return make_plan(a, true).total; }
+
+hipError_t launch_paged_attention(const jx_attend_args& a, uint8_t* work, hipStream_t st) { return launch(a, NULL, work, st); }
+hipError_t launch_paged_attention8(const jx_attend_args& a, const jx_kv_scales& s, uint8_t* work, hipStream_t st) { return launch(a, &s, work, st); }
 
 }  // namespace jx

@@ -1,11 +1,13 @@
 // Tiles of a paged attention call: what they are, how they are shared out over workgroups, how rows lie in LDS.
 #pragma once
 #include "attend_walk.h"
+#include "codes8.h"
 
 namespace jx {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int MAX_SLOTS = 1024;  // tiles that are shared out by keys, see Shares
 
@@ -17,6 +19,7 @@ struct __attribute__((aligned(16))) Join {
 
 struct PagedArgs {
     jx_attend_args a;
+    Scales scales;          // of keys and values in 8 bits
     int page_shift, group;  // group: query heads of a key head
     uint32_t group_mul, group_shift;  // see by_group
     int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
@@ -32,6 +35,8 @@ struct PagedArgs {
 
 hipError_t launch_paged_many(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 128, or 256 up to 128 elements
 hipError_t launch_paged_few(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 16 or 32
+hipError_t launch_paged_many8(const PagedArgs& g, int rows, hipStream_t st);  // over keys and values in 8 bits
+hipError_t launch_paged_few8(const PagedArgs& g, int rows, hipStream_t st);
 
 // wavefronts of a workgroup that takes few rows, by blocks of 32 elements: as many as have room for their values in LDS
 constexpr int FEW_WAVES(int nb) { return nb <= 4 ? 8 : 4; }
@@ -125,6 +130,41 @@ __device__ __forceinline__ constexpr int mix(int r) {
 }
 
 typedef __attribute__((address_space(3))) char* lds_ptr;
+
+// The cache holds elements of type T, or codes (C = uint8_t)
+template <typename C>
+constexpr bool CODED = sizeof(C) == 1;
+
+// Sixteen codes of one row, times its scale, into the row's chunks 2 c and 2 c + 1
+template <typename T, int CH>
+__device__ __forceinline__ void put_codes(u32x4 w, float scale, lds_ptr tile, int row, int c) {
+    typedef __attribute__((address_space(3))) u32x4* out;
+    const int at = row * CH * 16, place = 2 * c ^ mix<CH>(row);
+    *(out)(tile + at + place * 16) = (u32x4){codes_pair<T, false>(w[0], scale), codes_pair<T, true>(w[0], scale), codes_pair<T, false>(w[1], scale), codes_pair<T, true>(w[1], scale)};
+    *(out)(tile + at + (place ^ 1) * 16) = (u32x4){codes_pair<T, false>(w[2], scale), codes_pair<T, true>(w[2], scale), codes_pair<T, false>(w[3], scale), codes_pair<T, true>(w[3], scale)};
+}
+
+// A query row over keys i0 .. i1 - 1 by a wavefront, LPR lanes a row with eight elements each, q times scale * log2 e; where(i): chunks of 16
+// bytes from k and v to the row of key i, < 0 where it is masked; scale_at(i): its block among the scales
+template <typename T, typename C, int LPR, typename Where, typename ScaleAt>
+__device__ __forceinline__ Softmax one_row(const PagedArgs& g, const char* k, const char* v, f32x8 q, bool inside, int i0, int i1, Where where, ScaleAt scale_at) {
+    if constexpr (CODED<C>) {
+        float x[8];
+        for (int e = 0; e < 8; e++) x[e] = q[e];
+        SoftmaxCodes<8> s = walk_codes<LPR, 8>((const uint8_t*)k, (const uint8_t*)v, x, inside, i0, i1, [&](long long i) {
+            const long long at = where((int)i);
+            if (at < 0) return RowCodes{-1, 0.0f, 0.0f};
+            const long long b = scale_at((int)i);
+            return RowCodes{at * 16, scale_value(g.scales.k[b]), scale_value(g.scales.v[b])};
+        });
+        gather_codes<LPR>(s);
+        Softmax r = {s.m, s.l, {0, 0, 0, 0, 0, 0, 0, 0}};
+        for (int e = 0; e < 8; e++) r.acc[e] = s.acc[e];
+        return r;
+    } else {
+        return gather<LPR>(walk_keys<T, LPR>((const T*)k, (const T*)v, q, inside, i0, i1, [&](long long i) { const long long at = where((int)i); return at < 0 ? -1ll : at * 8; }));
+    }
+}
 
 __device__ __forceinline__ void load_lds16(const void* from, lds_ptr to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
