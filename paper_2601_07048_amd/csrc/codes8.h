@@ -64,7 +64,7 @@ struct SoftmaxCodes {
 template <int LPR, int N, typename Where>
 __device__ __forceinline__ SoftmaxCodes<N> walk_codes(const uint8_t* k, const uint8_t* v, const float (&q)[N], bool inside, long long i0, long long i1,
                                                       Where where) {
-    constexpr int AT_ONCE = 64 / LPR, U = AT_ONCE >= 16 ? 4 : AT_ONCE >= 8 ? 4 : 8, W = N / 4;
+    constexpr int AT_ONCE = 64 / LPR, U = N == 8 ? 2 : AT_ONCE >= 8 ? 4 : 8, W = N / 4;
     typedef uint32_t Words __attribute__((ext_vector_type(W)));
     const int lane = lane_id(), c = lane % LPR * N, group = lane / LPR;
     SoftmaxCodes<N> s;

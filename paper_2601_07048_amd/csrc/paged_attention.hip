@@ -7,8 +7,9 @@ namespace jx {
 
 namespace {
 
-// Workgroups for the elements of a tile's rows, eight a wavefront
-constexpr int JOINERS(int nb) { return nb <= 4 ? 1 : 2; }
+// Threads of a workgroup: a wavefront for eight elements of a tile's rows.  Small ones, since most of those of a launch have nothing to
+// join, and a tile of many pieces is read by as many CUs
+constexpr int JOIN_THREADS = 256;
 
 // The parts of a tile whose keys several workgroups share, as one: the tile that workgroup blockIdx.x began and did not end;
 // blockIdx.y: which 32 rows.  A wavefront takes 8 elements, as the lanes held them when the parts were written, and of few rows
@@ -16,14 +17,14 @@ constexpr int JOINERS(int nb) { return nb <= 4 ? 1 : 2; }
 // are no more (8 always: 27 and not 16 us for a chunk of 4,096 tokens): single tokens of 64 requests 4.8 us, 40 MB of parts of
 // 256 elements 15.2.
 template <typename T, int NB>
-__global__ __launch_bounds__(NB * 256 / JOINERS(NB)) void join_kernel(PagedArgs g) {
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(PagedArgs g) {
     constexpr int PIECES = 8;
     const jx_attend_args& a = g.a;
     const int lane = lane_id(), e0 = (int)((blockIdx.z * blockDim.x + threadIdx.x) >> 6) * 8, d = a.head_dim;
     const Join j = g.joins[blockIdx.x];
     const int count = j.pieces ? j.count - (int)blockIdx.y * 32 : 0;
     if (count <= 0 || e0 >= d) return;
-    const int wide = count <= 8 ? 16 : count <= 16 ? 32 : 64, side = 64 / wide;  // lanes of a piece, pieces side by side
+    const int wide = count <= 4 ? 8 : count <= 8 ? 16 : count <= 16 ? 32 : 64, side = 64 / wide;  // lanes of a piece, pieces side by side
     const int row = lane & (wide / 2 - 1), half = lane / (wide / 2) & 1;
     const float* parts = g.part + blockIdx.y * part_floats(NB);
     const int to_s = part_at(row, e0 + half * 4), to_m = NB * 1024 + row;
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(NB * 256 / JOINERS(NB)) void join_kernel(PagedArgs 
 
 struct Plan {
     int rows;  // of a tile: 16, 32: few rows, 128, 256: many
-    int slots, groups, n_work, part_rows, own;
+    int slots, groups, n_work, columns, part_rows, own;
     int64_t joins, total;  // bytes before the joins, in all
 };
 
@@ -111,21 +112,24 @@ Plan make_plan(const jx_attend_args& a, bool coded) {
     // 11.1 or 12.5; 64 requests 18 or 16.  64 elements, 16 key heads, 16 requests of up to 1,024 keys: 10.9, shared out 18.4.
     const int64_t room = (int64_t)a.table_pages * a.cache.page, keys = a.window ? std::min<int64_t>(room, (int64_t)a.window + 16) : room;
     p.own = p.rows < 128 && (int64_t)p.slots * a.n_kv_heads <= 384 && keys <= 1024 / (nb <= 2 ? 1 : nb);
-    const double units = ((double)a.table_pages * a.cache.page / UNIT + 1) * p.slots * a.n_kv_heads;  // at most
+    const double units = ((double)a.table_pages * a.cache.page / (coded ? UNIT / 2 : UNIT) + 1) * p.slots * a.n_kv_heads;  // at most
     // as many shares as the card holds workgroups (many rows) or wavefronts (few) at a time
     if (p.slots && !p.own && p.slots <= MAX_SLOTS && units < 2e9) {
         p.groups = 256 * (p.rows >= 128 ? MANY_PER_CU(nb, p.rows) : nb <= 2 ? 2 : 1);
         p.n_work = p.rows >= 128 ? p.groups : p.groups * FEW_WAVES(nb);
     }
+    p.columns = 1;
+    if (coded && p.rows < 128)
+        while (p.columns < 4 && a.n_kv_heads % (2 * p.columns) == 0) p.columns *= 2;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
-    p.joins = up(((int64_t)2 * p.groups * p.part_rows + (p.rows >= 128 ? 0 : p.n_work)) * part_floats(nb) * 4);
-    p.total = p.joins + up((int64_t)p.groups * sizeof(Join));
+    p.joins = up(((int64_t)2 * p.groups * p.columns * p.part_rows + (p.rows >= 128 ? 0 : p.n_work)) * part_floats(nb) * 4);
+    p.total = p.joins + up((int64_t)p.groups * p.columns * sizeof(Join));
     return p;
 }
 
 template <typename T, int NB>
 void join(const PagedArgs& g, hipStream_t st) {
-    join_kernel<T, NB><<<dim3(g.groups, g.part_rows, JOINERS(NB)), NB * 256 / JOINERS(NB), 0, st>>>(g);
+    join_kernel<T, NB><<<dim3(g.groups * g.columns, g.part_rows, NB * 256 / JOIN_THREADS), JOIN_THREADS, 0, st>>>(g);
 }
 
 template <typename T>
@@ -150,7 +154,7 @@ hipError_t launch(const jx_attend_args& a, const jx_kv_scales* s, uint8_t* work,
     const int group = a.n_heads / a.n_kv_heads, bits = group == 1 ? 1 : log2_of(group - 1) + 1;
     const uint32_t mul = (uint32_t)(((1ull << (31 + bits)) + group - 1) / group);
     const Scales scales = s ? Scales{s->d_k, s->d_v, log2_of(s->block), a.cache.page / s->block} : Scales{};
-    const PagedArgs g = {a, scales, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.part_rows, p.own,
+    const PagedArgs g = {a, scales, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.columns, p.part_rows, p.own,
                          (float*)work, (Join*)(work + p.joins)};
     hipError_t e = p.rows >= 128 ? (s ? launch_paged_many8 : launch_paged_many)(g, p.rows, st) : (s ? launch_paged_few8 : launch_paged_few)(g, p.rows, st);
     if (e != hipSuccess || !p.n_work) return e;

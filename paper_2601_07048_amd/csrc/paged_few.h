@@ -27,6 +27,11 @@ __device__ __forceinline__ void load_lds16_at(const char* from, uint32_t off, ui
                                              (__attribute__((address_space(3))) void*)to, 16, off, step, 0, 0);
 }
 
+// ... into registers
+__device__ __forceinline__ u32x4 load16_at(const char* from, uint32_t off, uint32_t step) {
+    return __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7FFFFFFF, 0x00020000), off, step, 0);
+}
+
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most the N latest are on their way
     asm volatile("" ::: "memory");
@@ -61,8 +66,9 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, h = lane >> 4, d = a.head_dim;
+    constexpr int U = CODED<C> ? 32 : UNIT;
     Shares sh;
-    const bool any = sh.begin<ROWS, WAVES>(g, (int*)(lds + WAVES * 2 * TILE), wave);
+    const bool any = sh.begin<ROWS, WAVES, U>(g, (int*)(lds + WAVES * 2 * TILE), wave);
     sh.clear_rows<T>(g);
     if (!any && !g.n_work) return;
 
@@ -112,13 +118,13 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         if (h < 2) part[NC * 1024 + h * 32 + b * 16 + r16] = h ? l : m;
     };
     while (sh.x0 < sh.x1) {
-        const Segment e = sh.next<ROWS, WAVES>(g);
+        const Segment e = sh.next<ROWS, WAVES, U>(g);
         t = e.t;
         if (t.r < 0) return;
         if (e.u0 == e.u1) break;  // more wavefronts than units
-        head = sh.head;
+        head = sh.key_head();
         units = e.units;
-        const int key0 = t.lo + e.u0 * UNIT, key1 = min(t.lo + e.u1 * UNIT, t.hi);
+        const int key0 = t.lo + e.u0 * U, key1 = min(t.lo + e.u1 * U, t.hi);
         const char* kb = (const char*)a.cache.d_k + head * a.cache.head_stride * sizeof(C);
         const char* vb = (const char*)a.cache.d_v + head * a.cache.head_stride * sizeof(C);
         const int32_t* table = a.d_table + (size_t)t.r * a.table_pages;
@@ -141,7 +147,10 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         auto load_keys = [&](int key, const Pages& p) {
             for (int b = 0; b < 2; b++) {
                 const char* from = kb + row_at(p.id[b], key + b * 16);
-                for (int i = 0; i < KC; i++) k[b][i] = *(const s16x8*)(from + k_row + k_chunk(i));
+                for (int i = 0; i < KC; i++) {
+                    if constexpr (CODED<C>) k[b][i] = __builtin_bit_cast(s16x8, load16_at(from, there(p.id[b]) ? k_row + k_chunk(i) : OUTSIDE, 0));
+                    else k[b][i] = *(const s16x8*)(from + k_row + k_chunk(i));
+                }
             }
         };
         // Codes: values pass through registers too, since they become elements on their way into LDS.  The scales of 32 keys and 32 values
@@ -152,10 +161,12 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             return ((long long)(there(id) ? id : 0) * g.scales.per_page + ((key & page_mask) >> g.scales.shift)) * a.n_kv_heads + head;
         };
         auto load_codes = [&](int key, const Pages& p) {
+            const uint32_t lane_off = lane / CHM * token_chunks * 16 + min(lane % CHM, d / 16 - 1) * 16;
+            const int left = key1 - key - (int)(lane / CHM);
             for (int i = 0; i < VC; i++) {  // 64 / CHM rows a load, 16 or fewer
-                const int b = i * 2 / VC;
-                const char* from = vb + row_at(p.id[b], key + b * 16);
-                y8[i] = *(const u32x4*)(from + (uint32_t)((i * (64 / CHM) & 15) + lane / CHM) * token_chunks * 16 + min(lane % CHM, d / 16 - 1) * 16);
+                const int b = i * 2 / VC, row = i * (64 / CHM) & 15;
+                const int rows = there(p.id[b]) ? left - b * 16 : INT_MIN;
+                y8[i] = load16_at(vb + row_at(p.id[b], key + b * 16), row < rows ? lane_off : OUTSIDE, row * token_chunks * 16);
             }
         };
         auto load_scales = [&](int key, const Pages& p) -> uint32_t {
@@ -174,10 +185,10 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             }
         };
         Pages here = pages_at(key0), next = pages_at(key0 + KEYS);
+        if constexpr (CODED<C>) bytes = load_scales(key0, here);
         load_keys(key0, here);
         if constexpr (CODED<C>) {
             load_codes(key0, here);
-            bytes = load_scales(key0, here);
         } else {
             load_values(key0, here, mine);
         }
@@ -223,6 +234,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                         for (int y = 0; y < 2; y++) {
                             const u32x4 e = {codes_pair<T, false>(w[2 * y], scale), codes_pair<T, true>(w[2 * y], scale), codes_pair<T, false>(w[2 * y + 1], scale), codes_pair<T, true>(w[2 * y + 1], scale)};
                             for (int b = 0; b < RB; b++) s[b][x] = mul16<T>(__builtin_bit_cast(s16x8, e), q[b][2 * i + y], s[b][x]);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
                     }
                 }
@@ -267,10 +279,10 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                 const int left = key1 - key;
                 for (int i = 0; i < VC; i++) {
                     const int row = i * (64 / CHM) + lane / CHM;
-                    // zeros, whose scale has to be a number, for values that are not there
+                    // what is not there has come as zeros, whose scale has to be a number
                     const bool gone = !all && (row >= left || !there(i * 2 / VC ? here.id[1] : here.id[0]));
                     const float scale = scale_bits((uint32_t)__shfl((int)bytes, 32 + row, 64));
-                    put_codes<T, CH>(gone ? (u32x4)0u : y8[i], gone ? 1.0f : scale, v, row, lane % CHM);
+                    put_codes<T, CH>(y8[i], gone ? 1.0f : scale, v, row, lane % CHM);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (more) load_codes(key + KEYS, next);
@@ -279,7 +291,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                 if (more) wait_loads<NV + NK>();
                 else wait_loads<0>();
             }
-            constexpr int AT_ONCE = RB == 1 ? OB : OB / 2;  // by the registers that are free
+            constexpr int AT_ONCE = OB / (CODED<C> ? 2 * RB : RB);  // by the registers that are free
             for (int i0 = 0; i0 < OB; i0 += AT_ONCE) {
                 s16x8 y[AT_ONCE];
                 for (int i = 0; i < AT_ONCE; i++) {
@@ -298,7 +310,15 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             }
             __builtin_amdgcn_sched_barrier(0);  // the place has been read before it is filled again
         };
-        if (key0 < key1) {
+        if (CODED<C> && key0 < key1) {
+            // The last time is like the others: what is asked for behind the last key is outside the range, and not read
+            for (int key = key0; key < key1; key += KEYS) {
+                const Pages then = pages_at(key + 2 * KEYS);
+                work_on(std::true_type{}, key, here, next, mine, mine);
+                here = next;
+                next = then;
+            }
+        } else if (key0 < key1) {
             int key = key0, buf = 0;
             for (; key + KEYS < key1; key += KEYS, buf ^= TILE) {
                 const Pages then = pages_at(key + 2 * KEYS);
@@ -314,7 +334,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
         // Results: of a whole tile, of a part that ends one, or of one that is open at the share's end
         const bool whole = e.whole(), open = !whole && (g.own || e.u1 < e.units);
         if (open) ends = e.u0 == 0 ? BEGUN : WITHIN;
-        float* part = whole || open ? NULL : wave == 0 ? sh.part(g, false, NC) : sh.inner(g, sh.work, NC);
+        float* part = whole || open ? NULL : wave == sh.first ? sh.part(g, false, NC) : sh.inner(g, sh.work, NC);
         float* sums = (float*)(lds + wave * 2 * TILE);  // [RB][OB][64][4], as the lanes hold them
         constexpr uint32_t ODD = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;  // infinities and what is not a number
         if (!ballot((worst & 0xFFFF) >= ODD || worst >> 16 >= ODD)) {
@@ -377,7 +397,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     // Tiles that shares of this workgroup have cut: the first of them takes what the others have added
     if (lane == 0) wave_end[wave] = ends;
     __syncthreads();
-    if (ends == CLOSED || (ends == WITHIN && wave > 0)) return;
+    if (ends == CLOSED || (ends == WITHIN && wave > sh.first)) return;
     for (int b = 0; b < RB; b++) {
         f32x4 o[OB];
         for (int i = 0; i < OB; i++) o[i] = *(const f32x4*)(lds + wave * 2 * TILE + ((b * OB + i) * 64 + lane) * 16);
@@ -393,10 +413,11 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
             }
         };
         int w = wave + 1;
-        for (; w < sh.active && wave_end[w] == WITHIN; w++)
+        const int end = sh.first + sh.active;
+        for (; w < end && wave_end[w] == WITHIN; w++)
             add(wave_m[w][b * 16 + r16], wave_l[w][b * 16 + r16],
                 [&](int i) { return *(const f32x4*)(lds + w * 2 * TILE + ((b * OB + i) * 64 + lane) * 16); });
-        const bool ended = w < sh.active;  // its share begins with the tile's end
+        const bool ended = w < end;  // its share begins with the tile's end
         if (ended && b * 16 + r16 < t.count) {
             const float* part = sh.inner(g, sh.work + w - wave, NC);
             add(part[NC * 1024 + b * 16 + r16], part[NC * 1024 + 32 + b * 16 + r16],

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const lds_ptr ring = (lds_ptr)lds;
     Shares sh;
-    const bool any = sh.begin<ROWS, 1>(g, (int*)(lds + 4 * TILE), 0);
+    const bool any = sh.begin<ROWS, 1, UNIT>(g, (int*)(lds + 4 * TILE), 0);
     sh.clear_rows<T>(g);
     if (!any) return;
 
@@ -172,10 +172,10 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
     const float c = fmaxf(fabsf(a.scale) * LOG2E, __FLT_MIN__);  // a scale of 0 has to leave -infinity what it is
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
     while (sh.x0 < sh.x1) {
-        const Segment e = sh.next<ROWS, 1>(g);
+        const Segment e = sh.next<ROWS, 1, UNIT>(g);
         const Tile& t = e.t;
         if (t.r < 0) return;
-        const int work = sh.group, head = sh.head;
+        const int work = sh.group, head = sh.key_head();
         const bool whole = e.whole();
         const int key0 = t.lo + e.u0 * KEYS, key1 = min(t.lo + e.u1 * KEYS, t.hi);
 

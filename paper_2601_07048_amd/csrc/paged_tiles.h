@@ -25,12 +25,13 @@ struct PagedArgs {
     int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
     int slots;              // tiles at most
     int groups, n_work;     // workgroups, and shares of all tiles (1 or FEW_WAVES for each workgroup); 0 = a share a tile
+    int columns;            // of few rows: key heads that the wavefronts of a workgroup share between them, see Shares
     int part_rows;          // tiles' rows / 32
     int own;                // few rows, n_work = 0: whether a workgroup takes a tile, not a wavefront
-    float* part;            // [2 groups][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's
+    float* part;            // [2 groups columns][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's
                             // keys, sums [NB][4][64][4], largest scores and weights' sums [2][32]; the sums as a wavefront holds
                             // them, see part_at
-    Join* joins;            // [groups]
+    Join* joins;            // [columns][groups]
 };
 
 hipError_t launch_paged_many(const PagedArgs& g, int rows, hipStream_t st);  // rows: of a tile, 128, or 256 up to 128 elements
@@ -191,7 +192,8 @@ struct Segment {  // units u0 .. u1 - 1 of the tile's
 
 __host__ __device__ inline size_t shares_bytes(int n_req, int slots) { return (size_t)(n_req + 1) * 8 + (size_t)(slots + 1) * 4 + (size_t)slots * 2; }
 
-__device__ __forceinline__ int units_of(const Tile& t) { return max((t.hi - t.lo + UNIT - 1) / UNIT, 1); }  // results have to be written
+template <int U>
+__device__ __forceinline__ int units_of(const Tile& t) { return max((t.hi - t.lo + U - 1) / U, 1); }  // results have to be written
 
 struct Shares {
     int *starts, *lens;  // [n_req + 1]
@@ -202,14 +204,17 @@ struct Shares {
     uint32_t x0, x1, per_head, each, rem;
     int head, slot;
     int group, per, work, active;  // workgroup in the order of the shares, shares of each, this share, shares that this workgroup has
+    int columns, column, first;    // see begin; the first share's wavefront of this column
 
     // For share `sub` of up to PER of the workgroup, by all of it.  false: there is no such share
-    template <int ROWS, int PER>
+    template <int ROWS, int PER, int U>
     __device__ __forceinline__ bool begin(const PagedArgs& g, int* lds, int sub) {
         const jx_attend_args& a = g.a;
         const int tid = threadIdx.x, lane = lane_id(), THREADS = (int)blockDim.x;
         x0 = 0;
         x1 = 1;
+        columns = 1;
+        column = first = 0;
         if (!g.n_work) {
             work = sub;
             const uint32_t i = g.own ? blockIdx.x : blockIdx.x * PER + sub;
@@ -234,7 +239,7 @@ struct Shares {
                 else hi = mid;
             }
             const Tile t = make_tile<ROWS>(g, lo, s, starts[lo], starts[lo + 1], lens[lo]);
-            cum[s + 1] = t.r < 0 ? 0 : units_of(t);
+            cum[s + 1] = t.r < 0 ? 0 : units_of<U>(t);
             req[s] = (uint16_t)lo;
         }
         if (tid == 0) cum[0] = 0;
@@ -253,25 +258,37 @@ struct Shares {
         }
         __syncthreads();
         per_head = __builtin_amdgcn_readfirstlane(cum[g.slots]);
-        const uint32_t all = per_head * a.n_kv_heads, shares = min((uint32_t)g.n_work, all);  // none is empty
+        const uint32_t units = per_head * a.n_kv_heads;
+        // With enough units each of `columns` neighbouring key heads has wavefronts of its own in every workgroup, which then reads the same
+        // tokens of all of them: rows of 128 bytes that lie side by side, about the same time (64 single tokens of up to 8,192 keys, 8 key
+        // heads of 128 codes: MEASURE us, each workgroup with a head MEASURE).
+        columns = PER == 1 || units < (uint32_t)g.n_work ? 1 : g.columns;
+        const int of_column = PER / columns, at = sub % of_column;
+        column = sub / of_column;
+        first = column * of_column;
+        const uint32_t all = units / columns, shares = min((uint32_t)g.n_work / columns, all);  // of a column; none is empty
         // shares of a workgroup follow each other; consecutive workgroups stay on one XCD's cache, few are spread over all
         per = PER == 1 ? 1 : (int)((shares + g.groups - 1) / g.groups);
-        group = all < (uint32_t)g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.groups / 8) + (int)(blockIdx.x / 8);
-        work = group * per + sub;
+        group = units < (uint32_t)g.n_work ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (g.groups / 8) + (int)(blockIdx.x / 8);
+        const int share = group * per + at;
+        work = group * PER + sub;
         active = min(per, (int)shares - group * per);
-        if (tid == 0) g.joins[group].pieces = 0;
-        if (sub >= active) {
+        if (tid < g.columns) g.joins[tid * g.groups + group].pieces = 0;
+        if (at >= active) {
             x1 = 0;
             return false;
         }
         each = all / shares;
         rem = all - each * shares;
-        x0 = work * each + min((uint32_t)work, rem);
-        x1 = x0 + each + ((uint32_t)work < rem);
+        x0 = share * each + min((uint32_t)share, rem);
+        x1 = x0 + each + ((uint32_t)share < rem);
         head = (int)(x0 / per_head);
         slot = -1;
         return true;
     }
+
+    // Heads are counted in their column
+    __device__ __forceinline__ int key_head() const { return head * columns + column; }
 
     // Rows that belong to no request: zeros and -infinity, by all workgroups, after begin
     template <typename T>
@@ -293,7 +310,7 @@ struct Shares {
     }
 
     // The segment that begins with unit x0
-    template <int ROWS, int PER>
+    template <int ROWS, int PER, int U>
     __device__ __forceinline__ Segment next(const PagedArgs& g) {
         const jx_attend_args& a = g.a;
         Segment e;
@@ -301,7 +318,7 @@ struct Shares {
             const int r = last_before(a.n_req, [&](int i) { return first_slot<ROWS>(a.d_q_start[i], i, g) <= slot; });
             e.t = make_tile<ROWS>(g, r, slot, a.d_q_start[r], a.d_q_start[r + 1], a.d_kv_len[r]);
             e.u0 = 0;
-            e.u1 = e.units = e.t.r < 0 ? 1 : units_of(e.t);
+            e.u1 = e.units = e.t.r < 0 ? 1 : units_of<U>(e.t);
             if (PER > 1 && g.own) {
                 active = min(PER, e.units);
                 e.u0 = (int)((long long)e.units * min(work, active) / active);
@@ -330,21 +347,21 @@ struct Shares {
         return e;
     }
 
-    // Where a workgroup leaves its part of a tile that it shares with others: of the tile that it begins and does not end (`first`) or
+    // Where a workgroup leaves its part of a tile that it shares with others: of the tile that it begins and does not end (`begun`) or
     // that it found begun
-    __device__ __forceinline__ float* part(const PagedArgs& g, bool first, int nb) const {
-        return g.part + (size_t)(2 * group + first) * g.part_rows * part_floats(nb);
+    __device__ __forceinline__ float* part(const PagedArgs& g, bool begun, int nb) const {
+        return g.part + (size_t)(2 * (column * g.groups + group) + begun) * g.part_rows * part_floats(nb);
     }
     // ... and a wavefront its part of a tile that others of its workgroup have begun
     __device__ __forceinline__ float* inner(const PagedArgs& g, int of_work, int nb) const {
-        return g.part + (size_t)(2 * g.groups + of_work) * part_floats(nb);
+        return g.part + (size_t)(2 * g.groups * g.columns + of_work) * part_floats(nb);
     }
 
     // The first workgroup of those that share a tile, which began with unit x of all, says who they are
     __device__ __forceinline__ void name(const PagedArgs& g, const Tile& t, uint32_t x, int units) const {
         const uint32_t end = x + units - 1, large = rem * (each + 1);  // the tile's last unit, and whose it is
         const int last = (int)(end < large ? end / (each + 1) : rem + (end - large) / each);
-        g.joins[group] = {last / per - group + 1, head, t.first, t.count, t.start, {0, 0, 0}};
+        g.joins[column * g.groups + group] = {last / per - group + 1, key_head(), t.first, t.count, t.start, {0, 0, 0}};
     }
 };
 
