@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import NamedTuple
 
 import torch
@@ -406,14 +407,15 @@ def _gpu(t):
     return i
 
 
-def _no_gradient(t):
-    assert not (t.requires_grad and torch.is_grad_enabled()), "no gradient goes through the attention calls: make them under torch.no_grad()"
+def _no_gradient():
+    assert not torch.is_grad_enabled(), "no gradient goes through the attention calls: make them under torch.no_grad()"
 
 
-def _rows(t, i, dtype):
+def _rows(t, i, dtype, strides):
     """A tensor of any strides whose last dimension holds a head's elements."""
-    _no_gradient(t)
-    assert t.get_device() == i and t.dtype is dtype and (t.stride(-1) == 1 or t.shape[-1] == 1), (t.device, i, t.dtype)
+    if t.requires_grad:
+        _no_gradient()
+    assert t.get_device() == i and t.dtype is dtype and (strides[-1] == 1 or t.shape[-1] == 1), (t.device, i, t.dtype)
     return t.data_ptr()
 
 
@@ -424,23 +426,30 @@ def _array(t, i, dtype, *shape):
 
 def _real(t, i, dtype, *shape):
     """An array that a model may have learnt or made."""
-    _no_gradient(t)
+    if t.requires_grad:
+        _no_gradient()
     return _array(t, i, dtype, *shape)
 
 
-def _alike(a, b):
+def _alike(a, b, sa, sb):
     """Whether two tensors are laid out alike; the stride of a dimension of one has no meaning."""
-    if a.shape != b.shape:
-        return False
-    sa, sb = a.stride(), b.stride()
-    return sa == sb or all(n <= 1 or x == y for n, x, y in zip(a.shape, sa, sb))
+    return a.shape == b.shape and (sa == sb or all(n <= 1 or x == y for n, x, y in zip(a.shape, sa, sb)))
+
+
+# Records as bytes: made in a third of the time that a Structure takes
+_ROPE = struct.Struct("6i2q3q6q2qf4x5q2q3q2i")
+_ATTEND = struct.Struct("4iq3q2q3q2iq2i2qfi2q")
+_FOUND = struct.Struct("4iq3q2q3qqif2q2q")
+_SCALES = struct.Struct("2qi4x")
+assert (_ROPE.size, _ATTEND.size, _FOUND.size, _SCALES.size) == tuple(C.sizeof(x) for x in (RopeArgs, AttendArgs, FoundArgs, KvScales))
 
 
 def _kv_cache(k_cache, v_cache, i, dtype, head_dim):
+    """The fields of a jx_kv_cache."""
     pages, page, _, d = k_cache.shape
-    strides = k_cache.stride()
-    assert d == head_dim and _alike(k_cache, v_cache)
-    return KvCache(_rows(k_cache, i, dtype), _rows(v_cache, i, dtype), strides[0], strides[1], strides[2], page, pages)
+    ks, vs = k_cache.stride(), v_cache.stride()
+    assert d == head_dim and _alike(k_cache, v_cache, ks, vs)
+    return _rows(k_cache, i, dtype, ks), _rows(v_cache, i, dtype, vs), ks[0], ks[1], ks[2], page, pages
 
 
 def _kv_scales(k_cache, k_scale, v_scale, i):
@@ -448,7 +457,7 @@ def _kv_scales(k_cache, k_scale, v_scale, i):
     pages, page, kv, _ = k_cache.shape
     blocks = k_scale.shape[1]
     assert blocks >= 1 and page % blocks == 0, (page, blocks)
-    return KvScales(_real(k_scale, i, _E8M0, pages, blocks, kv), _real(v_scale, i, _E8M0, pages, blocks, kv), page // blocks)
+    return _SCALES.pack(_real(k_scale, i, _E8M0, pages, blocks, kv), _real(v_scale, i, _E8M0, pages, blocks, kv), page // blocks)
 
 
 def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
@@ -488,18 +497,18 @@ def _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, ep
     kv = k_cache.shape[2]
     dt, i = q.dtype, _gpu(q)
     if out is None:
-        out = torch.empty((t, h, d), dtype=dt, device=q.device)
+        out = q.new_empty((t, h, d))
     else:
         _array(out, i, dt, t, h, d)
     n_pos, half = cos.shape if cos is not None else (0x7FFFFFFF, 0)
     assert k.shape == v.shape == (t, kv, d)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
-    return out, i, RopeArgs(
-        _HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt), _rows(k, i, dt), _rows(v, i, dt), qs[0], qs[1], ks[0],
-        ks[1], vs[0], vs[1], _real(q_weight, i, dt, d) if q_weight is not None else None,
-        _real(k_weight, i, dt, d) if k_weight is not None else None, eps, _real(cos, i, _F32, n_pos, half) if half else None,
-        _real(sin, i, _F32, n_pos, half) if half else None, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
-        _kv_cache(k_cache, v_cache, i, of_cache or dt, d))
+    return out, i, _ROPE.pack(
+        _HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt, qs), _rows(k, i, dt, ks), _rows(v, i, dt, vs), qs[0], qs[1],
+        ks[0], ks[1], vs[0], vs[1], _real(q_weight, i, dt, d) if q_weight is not None else 0,
+        _real(k_weight, i, dt, d) if k_weight is not None else 0, eps, _real(cos, i, _F32, n_pos, half) if half else 0,
+        _real(sin, i, _F32, n_pos, half) if half else 0, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
+        *_kv_cache(k_cache, v_cache, i, of_cache or dt, d))
 
 
 def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
@@ -507,7 +516,7 @@ def qk_norm_rope(q, k, v, k_cache, v_cache, pos, slot, cos=None, sin=None, q_wei
     """jx_qk_norm_rope: the queries [tokens][heads][head_dim] made ready (in `out`, which may be a contiguous q); keys and values
     go to their slots of the caches [pages][page][kv_heads][head_dim] (any strides, alike in both)."""
     out, i, a = _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, eps, interleaved, out, None)
-    _run(_lib.jx_qk_norm_rope, i, C.byref(a))
+    _run(_lib.jx_qk_norm_rope, i, a)
     return out
 
 
@@ -516,17 +525,17 @@ def qk_norm_rope8(q, k, v, k_cache, v_cache, k_scale, v_scale, pos, slot, cos=No
     """jx_qk_norm_rope8: as qk_norm_rope, into caches of torch.float8_e4m3fn with scales [pages][blocks of a page][kv_heads] of
     torch.float8_e8m0fnu, both of which it updates."""
     out, i, a = _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, eps, interleaved, out, _E4M3)
-    _run(_lib.jx_qk_norm_rope8, i, C.byref(a), C.byref(_kv_scales(k_cache, k_scale, v_scale, i)))
+    _run(_lib.jx_qk_norm_rope8, i, a, _kv_scales(k_cache, k_scale, v_scale, i))
     return out
 
 
 def _outputs(out, q, i, t, h, d):
     """The pair to write into, made here if there is none, and its pointers."""
     if out is None:
-        o, lse = torch.empty((t, h, d), dtype=q.dtype, device=q.device), torch.empty((t, h), dtype=_F32, device=q.device)
+        o, lse = q.new_empty((t, h, d)), q.new_empty((t, h), dtype=_F32)
         return o, lse, o.data_ptr(), lse.data_ptr()
     o, lse = out
-    return o, lse, _array(o, i, q.dtype, t, h, d), _array(lse, i, _F32, t, h) if lse is not None else None
+    return o, lse, _array(o, i, q.dtype, t, h, d), _array(lse, i, _F32, t, h) if lse is not None else 0
 
 
 def _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, of_cache):
@@ -536,36 +545,37 @@ def _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, of_
     dt, i = q.dtype, _gpu(q)
     o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
     qs = q.stride()
-    return o, lse, i, AttendArgs(
-        _HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, i, dt), qs[0], qs[1], _kv_cache(k_cache, v_cache, i, of_cache or dt, d),
+    return o, lse, i, _ATTEND.pack(
+        _HEAD_TYPES[dt], h, k_cache.shape[2], d, t, _rows(q, i, dt, qs), qs[0], qs[1], *_kv_cache(k_cache, v_cache, i, of_cache or dt, d),
         _array(table, i, _I32, n, w), w, n, _array(q_start, i, _I32, n + 1), _array(kv_len, i, _I32, n), scale, window, p_out, p_lse)
 
 
-def _with_work(work, q, i, size, fn, *refs):
+def _with_work(work, q, i, size, fn, *records):
     """Calls fn with `work`, or with as many bytes as `size` asks for."""
     if work is None:
-        nbytes = size(*refs)
+        nbytes = size(*records)
         if nbytes < 0:
             _check(int(nbytes))
-        work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        work = q.new_empty(nbytes, dtype=torch.uint8)
     else:
         nbytes = work.shape[0]
         _array(work, i, torch.uint8, nbytes)
-    _run(fn, i, *refs, work.data_ptr(), nbytes)
+    _run(fn, i, *records, work.data_ptr(), nbytes)
 
 
 def paged_attention(q, k_cache, v_cache, table, q_start, kv_len, scale, window=0, out=None, work=None):
     """jx_paged_attention: (out [tokens][heads][head_dim], lse [tokens][heads]).  `out`: those two, to write into (lse may be None);
     `work`: a uint8 tensor as large as the call needs (made here where it is None)."""
     o, lse, i, a = _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, None)
-    _with_work(work, q, i, _lib.jx_paged_attention_bytes, _lib.jx_paged_attention, C.byref(a))
+    _with_work(work, q, i, _lib.jx_paged_attention_bytes, _lib.jx_paged_attention, a)
     return o, lse
 
 
 def paged_attention8(q, k_cache, v_cache, k_scale, v_scale, table, q_start, kv_len, scale, window=0, out=None, work=None):
     """jx_paged_attention8: as paged_attention, over caches and scales as qk_norm_rope8 fills them."""
     o, lse, i, a = _attend(q, k_cache, v_cache, table, q_start, kv_len, scale, window, out, _E4M3)
-    _with_work(work, q, i, _lib.jx_paged_attention8_bytes, _lib.jx_paged_attention8, C.byref(a), C.byref(_kv_scales(k_cache, k_scale, v_scale, i)))
+    _with_work(work, q, i, _lib.jx_paged_attention8_bytes, _lib.jx_paged_attention8, a,
+               _kv_scales(k_cache, k_scale, v_scale, i))
     return o, lse
 
 
@@ -577,19 +587,19 @@ def _found(q, keys, values, ids, scale, part, out, of_rows):
     dt, i = q.dtype, _gpu(q)
     of_rows = of_rows or dt
     o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
-    qs, ks = q.stride(), keys.stride()
-    assert kd == d and _alike(keys, values)
-    return o, lse, i, FoundArgs(
-        _HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt), qs[0], qs[1], _rows(keys, i, of_rows), _rows(values, i, of_rows), ks[0], ks[1], n,
-        _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else None,
-        _real(part[1], i, _F32, t, h) if part else None, p_out, p_lse)
+    qs, ks, vs = q.stride(), keys.stride(), values.stride()
+    assert kd == d and _alike(keys, values, ks, vs)
+    return o, lse, i, _FOUND.pack(
+        _HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt, qs), qs[0], qs[1], _rows(keys, i, of_rows, ks), _rows(values, i, of_rows, vs), ks[0], ks[1], n,
+        _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else 0,
+        _real(part[1], i, _F32, t, h) if part else 0, p_out, p_lse)
 
 
 def found_attention(q, keys, values, ids, scale, part=None, out=None):
     """jx_found_attention: (out, lse) over the rows ids [tokens][heads][k] of keys and values [rows][kv_heads][head_dim] (any
     strides, alike in both), joined with part = (out, lse) of other keys if given.  `out`: two tensors to write into (may be `part`)."""
     o, lse, i, a = _found(q, keys, values, ids, scale, part, out, None)
-    _run(_lib.jx_found_attention, i, C.byref(a))
+    _run(_lib.jx_found_attention, i, a)
     return o, lse
 
 
@@ -600,8 +610,7 @@ def found_attention8(q, keys, values, k_scale, v_scale, ids, scale, block, part=
     n, kv, _ = keys.shape
     assert block >= 1, block
     blocks = -(-n // block)
-    sc = KvScales(_real(k_scale, i, _E8M0, blocks, kv), _real(v_scale, i, _E8M0, blocks, kv), block)
-    _run(_lib.jx_found_attention8, i, C.byref(a), C.byref(sc))
+    _run(_lib.jx_found_attention8, i, a, _SCALES.pack(_real(k_scale, i, _E8M0, blocks, kv), _real(v_scale, i, _E8M0, blocks, kv), block))
     return o, lse
 
 

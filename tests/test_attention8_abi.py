@@ -175,3 +175,18 @@ def test_scales_that_do_not_belong_to_the_cache(noted):  # noqa: F811
     with pytest.raises(AssertionError):
         run(jx, t)
     assert not lib.made
+
+
+def test_records_are_packed_as_they_are_declared(jx):  # noqa: F811
+    def fields(cls, at=0):
+        for name, kind in cls._fields_:
+            off = at + getattr(cls, name).offset
+            if issubclass(kind, C.Structure):
+                yield from fields(kind, off)
+            else:
+                yield kind, off
+
+    for packed, cls in ((jx._ROPE, jx.RopeArgs), (jx._ATTEND, jx.AttendArgs), (jx._FOUND, jx.FoundArgs), (jx._SCALES, jx.KvScales)):
+        want = list(fields(cls))
+        record = packed.pack(*[float(n + 1) if kind is C.c_float else n + 1 for n, (kind, _) in enumerate(want)])
+        assert [kind.from_buffer_copy(record, off).value for kind, off in want] == list(range(1, len(want) + 1)), cls
