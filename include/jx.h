@@ -582,7 +582,7 @@ typedef struct {
  * not a number and take no part in E.
  * Rows of one block follow one another, in the order of their slots, as jx_kv_plan
  * gives them; rows that are not stored stand elsewhere.
- * n_tokens * n_kv_heads * 512 + n_tokens * n_heads * 32 < 2^32 is enough.
+ * n_tokens * (n_kv_heads * 256 + n_heads * 32) < 2^32 is enough.
  */
 int jx_qk_norm_rope8(const jx_rope_args* args, const jx_kv_scales* scales, void* stream);
 

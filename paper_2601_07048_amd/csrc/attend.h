@@ -42,19 +42,22 @@ inline int64_t rope_threads(const jx_rope_args& a) {
     const int64_t rows = a.n_heads + 2ll * a.n_kv_heads;
     return (a.n_tokens * (rope_many(a) ? (rows + 3) / 4 : rows) * row_lanes(a.head_dim) + 255) / 256 * 256;
 }
-// Into a cache of 8 bits: 256 / lanes of a row heads, or four times as many, for each workgroup of the queries; a workgroup for each
-// key head's keys or values of `rows` tokens
+// Into a cache of 8 bits: workgroups for keys and values, then those for the queries.  A team of lanes takes a key head's keys and values of the
+// rows in one block, as many runs of them as begin among `rows` rows: one where there are no more than the card holds wavefronts a few
+// times, and where a wavefront has several teams
 struct Rope8Grid {
-    int q_rows, rows;
+    int q_rows, rows, team, apart;  // apart: the queries in a launch of their own
     int64_t q_blocks, kv_blocks;
 };
 inline Rope8Grid rope8_grid(const jx_rope_args& a, int block) {
     Rope8Grid g;
-    const int lpr = row_lanes(a.head_dim);
+    const int lpr = row_lanes(a.head_dim), lanes = lpr * block;
     g.q_rows = a.n_tokens * a.n_heads * lpr > 256 * 2048 ? 4 : 1;
+    g.apart = a.n_tokens * a.n_heads * lpr > 4 * 256 * 2048;
     g.q_blocks = (a.n_tokens * ((a.n_heads + g.q_rows - 1) / g.q_rows) * lpr + 255) / 256;
-    g.rows = a.n_tokens * 2 * a.n_kv_heads <= 16384 ? 1 : block;
-    g.kv_blocks = (a.n_tokens + g.rows - 1) / g.rows * 2 * a.n_kv_heads;
+    g.team = lanes <= 64 ? lanes : lanes <= 256 ? 64 : 256;
+    g.rows = g.team < 64 || a.n_tokens * a.n_kv_heads * (g.team / 64) <= 32768 ? 1 : block < 64 ? block : 32;
+    g.kv_blocks = ((a.n_tokens + g.rows - 1) / g.rows * a.n_kv_heads * g.team + 255) / 256;
     return g;
 }
 inline int64_t found_threads(const jx_found_args& a) { return (a.n_tokens * a.n_heads + 3) / 4 * 256; }

@@ -1375,7 +1375,7 @@ int jx_qk_norm_rope8(const jx_rope_args* a, const jx_kv_scales* scales, void* st
     if (int rc = check_cache(a->cache, a->n_kv_heads, 16)) return rc;
     if (int rc = check_scales(scales, a->head_dim, std::min(64, a->cache.page))) return rc;
     const jx::Rope8Grid n = jx::rope8_grid(*a, scales->block);
-    if (n.q_blocks + n.kv_blocks >= 1 << 24) return fail(JX_EINVAL, "n_tokens out of range: 2^32 threads and more");
+    if (n.q_blocks >= 1 << 24 || n.kv_blocks >= 1 << 24 || (!n.apart && n.q_blocks + n.kv_blocks >= 1 << 24)) return fail(JX_EINVAL, "n_tokens out of range: 2^32 threads and more");
     if (a->n_tokens == 0) return JX_OK;
     if (int rc = check_rope_rows(a)) return rc;
     if (int rc = check_scales_there(scales)) return rc;

@@ -1,5 +1,6 @@
 // Queries and keys of a step made ready for attention over a cache of 8 bits: RMS norm per head, rotation by position, keys and
 // values put into their blocks as e4m3 beside one power of two for each block and key head.
+#include "attend_walk.h"
 #include "codes8.h"
 #include "rope_row.h"
 
@@ -11,27 +12,27 @@ namespace {
 // E = the largest exponent among the new |y|, the scale is 2^(E - 7), or what the block has if that is more and the block has tokens
 // in front of the new ones; codes are y / scale, rounded once.  So the largest code is 128 up to 256: e4m3 has as many digits at any power of two, and
 // what a block holds moves to a larger scale by its exponents alone, but for numbers under 2^-6 of the scale.
-// Bound: bytes for many tokens, the chain slot - row - largest - store for few.  A workgroup takes a run of rows of one block, one
-// head, keys or values: LPR lanes a row as for the queries, rows held in registers from their one read to their store, the largest
-// through LDS.
+// Bound: bytes for many tokens, the chain slot - row - largest - store for few.  A team takes the rows of one block, one head, keys or
+// values: LPR lanes a row as for the queries, rows held in registers from their one read to their store.  A team is as many lanes as
+// the block has rows for, up to a wavefront (with four rows a lane), and a workgroup for larger blocks, whose largest value goes through LDS.
+// With very many tokens the queries are a launch of their own, which has more wavefronts resident than these have registers for.
 struct Args {
     jx_rope_args a;
     uint8_t *k_scale, *v_scale;
     int page_shift, block_shift;
-    unsigned q_blocks;  // workgroups for the queries
-    int rows;           // rows of a workgroup for keys and values: it takes the runs that begin there
+    Rope8Grid n;
 };
 
 template <typename T>
 constexpr float LARGEST = __is_same(T, _Float16) ? 0x1.ep15f : 0x1.ep127f;  // the largest code times the largest scale that the type holds
 
 template <typename T, int LPR, int ROWS>
-__device__ __forceinline__ void queries(const Args& g) {
+__device__ __forceinline__ void queries(const Args& g, uint32_t block) {
     typedef typename Vec<T>::x8 X8;
     const jx_rope_args& a = g.a;
     const int c = threadIdx.x % LPR, c8 = c * 8;
     const int groups = (a.n_heads + ROWS - 1) / ROWS;
-    const uint32_t i = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, t = i / groups;
+    const uint32_t i = block * (256 / LPR) + threadIdx.x / LPR, t = i / groups;
     if (t >= a.n_tokens) return;  // whole groups of LPR lanes
     const int row0 = (int)(i - t * groups) * ROWS;
     const bool inside = c8 < a.head_dim;
@@ -49,123 +50,212 @@ __device__ __forceinline__ void queries(const Args& g) {
     }
 }
 
-// ITER: rows of a block / rows that the workgroup holds at a time
-template <typename T, int LPR, int ITER>
-__device__ __forceinline__ void keys_values(const Args& g, float* red) {
+constexpr uint32_t INFINITE = 0x7F800000u;
+template <typename T>
+constexpr uint32_t MOST_BYTE = __is_same(T, _Float16) ? 127 + 15 - 7 : 127 + 127 - 7;
+
+// The largest |x| of eight elements, as bits: those of numbers are in order, and what is none is at least INFINITE
+__device__ __forceinline__ uint32_t largest_bits(f32x8 x) {
+    uint32_t m = 0;
+    for (int j = 0; j < 8; j++) m = max(m, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    return m;
+}
+__device__ __forceinline__ uint32_t largest_number(f32x8 x) {
+    uint32_t m = 0;
+    for (int j = 0; j < 8; j++) {
+        const uint32_t y = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+        m = y < INFINITE ? max(m, y) : m;
+    }
+    return m;
+}
+
+// The scale's byte, from the largest of a block's new rows and what the block has
+template <typename T>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most, uint32_t old) {
+    return max(min(max((int)(most >> 23) - 7, 1), (int)MOST_BYTE<T>), (int)old);
+}
+
+// held: whether values over LARGEST are possible, which would be rounded up to what the type does not have
+template <typename T>
+__device__ __forceinline__ uint2 encode(f32x8 x, float scale, bool held) {
+    if (held)
+        for (int j = 0; j < 8; j++) x[j] = fabsf(x[j]) < INFINITY ? fminf(fmaxf(x[j], -LARGEST<T>), LARGEST<T>) : x[j];
+    return make_uint2(codes_of(x[0], x[1], x[2], x[3], scale), codes_of(x[4], x[5], x[6], x[7], scale));
+}
+
+// ITER: rows of a block / rows that the team holds at a time
+template <typename T, int LPR, int ITER, bool WIDE>
+__device__ __forceinline__ void keys_values(const Args& g, uint32_t (&red)[2][4]) {
     typedef typename Vec<T>::x8 X8;
-    constexpr int AT_ONCE = 256 / LPR;
     const jx_rope_args& a = g.a;
-    const int tid = threadIdx.x, lane = lane_id(), c = tid % LPR, c8 = c * 8, mine = tid / LPR;
-    const uint32_t i = blockIdx.x - g.q_blocks, roles = 2 * a.n_kv_heads;
-    const int64_t t0 = (int64_t)(i / roles) * g.rows;
-    const int role = (int)(i % roles), head = role >> 1, block = 1 << g.block_shift;
-    const bool key = (role & 1) == 0, inside = c8 < a.head_dim;
-    const int64_t token_stride = key ? a.k_token_stride : a.v_token_stride;
-    const T* from = (const T*)(key ? a.d_k : a.d_v) + head * (key ? a.k_head_stride : a.v_head_stride) + c8;
-    uint8_t* cache = (uint8_t*)(key ? a.cache.d_k : a.cache.d_v) + head * a.cache.head_stride;
-    // the block of a row, -1 where it is not stored; the slots of a cache are below 2^43
-    auto block_of = [&](int64_t t) -> int64_t {
-        if (t < 0 || t >= a.n_tokens) return -1;
-        const int64_t slot = a.d_slot[t];
-        const bool stored = (uint32_t)a.d_pos[t] < (uint32_t)a.n_pos && slot >= 0 && (slot >> g.page_shift) < a.cache.n_pages;
-        return stored ? slot >> g.block_shift : -1;
+    const int tid = threadIdx.x, lane = lane_id(), team = WIDE ? 256 : g.n.team, at_once = team / LPR;
+    const int in_team = tid & (team - 1), c = in_team % LPR, c8 = c * 8, mine = in_team / LPR;
+    const uint32_t i = (blockIdx.x * 256 + tid) / team, window = i / a.n_kv_heads;
+    const int64_t t0 = (int64_t)window * g.n.rows;
+    if (t0 >= a.n_tokens) return;  // whole teams
+    const int head = (int)(i - window * a.n_kv_heads), block = 1 << g.block_shift;
+    const bool inside = c8 < a.head_dim;
+    // the slot of a row, -1 where it is not stored, and its position; no branch, so that reads of several rows are on their way together
+    struct At {
+        int64_t slot;
+        int pos;
     };
-    const int64_t own = lane < g.rows ? block_of(t0 + lane) : -1, before = lane < g.rows ? block_of(t0 + lane - 1) : -1;
-    for (uint64_t begins = ballot(own >= 0 && own != before); begins; begins &= begins - 1) {
-        const int64_t t = t0 + __builtin_ctzll(begins);
-        const int64_t slot = a.d_slot[t], b = slot >> g.block_shift;
-        const uint64_t others = ~ballot(lane < block && block_of(t + lane) == b);
-        const int count = others ? __builtin_ctzll(others) : 64;  // rows of the run, at most those of a block
-        const int first = (int)(slot & (block - 1));
-        uint8_t* scale = (key ? g.k_scale : g.v_scale) + b * a.n_kv_heads + head;
-        const uint32_t old = first ? *scale : 0;
-        auto place = [&](int64_t s) { return (s >> g.page_shift) * a.cache.page_stride + (s & (a.cache.page - 1)) * a.cache.token_stride + c8; };
+    auto row_at = [&](int64_t t) {
+        const int64_t i = min(max(t, (int64_t)0), a.n_tokens - 1), slot = a.d_slot[i];
+        const int pos = a.d_pos[i];
+        const bool stored = t == i && (uint32_t)pos < (uint32_t)a.n_pos && slot >= 0 && (slot >> g.page_shift) < a.cache.n_pages;
+        return At{stored ? slot : -1, stored ? pos : 0};
+    };
+    auto block_of = [&](int64_t slot) { return slot >> g.block_shift; };  // of -1: -1
+
+    // The run that begins with row t in slot `slot`; rows: the team's, from t on
+    auto store = [&](int64_t t, int64_t slot, const At (&rows)[ITER]) {
+        const int64_t b = block_of(slot), at = b * a.n_kv_heads + head;
+        const int first = (int)(slot & (block - 1)), begin = (int)(slot & (a.cache.page - 1)) - first;  // of the block in its page
+        const int64_t to = (slot >> g.page_shift) * a.cache.page_stride + begin * a.cache.token_stride + head * a.cache.head_stride;  // the block's first
+        const uint32_t old_k = first ? g.k_scale[at] : 0, old_v = first ? g.v_scale[at] : 0;
+        const T* from_k = (const T*)a.d_k + t * a.k_token_stride + head * a.k_head_stride;
+        const T* from_v = (const T*)a.d_v + t * a.v_token_stride + head * a.v_head_stride;
+        uint8_t *to_k = (uint8_t*)a.cache.d_k + to, *to_v = (uint8_t*)a.cache.d_v + to;
+        X8 k[ITER], v[ITER];
+        int places[ITER];  // in the block; -1: not a row of this run, or not a part of one
+#pragma unroll
+        for (int r = 0; r < ITER; r++) {
+            const int row = r * at_once + mine;
+            const bool there = row < block && block_of(rows[r].slot) == b;
+            places[r] = there && inside ? (int)rows[r].slot & (block - 1) : -1;
+            k[r] = v[r] = (X8)(T)0.0f;
+            if (places[r] >= 0) {
+                k[r] = *(const X8*)(from_k + row * a.k_token_stride + c8);
+                v[r] = *(const X8*)(from_v + row * a.v_token_stride + c8);
+            }
+        }
+        // the angles of two rows are asked for with them: those of more have no registers
+        constexpr int EARLY = ITER <= 2 ? ITER : 0;
+        Angles angles[EARLY ? EARLY : 1];
+#pragma unroll
+        for (int r = 0; r < EARLY; r++) angles[r] = angles_at(a, rows[r].pos, places[r] >= 0, c);
         f32x8 x[ITER];
-        float most = 0.0f;
+        uint32_t most_k = 0, most_v = 0;
 #pragma unroll
         for (int r = 0; r < ITER; r++) {
-            const int row = r * AT_ONCE + mine;
-            const bool there = row < count;
-            X8 raw = there && inside ? *(const X8*)(from + (t + row) * token_stride) : (X8)(T)0.0f;
-            x[r] = __builtin_convertvector(raw, f32x8);
-            if (key) x[r] = norm_and_turn<T, LPR>(a, x[r], (const T*)a.d_k_weight, inside, c8, angles_at(a, there ? a.d_pos[t + row] : 0, there, c));
-            for (int j = 0; j < 8; j++) {
-                const float y = fabsf(x[r][j]);
-                if (y < INFINITY) {  // not what is not a number
-                    x[r][j] = fminf(fmaxf(x[r][j], -LARGEST<T>), LARGEST<T>);
-                    most = fmaxf(most, fminf(y, LARGEST<T>));
-                }
+            x[r] = (f32x8)0.0f;
+            if (!ballot(places[r] >= 0)) continue;
+            const Angles turn = EARLY ? angles[EARLY ? r : 0] : angles_at(a, rows[r].pos, places[r] >= 0, c);
+            x[r] = norm_and_turn<T, LPR>(a, __builtin_convertvector(k[r], f32x8), (const T*)a.d_k_weight, inside, c8, turn);
+            const f32x8 y = __builtin_convertvector(v[r], f32x8);
+            uint32_t m_k = largest_bits(x[r]), m_v = largest_bits(y);
+            if (ballot(max(m_k, m_v) >= INFINITE)) {
+                m_k = largest_number(x[r]);
+                m_v = largest_number(y);
             }
+            most_k = max(most_k, m_k);
+            most_v = max(most_v, m_v);
         }
-        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d, 64));
-        if (lane == 0) red[tid >> 6] = most;
-        __syncthreads();
-        most = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        const uint32_t byte = max(max((int)(__float_as_uint(most) >> 23) - 7, 1), (int)old);
-        const float to = scale_bits(byte);
+        for (int d = 1; d < min(team, 64); d *= 2) {
+            most_k = max(most_k, (uint32_t)__shfl_xor((int)most_k, d, 64));
+            most_v = max(most_v, (uint32_t)__shfl_xor((int)most_v, d, 64));
+        }
+        if (WIDE) {
+            if (lane == 0) {
+                red[0][tid >> 6] = most_k;
+                red[1][tid >> 6] = most_v;
+            }
+            __syncthreads();
+            most_k = max(max(red[0][0], red[0][1]), max(red[0][2], red[0][3]));
+            most_v = max(max(red[1][0], red[1][1]), max(red[1][2], red[1][3]));
+        }
+        const uint32_t byte_k = scale_byte<T>(most_k, old_k), byte_v = scale_byte<T>(most_v, old_v);
+        const bool held = ballot(max(byte_k, byte_v) >= MOST_BYTE<T>) != 0;
 #pragma unroll
-        for (int r = 0; r < ITER; r++) {
-            const int row = r * AT_ONCE + mine;
-            if (row < count && inside) {
-                const int64_t s = a.d_slot[t + row];
-                const uint2 w = make_uint2(codes_of(x[r][0], x[r][1], x[r][2], x[r][3], to), codes_of(x[r][4], x[r][5], x[r][6], x[r][7], to));
-                *(uint2*)(cache + place(s)) = w;
+        for (int r = 0; r < ITER; r++)
+            if (places[r] >= 0) {
+                const int64_t row = places[r] * a.cache.token_stride + c8;
+                *(uint2*)(to_k + row) = encode<T>(x[r], scale_bits(byte_k), held);
+                *(uint2*)(to_v + row) = encode<T>(__builtin_convertvector(v[r], f32x8), scale_bits(byte_v), held);
             }
-        }
-        if (first && byte != old) {
-            const int64_t s0 = slot - first;
-            for (int row = mine; row < first; row += AT_ONCE)
-                if (inside) {
-                    uint2* p = (uint2*)(cache + place(s0 + row));
+        auto move = [&](uint8_t* cache, uint32_t from, uint32_t to) {
+            if (first && from != to && inside)
+                for (int row = mine; row < first; row += at_once) {
+                    uint2* p = (uint2*)(cache + row * a.cache.token_stride + c8);
                     const uint2 w = *p;
-                    *p = make_uint2(codes_moved(w.x, scale_bits(old), to), codes_moved(w.y, scale_bits(old), to));
+                    *p = make_uint2(codes_moved(w.x, scale_bits(from), scale_bits(to)), codes_moved(w.y, scale_bits(from), scale_bits(to)));
                 }
+        };
+        move(to_k, old_k, byte_k);
+        move(to_v, old_v, byte_v);
+        if (WIDE) __syncthreads();  // every wavefront has read the old scales and red
+        if (in_team == 0) {
+            g.k_scale[at] = (uint8_t)byte_k;
+            g.v_scale[at] = (uint8_t)byte_v;
         }
-        __syncthreads();  // every wavefront has read the old scale and red
-        if (tid == 0) *scale = (uint8_t)byte;
+    };
+    At rows[ITER];
+    if (g.n.rows == 1) {
+        const int64_t slot = row_at(t0).slot, before = row_at(t0 - 1).slot;
+#pragma unroll
+        for (int r = 0; r < ITER; r++) rows[r] = row_at(t0 + r * at_once + mine);
+        if (slot >= 0 && block_of(before) != block_of(slot)) store(t0, slot, rows);
+        return;
+    }
+    // a team of 64 lanes or more: the runs that begin among `rows` rows, of up to 32 rows each
+    const At at = row_at(t0 + lane);
+    const int64_t before = row_at(t0 + lane - 1).slot;
+    for (uint64_t begins = ballot(lane < g.n.rows && at.slot >= 0 && block_of(before) != block_of(at.slot)); begins; begins &= begins - 1) {
+        const int j = __builtin_ctzll(begins);
+#pragma unroll
+        for (int r = 0; r < ITER; r++) {
+            const int from = j + r * at_once + mine;
+            rows[r] = block <= 32 ? At{shfl64(at.slot, from), __shfl(at.pos, from, 64)} : row_at(t0 + from);
+        }
+        store(t0 + j, (int64_t)readlane64((uint64_t)at.slot, j), rows);
     }
 }
 
-template <typename T, int LPR, int ROWS, int ITER>
+template <typename T, int LPR, int ITER, bool WIDE>
 __global__ __launch_bounds__(256) void qk_norm_rope8_kernel(Args g) {
-    __shared__ float red[4];
-    if (blockIdx.x < g.q_blocks) queries<T, LPR, ROWS>(g);
-    else keys_values<T, LPR, ITER>(g, red);
+    __shared__ uint32_t red[2][4];
+    if (blockIdx.x < g.n.kv_blocks) keys_values<T, LPR, ITER, WIDE>(g, red);
+    else if (g.n.q_rows == 4) queries<T, LPR, 4>(g, blockIdx.x - (uint32_t)g.n.kv_blocks);
+    else queries<T, LPR, 1>(g, blockIdx.x - (uint32_t)g.n.kv_blocks);
 }
 
-template <typename T, int LPR, int ITER>
-hipError_t launch(const Args& g, bool many, unsigned blocks, hipStream_t st) {
-    if (many) qk_norm_rope8_kernel<T, LPR, 4, ITER><<<blocks, 256, 0, st>>>(g);
-    else qk_norm_rope8_kernel<T, LPR, 1, ITER><<<blocks, 256, 0, st>>>(g);
+template <typename T, int LPR, int ITER, bool WIDE>
+hipError_t launch(const Args& g, hipStream_t st) {
+    qk_norm_rope8_kernel<T, LPR, ITER, WIDE><<<(unsigned)(g.n.kv_blocks + (g.n.apart ? 0 : g.n.q_blocks)), 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
 template <typename T, int LPR>
-hipError_t launch_block(const Args& g, bool many, unsigned blocks, hipStream_t st) {
-    const int iter = ((1 << g.block_shift) * LPR + 255) / 256;
-    if (iter <= 1) return launch<T, LPR, 1>(g, many, blocks, st);
-    if (iter == 2) return launch<T, LPR, 2>(g, many, blocks, st);
+hipError_t launch_block(const Args& g, hipStream_t st) {
+    const int lanes = LPR << g.block_shift;
+    if (lanes <= 64) return launch<T, LPR, 1, false>(g, st);
+    if (lanes == 128) return launch<T, LPR, 2, false>(g, st);
+    if (lanes == 256) return launch<T, LPR, 4, false>(g, st);
+    if (lanes == 512) return launch<T, LPR, 2, true>(g, st);
     if constexpr (LPR >= 16)
-        if (iter == 4) return launch<T, LPR, 4>(g, many, blocks, st);
-    if constexpr (LPR == 32) return launch<T, LPR, 8>(g, many, blocks, st);
+        if (lanes == 1024) return launch<T, LPR, 4, true>(g, st);
+    if constexpr (LPR == 32) return launch<T, LPR, 8, true>(g, st);
     return hipErrorInvalidValue;
 }
 
 template <typename T>
-hipError_t launch_dim(const Args& g, bool many, unsigned blocks, hipStream_t st) {
+hipError_t launch_dim(const Args& g, hipStream_t st) {
     const int lpr = row_lanes(g.a.head_dim);
-    return lpr == 8    ? launch_block<T, 8>(g, many, blocks, st)
-           : lpr == 16 ? launch_block<T, 16>(g, many, blocks, st)
-                       : launch_block<T, 32>(g, many, blocks, st);
+    return lpr == 8 ? launch_block<T, 8>(g, st) : lpr == 16 ? launch_block<T, 16>(g, st) : launch_block<T, 32>(g, st);
 }
 
 }  // namespace
 
 hipError_t launch_qk_norm_rope8(const jx_rope_args& a, const jx_kv_scales& s, hipStream_t st) {
     const Rope8Grid n = rope8_grid(a, s.block);
-    const Args g = {a, s.d_k, s.d_v, log2_of(a.cache.page), log2_of(s.block), (unsigned)n.q_blocks, n.rows};
-    const unsigned blocks = (unsigned)(n.q_blocks + n.kv_blocks);
-    return a.dtype == JX_BF16 ? launch_dim<__bf16>(g, n.q_rows == 4, blocks, st) : launch_dim<_Float16>(g, n.q_rows == 4, blocks, st);
+    if (n.apart) {
+        jx_rope_args queries = a;
+        queries.n_kv_heads = 0;
+        if (hipError_t e = launch_qk_norm_rope(queries, st); e != hipSuccess) return e;
+    }
+    const Args g = {a, s.d_k, s.d_v, log2_of(a.cache.page), log2_of(s.block), n};
+    return a.dtype == JX_BF16 ? launch_dim<__bf16>(g, st) : launch_dim<_Float16>(g, st);
 }
 
 }  // namespace jx
