@@ -282,7 +282,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
                     // what is not there has come as zeros, whose scale has to be a number
                     const bool gone = !all && (row >= left || !there(i * 2 / VC ? here.id[1] : here.id[0]));
                     const float scale = scale_bits((uint32_t)__shfl((int)bytes, 32 + row, 64));
-                    put_codes<T, CH>(y8[i], gone ? 1.0f : scale, v, row, lane % CHM);
+                    for (int y = 0; y < 2; y++) put_codes<T, CH>(y8[i][2 * y], y8[i][2 * y + 1], gone ? 1.0f : scale, v, row, lane % CHM * 2 + y);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (more) load_codes(key + KEYS, next);

@@ -101,8 +101,10 @@ struct Rows32 {
 
     // One tile's scores to weights while the next one's scores are formed, then the weighted values, while the next scores' largest
     // is looked for: matrix and vector instructions alternate, reads of LDS run AHEAD matrix instructions before their use.
-    // What stands between two fences is not moved over them.
-    __device__ __forceinline__ void advance(const f32x16 (&s)[2], f32x16 (&next)[2], lds_ptr k, lds_ptr v, float c) {
+    // What stands between two fences is not moved over them.  between: done between the two halves, beside: beside each matrix instruction
+    // of the second half, which has few vector instructions of its own.
+    template <typename Between, typename Beside>
+    __device__ __forceinline__ void advance(const f32x16 (&s)[2], f32x16 (&next)[2], lds_ptr k, lds_ptr v, float c, Between between, Beside beside) {
         constexpr int N = 4 * NB, AHEAD = 3;  // matrix instructions of each half, with 32 / N scores each
         const float base = m == -INFINITY ? 0.0f : m;
         s16x8 kf[AHEAD], vf[AHEAD], p[4];
@@ -128,10 +130,12 @@ struct Rows32 {
         }
         l += sum;
         top = -INFINITY;
+        between();
 #pragma unroll
         for (int i = 0; i < N; i++) {
             o[i % NB] = Mfma<T>::mul(vf[i % AHEAD], p[i / NB], o[i % NB]);
             if (i + AHEAD < N) vf[i % AHEAD] = values_at(v, i + AHEAD);
+            beside(i);
 #pragma unroll
             for (int e = i * 32 / N; e < (i + 1) * 32 / N; e++)
                 if (e & 1) top = fmaxf(fmaxf(top, next[e >> 4][(e & 15) - 1]), next[e >> 4][e & 15]);
@@ -155,7 +159,9 @@ template <typename T, typename C, int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel(PagedArgs g) {
     typedef Rows32<T, NB> R;
     constexpr int ROWS = WAVES * 32, THREADS = WAVES * 64, KEYS = UNIT, TILE = KEYS * R::PITCH;
-    constexpr int CHM = R::CH * (int)sizeof(C) / 2, LOADS = KEYS * CHM < THREADS ? 1 : KEYS * CHM / THREADS;  // chunks of a row in memory
+    constexpr int CHM = R::CH * (int)sizeof(C) / 2;     // chunks of a row in memory
+    constexpr bool HALVES = KEYS * CHM < THREADS;        // one half of the wavefronts takes keys, the other values
+    constexpr int LOADS = HALVES ? 1 : KEYS * CHM / THREADS, ARRIVALS = HALVES ? 1 : 2 * LOADS;
     extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2] keys, [2] values; slots' sums of units, their requests
     const jx_attend_args& a = g.a;
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -218,13 +224,24 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
         // wavefront are neighbours in a page, if that has as many: their place is then a matter of scalar instructions.  Codes arrive in
         // the place of the rows that their wavefront will make of them; see `expand`.
         const uint32_t lane_row = lane / CHM * token_chunks * 16, lane_chunk = CODED<C> ? lane % CHM : lane % R::CH ^ mix<R::CH>(tid / R::CH);
+        // Of codes, places are worked out from the lane again each time: over the loop there are no registers for them.
+        auto fresh_lane = [&] {
+            int l = lane;
+            asm volatile("" : "+v"(l));
+            return l;
+        };
+        const int turn = HALVES ? wave & (WAVES / 2 - 1) : wave;  // which of a load's rows
+        const bool takes_k = !HALVES || wave < WAVES / 2, takes_v = !HALVES || wave >= WAVES / 2;
         auto stage = [&](const char* from, int key, int ids, lds_ptr to) {
             if (g.near && !ballot(ids < 0)) {
                 for (int i = 0; i < LOADS; i++) {
-                    const int at = i * (THREADS / CHM) + wave * (64 / CHM), odd = CODED<C> ? 0 : mix<R::CH>(i * (THREADS / CHM) & 15);
-                    if (KEYS * CHM < THREADS && at >= KEYS) return;
+                    const int at = i * (THREADS / CHM) + turn * (64 / CHM), odd = CODED<C> ? 0 : mix<R::CH>(i * (THREADS / CHM) & 15);
                     const uint64_t row = row_at(__builtin_amdgcn_readlane(ids, at), key + at);
-                    const uint32_t off = lane_row + (lane_chunk ^ odd) * 16;
+                    uint32_t off = lane_row + (lane_chunk ^ odd) * 16;
+                    if constexpr (CODED<C>) {
+                        const int l = fresh_lane();
+                        off = ((uint32_t)(l / CHM) * token_chunks + l % CHM) * 16;
+                    }
                     if (d == R::CH * 8) load_lds16(from + row * 16 + off, to + at * R::PITCH);
                     else if ((int)(lane_chunk ^ odd) * 16 < d * (int)sizeof(C))  // the other places are never written: see above
                         load_lds16(from + row * 16 + off, to + at * R::PITCH);
@@ -234,11 +251,10 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
             const uint64_t rows = row_at(max(ids, 0), key + lane);
 #pragma unroll 1
             for (int i = 0; i < LOADS; i++) {
-                const int at = i * (THREADS / CHM) + tid / CHM, chunk = CODED<C> ? tid % CHM : tid % R::CH ^ mix<R::CH>(at);
-                if (KEYS * CHM < THREADS && at >= KEYS) return;
+                const int at = i * (THREADS / CHM) + turn * (64 / CHM) + lane / CHM, chunk = CODED<C> ? tid % CHM : tid % R::CH ^ mix<R::CH>(at);
                 const char* p = from + ((uint64_t)shfl64((long long)rows, at) + chunk) * 16;
                 load_lds16(__shfl(ids, at, 64) >= 0 && chunk * 16 < d * (int)sizeof(C) ? p : (const char*)zero_chunk,
-                           to + (i * (THREADS / CHM) + wave * (64 / CHM)) * R::PITCH);
+                           to + (i * (THREADS / CHM) + turn * (64 / CHM)) * R::PITCH);
             }
         };
         // Lane i's block among the scales, of a key whose page is `id`
@@ -247,31 +263,68 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
         };
         // Codes that have arrived, as elements: a wavefront's rows are its own, and it has read all of a load's codes before it writes.  `byte`:
         // lane i has the scale of the i-th row.  What is not there arrives as zeros, whose scale has to be a number.
+        auto raw = [&](int l, int i, lds_ptr to) {
+            const u32x4 w = *(const __attribute__((address_space(3))) u32x4*)(to + (i * (THREADS / CHM) + turn * (64 / CHM)) * R::PITCH + l * 16);
+            return l % CHM * 16 < d ? w : (u32x4)0u;
+        };
+        auto scale = [&](int l, int i, uint32_t byte, int ids) {
+            return scale_bits((uint32_t)__shfl((int)(ids < 0 ? 127 : byte), i * (THREADS / CHM) + turn * (64 / CHM) + l / CHM, 64));
+        };
+        auto put = [&](int l, int i, int half, u32x4 w, float scale, lds_ptr to) {
+            put_codes<T, R::CH>(w[2 * half], w[2 * half + 1], scale, to, i * (THREADS / CHM) + turn * (64 / CHM) + l / CHM, l % CHM * 2 + half);
+        };
         auto expand = [&](uint32_t byte, int ids, lds_ptr to) {
-            const uint32_t known = ids < 0 ? 127 : byte;
-#pragma unroll
+            const int l = fresh_lane();
             for (int i = 0; i < LOADS; i++) {
-                const int at0 = i * (THREADS / CHM) + wave * (64 / CHM), at = at0 + lane / CHM;
-                if (KEYS * CHM < THREADS && at0 >= KEYS) return;
-                u32x4 w = *(const __attribute__((address_space(3))) u32x4*)(to + at0 * R::PITCH + lane * 16);
-                if ((int)lane_chunk * 16 >= d) w = (u32x4)0u;
-                put_codes<T, R::CH>(w, scale_bits((uint32_t)__shfl((int)known, at, 64)), to, at, lane_chunk);
+                const u32x4 w = raw(l, i, to);
+                const float x = scale(l, i, byte, ids);
+                for (int half = 0; half < 2; half++) put(l, i, half, w, x, to);
             }
         };
         auto scale_of = [&](const uint8_t* scales, int key, int ids) -> uint32_t { return CODED<C> ? scales[scale_at(max(ids, 0), key + lane)] : 0; };
+        // The keys after the next tile's and the next tile's values
+        auto ask = [&](int key, int ids_v, int ids_k, lds_ptr next_k, lds_ptr next_v, uint32_t& k_byte, uint32_t& v_byte) __attribute__((always_inline)) {
+            if (takes_k && key + 2 * KEYS < key1) {
+                stage(kb, key + 2 * KEYS, ids_k, next_k);
+                k_byte = scale_of(g.scales.k, key + 2 * KEYS, ids_k);
+            }
+            if (takes_v && key + KEYS < key1) {
+                stage(vb, key + KEYS, ids_v, next_v);
+                v_byte = scale_of(g.scales.v, key + KEYS, ids_v);
+            }
+        };
         // One tile's weights and values, the next one's scores; the keys after that and the next values on their way into the places that
         // the last step has read.  The compiler has to know that those are apart: it would wait for what is on its way before it reads.
         auto step = [&](int key, uint64_t there, int ids_v, int ids_k, f32x16 (&s)[2], f32x16 (&next)[2], const lds_ptr __restrict k,
                         const lds_ptr __restrict v, const lds_ptr __restrict next_k, const lds_ptr __restrict next_v) __attribute__((always_inline)) {
             uint32_t k_byte = 0, v_byte = 0;
-            if (key + 2 * KEYS < key1) {
-                stage(kb, key + 2 * KEYS, ids_k, next_k);
-                k_byte = scale_of(g.scales.k, key + 2 * KEYS, ids_k);
-            }
-            if (key + KEYS < key1) {
-                stage(vb, key + KEYS, ids_v, next_v);
-                v_byte = scale_of(g.scales.v, key + KEYS, ids_v);
-            }
+            ask(key, ids_v, ids_k, next_k, next_v, k_byte, v_byte);
+            // Of codes: what has arrived becomes elements beside the second half's matrix instructions, two loads at hand.  After the last
+            // keys too, in places that nobody reads any more.
+            constexpr int N = 4 * NB, EVERY = CODED<C> ? N / (2 * ARRIVALS) : N;
+            u32x4 w[2];
+            float x_of[2];
+            int l = 0;
+            auto of_keys = [&](int q) { return HALVES ? takes_k : q < LOADS; };
+            auto arrive = [&](int q) {
+                w[q & 1] = raw(l, q % LOADS, of_keys(q) ? next_k : next_v);
+                x_of[q & 1] = scale(l, q % LOADS, of_keys(q) ? k_byte : v_byte, of_keys(q) ? ids_k : ids_v);
+            };
+            auto between = [&] {
+                if constexpr (CODED<C>) {
+                    __builtin_amdgcn_s_waitcnt(0x0F70);
+                    l = fresh_lane();
+                    for (int q = 0; q < ARRIVALS && q < 2; q++) arrive(q);
+                }
+            };
+            auto beside = [&](int i) {
+                if constexpr (CODED<C>) {
+                    const int q = i / EVERY / 2, half = i / EVERY & 1;
+                    if (i % EVERY != EVERY - 1 || q >= ARRIVALS) return;
+                    put(l, q % LOADS, half, w[q & 1], x_of[q & 1], of_keys(q) ? next_k : next_v);
+                    if (half && q + 2 < ARRIVALS) arrive(q + 2);
+                }
+            };
             if (busy) {
                 const bool all = there == ~0ull && key + KEYS - 1 <= w0 && (!a.window || key > w1 - a.window);
                 if (!all) {
@@ -290,12 +343,7 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
                     odd_values |= odd_values_in<T>(v, TILE);
                 }
                 x.raise(c);
-                x.advance(s, next, k, v, c);  // the scores after the last tile are of no use: what lies there is read all the same
-            }
-            if constexpr (CODED<C>) {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
-                if (key + 2 * KEYS < key1) expand(k_byte, ids_k, next_k);
-                if (key + KEYS < key1) expand(v_byte, ids_v, next_v);
+                x.advance(s, next, k, v, c, between, beside);  // the scores after the last tile are of no use: what lies there is read all the same
             }
         };
         // Keys of tile i lie in half i & 1 of the ring's first part, values in the same half of its second
@@ -304,20 +352,33 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
         int ids = page_of(key0 + lane), ids_1 = page_of(key0 + KEYS + lane);
         if (key0 < key1) {
             const bool more = key0 + KEYS < key1;
-            stage(kb, key0, ids, ring);
-            stage(vb, key0, ids, ring + 2 * TILE);
-            if (more) stage(kb, key0 + KEYS, ids_1, ring + TILE);
+            if (takes_k) stage(kb, key0, ids, ring);
+            if (takes_v) stage(vb, key0, ids, ring + 2 * TILE);
+            if (takes_k && more) stage(kb, key0 + KEYS, ids_1, ring + TILE);
             const uint32_t k_byte = scale_of(g.scales.k, key0, ids), v_byte = scale_of(g.scales.v, key0, ids);
             const uint32_t k_byte_1 = more ? scale_of(g.scales.k, key0 + KEYS, ids_1) : 0;
             __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
             if constexpr (CODED<C>) {
-                expand(k_byte, ids, ring);
-                expand(v_byte, ids, ring + 2 * TILE);
-                if (more) expand(k_byte_1, ids_1, ring + TILE);
+                if (takes_k) expand(k_byte, ids, ring);
+                if (takes_v) expand(v_byte, ids, ring + 2 * TILE);
+                if (takes_k && more) expand(k_byte_1, ids_1, ring + TILE);
             }
             __syncthreads();
             if (busy) x.scores(ring, s0);
         }
+        if (CODED<C> && !busy)  // a loop of its own: what goes on without products beside it costs the other one its registers
+            for (int at = key0, odd = 0; at < key1; at += KEYS, odd ^= 1) {
+                const int ids_2 = page_of(at + 2 * KEYS + lane);
+                const lds_ptr next_k = odd ? ring + TILE : ring, next_v = odd ? ring + 2 * TILE : ring + 3 * TILE;
+                uint32_t k_byte = 0, v_byte = 0;
+                __syncthreads();
+                ask(at, ids_1, ids_2, next_k, next_v, k_byte, v_byte);
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+                if (takes_k) expand(k_byte, ids_2, next_k);
+                if (takes_v) expand(v_byte, ids_1, next_v);
+                ids_1 = ids_2;
+            }
+        else
         for (int key = key0; key < key1; key += 2 * KEYS) {
 #pragma unroll
             for (int odd = 0; odd < 2; odd++) {

@@ -136,13 +136,11 @@ typedef __attribute__((address_space(3))) char* lds_ptr;
 template <typename C>
 constexpr bool CODED = sizeof(C) == 1;
 
-// Sixteen codes of one row, times its scale, into the row's chunks 2 c and 2 c + 1
+// Eight codes of one row, times its scale, as chunk c of the row
 template <typename T, int CH>
-__device__ __forceinline__ void put_codes(u32x4 w, float scale, lds_ptr tile, int row, int c) {
-    typedef __attribute__((address_space(3))) u32x4* out;
-    const int at = row * CH * 16, place = 2 * c ^ mix<CH>(row);
-    *(out)(tile + at + place * 16) = (u32x4){codes_pair<T, false>(w[0], scale), codes_pair<T, true>(w[0], scale), codes_pair<T, false>(w[1], scale), codes_pair<T, true>(w[1], scale)};
-    *(out)(tile + at + (place ^ 1) * 16) = (u32x4){codes_pair<T, false>(w[2], scale), codes_pair<T, true>(w[2], scale), codes_pair<T, false>(w[3], scale), codes_pair<T, true>(w[3], scale)};
+__device__ __forceinline__ void put_codes(uint32_t a, uint32_t b, float scale, lds_ptr tile, int row, int c) {
+    *(__attribute__((address_space(3))) u32x4*)(tile + (row * CH + (c ^ mix<CH>(row))) * 16) =
+        (u32x4){codes_pair<T, false>(a, scale), codes_pair<T, true>(a, scale), codes_pair<T, false>(b, scale), codes_pair<T, true>(b, scale)};
 }
 
 // A query row over keys i0 .. i1 - 1 by a wavefront, LPR lanes a row with eight elements each, q times scale * log2 e; where(i): chunks of 16
