@@ -111,7 +111,11 @@ Plan make_plan(const jx_attend_args& a, bool coded) {
     // are sized for more than the step's requests hold.  128 elements, 8 key heads, 16 requests of up to 256 or 512 keys: 8.9 or 12.7 us, shared out
     // 11.1 or 12.5; 64 requests 18 or 16.  64 elements, 16 key heads, 16 requests of up to 1,024 keys: 10.9, shared out 18.4.
     const int64_t room = (int64_t)a.table_pages * a.cache.page, keys = a.window ? std::min<int64_t>(room, (int64_t)a.window + 16) : room;
-    p.own = p.rows < 128 && (int64_t)p.slots * a.n_kv_heads <= 384 && keys <= 1024 / (nb <= 2 ? 1 : nb);
+    const int64_t tiles = (int64_t)p.slots * a.n_kv_heads, few = 1024 / (nb <= 2 ? 1 : nb);
+    p.own = p.rows < 128 && tiles <= 384 && keys <= few;
+    // Of codes also where there are tiles for most CUs: 8 key heads of 128, single tokens of 250 / 500 / 1,000 keys, a request 10.0 / 11.7 / 14.7 us
+    // (shared out 10.4 / 10.5 / 11.9), 4 requests 10.3 / 12.2 / 15.1 (11.5 / 12.0 / 13.2), 16 requests 10.5 / 12.4 / 16.0 (13.7 / 18.9 / 21.2).
+    if (coded && p.rows < 128 && tiles <= 256) p.own = p.own || keys <= std::min(4 * few, tiles * 64 / nb);
     const double units = ((double)a.table_pages * a.cache.page / (coded ? UNIT / 2 : UNIT) + 1) * p.slots * a.n_kv_heads;  // at most
     // as many shares as the card holds workgroups (many rows) or wavefronts (few) at a time
     if (p.slots && !p.own && p.slots <= MAX_SLOTS && units < 2e9) {

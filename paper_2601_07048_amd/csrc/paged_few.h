@@ -433,7 +433,7 @@ template <typename T, typename C, int NC, int RB>
 hipError_t launch_few(const PagedArgs& g, hipStream_t st) {
     constexpr int WAVES = FEW_WAVES(NC), CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32;
     const size_t lds = WAVES * 2 * 32 * CH * 16 + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
-    hipError_t e = hipFuncSetAttribute((const void*)paged_few_kernel<T, C, NC, RB, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
+    hipError_t e = allow_lds<paged_few_kernel<T, C, NC, RB, WAVES>>(150 * 1024);
     if (e != hipSuccess) return e;
     const unsigned tiles = (unsigned)(g.slots * g.a.n_kv_heads), blocks = g.n_work ? g.groups : g.own ? tiles : (tiles + WAVES - 1) / WAVES;
     paged_few_kernel<T, C, NC, RB, WAVES><<<blocks ? blocks : 256, WAVES * 64, lds, st>>>(g);

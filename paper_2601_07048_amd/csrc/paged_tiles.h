@@ -1,5 +1,6 @@
 // Tiles of a paged attention call: what they are, how they are shared out over workgroups, how rows lie in LDS.
 #pragma once
+#include <atomic>
 #include "attend_walk.h"
 #include "codes8.h"
 
@@ -47,6 +48,19 @@ constexpr int MANY_PER_CU(int nb, int rows) { return nb <= 4 && rows == 128 ? 2 
 
 // blocks of 32 elements that hold a head: those for which there is a kernel
 inline int blocks_of(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 96 ? 3 : head_dim <= 128 ? 4 : head_dim <= 192 ? 6 : 8; }
+
+// Lets a kernel have `bytes` of LDS that its launches ask for, once for each device: the call takes as long as a fifth of a launch
+template <auto Kernel>
+hipError_t allow_lds(int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    if (hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess && device < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 namespace {
 
