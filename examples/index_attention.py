@@ -1,11 +1,14 @@
 """Decoding with a long past in an index.
 
-    python examples/index_attention.py [--past 20000] [--steps 16]
+    python examples/index_attention.py [--past 20000] [--steps 16] [--bits 8]
 
 A request's prompt goes through the paged cache in chunks.  Then its older part moves out: the keys of every key head become
 the vectors of an index (inner products as distances, jx.mips_augment), the values stay in an array, and the pages go back to the
 free ones.  Every further token attends to what is left in the cache and to the rows that a search with each query head finds,
 joined.  What comes out is compared with attention over everything.
+
+With 8 bits the cache and the rows that have left it are e4m3 codes with a power of two for each block of tokens and key head, half the
+memory and half the bytes of a step; whole pages are whole blocks, so that they move as they are.
 
 Projections and prompt are random; each past key is near some direction that queries take up again, as it is with the
 keys that a model goes back to.
@@ -21,17 +24,20 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2601_07048_amd import jx  # noqa: E402
 
-HEADS, KV_HEADS, DIM, PAGE = 8, 2, 64, 16
+HEADS, KV_HEADS, DIM, PAGE, BLOCK = 8, 2, 64, 16, 8
 
 
 class Server:
     """One request: its paged cache, its table of pages and what has moved into an index."""
 
-    def __init__(self, past, room, dtype=torch.bfloat16, seed=0):
+    def __init__(self, past, room, dtype=torch.bfloat16, seed=0, bits=16):
         g = torch.Generator(device="cuda").manual_seed(seed)
-        self.g, self.dtype = g, dtype
+        self.g, self.dtype, self.bits = g, dtype, bits
         pages = -(-(past + room) // PAGE) + 8
-        self.k_cache, self.v_cache = (torch.zeros((pages, PAGE, KV_HEADS, DIM), dtype=dtype, device="cuda") for _ in range(2))
+        self.k_cache, self.v_cache = (torch.zeros((pages, PAGE, KV_HEADS, DIM), dtype=dtype if bits == 16 else torch.float8_e4m3fn, device="cuda")
+                                      for _ in range(2))
+        self.k_scale, self.v_scale = (torch.zeros((pages, PAGE // BLOCK, KV_HEADS), dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+                                      for _ in range(2))
         self.table = torch.full((1, pages), -1, dtype=torch.int32, device="cuda")
         self.free = torch.randperm(pages, generator=g, device="cuda").to(torch.int32)
         self.n_free = torch.tensor([pages], dtype=torch.int32, device="cuda")
@@ -58,8 +64,12 @@ class Server:
         plan = jx.kv_plan(self.len, new, self.table, self.free, self.n_free, PAGE, tokens)
         # kv_len is 0 where there was no room: such a step leaves the request as it was (its results are zeros)
         self.n_free, self.len = plan.n_free, torch.where(plan.kv_len > 0, plan.kv_len, self.len)
-        ready = jx.qk_norm_rope(q, key, value, self.k_cache, self.v_cache, plan.pos, plan.slot, self.cos, self.sin, self.weight, self.weight)
-        part = jx.paged_attention(ready, self.k_cache, self.v_cache, self.table, plan.q_start, plan.kv_len, self.scale)
+        cache = self.k_cache, self.v_cache
+        if self.bits == 8:
+            cache += self.k_scale, self.v_scale
+        store, attend = (jx.qk_norm_rope8, jx.paged_attention8) if self.bits == 8 else (jx.qk_norm_rope, jx.paged_attention)
+        ready = store(q, key, value, *cache, plan.pos, plan.slot, self.cos, self.sin, self.weight, self.weight)
+        part = attend(ready, *cache, self.table, plan.q_start, plan.kv_len, self.scale)
         if not self.moved:
             return (*part, ready, None)
         ids = torch.empty((tokens, HEADS, k), dtype=torch.int32, device="cuda")
@@ -68,19 +78,47 @@ class Server:
             asked = ready[:, c * group:(c + 1) * group].reshape(-1, DIM).float().contiguous()
             found, _ = index.search(jx.mips_augment(asked, is_query=True, dim_out=DIM + 4), k, L)
             ids[:, c * group:(c + 1) * group] = found.view(tokens, group, k)
-        return (*jx.found_attention(ready, self.keys, self.values, ids, self.scale, part=part), ready, ids)
+        if self.bits == 8:
+            out = jx.found_attention8(ready, self.keys, self.values, self.key_scale, self.value_scale, ids, self.scale, BLOCK, part=part)
+        else:
+            out = jx.found_attention(ready, self.keys, self.values, ids, self.scale, part=part)
+        return (*out, ready, ids)
+
+    def held(self, first, end):
+        """What the cache holds in the pages from that of position first to that of end - 1: (keys, values, their scales), in order."""
+        pages = self.table[0, first // PAGE:-(-end // PAGE)].long()
+        bytes_of = lambda x: x.view(torch.uint8)[pages].flatten(0, 1).view(x.dtype)  # noqa: E731
+        if self.bits == 8:
+            return tuple(bytes_of(x) for x in (self.k_cache, self.v_cache, self.k_scale, self.v_scale))
+        return tuple(x[pages].flatten(0, 1) for x in (self.k_cache, self.v_cache))
+
+    def numbers(self, codes, scale):
+        """What rows of whole blocks stand for."""
+        return codes.float() * scale.float().repeat_interleave(BLOCK, 0)[..., None]
 
     def rows(self, first, end):
         """Keys and values of positions first .. end - 1, in order."""
-        pages = self.table[0, first // PAGE:-(-end // PAGE)].long()
-        return tuple(x[pages].flatten(0, 1)[first % PAGE:first % PAGE + end - first].clone() for x in (self.k_cache, self.v_cache))
+        held = self.held(first, end)
+        if self.bits == 8:
+            held = self.numbers(held[0], held[2]), self.numbers(held[1], held[3])
+        return tuple(x[first % PAGE:first % PAGE + end - first].clone() for x in held)
+
+    def past(self):
+        """Keys and values of the positions that have moved."""
+        if self.bits == 8:
+            return self.numbers(self.keys, self.key_scale), self.numbers(self.values, self.value_scale)
+        return self.keys, self.values
 
     def move(self, tokens, R=32, L_build=64):
         """The first `tokens` (whole pages) leave the cache for an index for each key head."""
         assert tokens % PAGE == 0 and not self.moved
-        self.keys, self.values = self.rows(0, tokens)
+        if self.bits == 8:
+            self.keys, self.values, self.key_scale, self.value_scale = self.held(0, tokens)
+        else:
+            self.keys, self.values = self.rows(0, tokens)
+        keys = self.past()[0]
         for c in range(KV_HEADS):
-            x = self.keys[:, c].float().contiguous()
+            x = keys[:, c].float().contiguous()
             longest = float(jx.mips_augment(x, want_norms=True).max())
             index = jx.Index(DIM + 4, jx.F32, R, L_build, 1.2, capacity=tokens, max_batch=tokens)
             index.insert(jx.mips_augment(x, longest * 1.0001, dim_out=DIM + 4))
@@ -95,16 +133,16 @@ def over_all(server, ready):
     n = int(server.len)
     k, v = server.rows(server.moved, n)
     if server.moved:
-        k, v = torch.cat([server.keys, k]), torch.cat([server.values, v])
+        k, v = (torch.cat(x) for x in zip(server.past(), (k, v)))
     q = ready.double().view(-1, KV_HEADS, HEADS // KV_HEADS, DIM)
     s = torch.matmul(q[0], k.double().permute(1, 2, 0).contiguous()) * server.scale
     w = torch.softmax(s, -1)
     return torch.matmul(w, v.double().transpose(0, 1).contiguous()).reshape(1, HEADS, DIM), w.reshape(HEADS, n)
 
 
-def main(past=20000, recent=400, steps=16, k=64, chunk=2048, quiet=False):
+def main(past=20000, recent=400, steps=16, k=64, chunk=2048, quiet=False, bits=16):
     past = past // PAGE * PAGE
-    server = Server(past, recent + steps)
+    server = Server(past, recent + steps, bits=bits)
     done = 0
     while done < past + recent:
         tokens = min(chunk, past + recent - done)
@@ -130,5 +168,6 @@ if __name__ == "__main__":
     ap.add_argument("--past", type=int, default=20000)
     ap.add_argument("--steps", type=int, default=16)
     ap.add_argument("--found", type=int, default=64)
+    ap.add_argument("--bits", type=int, choices=(8, 16), default=16)
     a = ap.parse_args()
-    main(past=a.past, steps=a.steps, k=a.found)
+    main(past=a.past, steps=a.steps, k=a.found, bits=a.bits)
