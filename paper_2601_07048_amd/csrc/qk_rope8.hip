@@ -43,10 +43,13 @@ __device__ __forceinline__ void queries(const Args& g, uint32_t block) {
     for (int r = 0; r < ROWS; r++)
         raw[r] = inside && row0 + r < a.n_heads && placed ? *(const X8*)((const T*)a.d_q + t * a.q_token_stride + (row0 + r) * a.q_head_stride + c8) : (X8)(T)0.0f;
     const Angles angles = angles_at(a, pos, placed, c);
+    f32x8 x[ROWS];
+    for (int r = 0; r < ROWS; r++) x[r] = __builtin_convertvector(raw[r], f32x8);
+    norm_rows<T, LPR, ROWS>(a, x, (const T*)a.d_q_weight, inside, c8);
 #pragma unroll
     for (int r = 0; r < ROWS; r++) {
-        const f32x8 x = norm_and_turn<T, LPR>(a, __builtin_convertvector(raw[r], f32x8), (const T*)a.d_q_weight, inside, c8, angles);
-        if (inside && row0 + r < a.n_heads) store8((T*)a.d_q_out + ((int64_t)t * a.n_heads + row0 + r) * a.head_dim + c8, placed ? x : (f32x8)0.0f);
+        x[r] = turned(a, x[r], angles);
+        if (inside && row0 + r < a.n_heads) store8((T*)a.d_q_out + ((int64_t)t * a.n_heads + row0 + r) * a.head_dim + c8, placed ? x[r] : (f32x8)0.0f);
     }
 }
 
@@ -137,12 +140,12 @@ __device__ __forceinline__ void keys_values(const Args& g, uint32_t (&red)[2][4]
         for (int r = 0; r < EARLY; r++) angles[r] = angles_at(a, rows[r].pos, places[r] >= 0, c);
         f32x8 x[ITER];
         uint32_t most_k = 0, most_v = 0;
+        for (int r = 0; r < ITER; r++) x[r] = __builtin_convertvector(k[r], f32x8);
+        norm_rows<T, LPR, ITER>(a, x, (const T*)a.d_k_weight, inside, c8);
 #pragma unroll
         for (int r = 0; r < ITER; r++) {
-            x[r] = (f32x8)0.0f;
             if (!ballot(places[r] >= 0)) continue;
-            const Angles turn = EARLY ? angles[EARLY ? r : 0] : angles_at(a, rows[r].pos, places[r] >= 0, c);
-            x[r] = norm_and_turn<T, LPR>(a, __builtin_convertvector(k[r], f32x8), (const T*)a.d_k_weight, inside, c8, turn);
+            x[r] = turned(a, x[r], EARLY ? angles[EARLY ? r : 0] : angles_at(a, rows[r].pos, places[r] >= 0, c));
             const f32x8 y = __builtin_convertvector(v[r], f32x8);
             uint32_t m_k = largest_bits(x[r]), m_v = largest_bits(y);
             if (ballot(max(m_k, m_v) >= INFINITE)) {
@@ -220,8 +223,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope8_kernel(Args g) {
     else queries<T, LPR, 1>(g, blockIdx.x - (uint32_t)g.n.kv_blocks);
 }
 
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void qk_norm_rope8_queries_kernel(Args g) {
+    queries<T, LPR, 4>(g, blockIdx.x);
+}
+
 template <typename T, int LPR, int ITER, bool WIDE>
 hipError_t launch(const Args& g, hipStream_t st) {
+    if (g.n.apart) qk_norm_rope8_queries_kernel<T, LPR><<<(unsigned)g.n.q_blocks, 256, 0, st>>>(g);
     qk_norm_rope8_kernel<T, LPR, ITER, WIDE><<<(unsigned)(g.n.kv_blocks + (g.n.apart ? 0 : g.n.q_blocks)), 256, 0, st>>>(g);
     return hipGetLastError();
 }
@@ -248,13 +257,7 @@ hipError_t launch_dim(const Args& g, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_qk_norm_rope8(const jx_rope_args& a, const jx_kv_scales& s, hipStream_t st) {
-    const Rope8Grid n = rope8_grid(a, s.block);
-    if (n.apart) {
-        jx_rope_args queries = a;
-        queries.n_kv_heads = 0;
-        if (hipError_t e = launch_qk_norm_rope(queries, st); e != hipSuccess) return e;
-    }
-    const Args g = {a, s.d_k, s.d_v, log2_of(a.cache.page), log2_of(s.block), n};
+    const Args g = {a, s.d_k, s.d_v, log2_of(a.cache.page), log2_of(s.block), rope8_grid(a, s.block)};
     return a.dtype == JX_BF16 ? launch_dim<__bf16>(g, st) : launch_dim<_Float16>(g, st);
 }
 
