@@ -171,6 +171,57 @@ def test_store_of_many_tokens():
     check_store(c)
 
 
+@pytest.mark.parametrize("tokens,heads,kv,dim,rot,page,block", [(2000, 42, 2, 64, 32, 64, 32), (4500, 66, 3, 64, 64, 64, 64), (4500, 32, 8, 128, 128, 16, 16),
+                                                                (1200, 62, 1, 192, 16, 128, 64)])
+def test_store_of_very_many_heads(tokens, heads, kv, dim, rot, page, block):
+    """Four heads a group of lanes, and the queries in a launch of their own."""
+    check_store(store_case(BF, [(7, tokens - 100), (3, 99), (block, 1)], heads, kv, dim, rot, page, block, dim == 192, True, seed=tokens))
+
+
+def test_a_request_that_goes_back():
+    """Tokens are taken back and others take their places: what stands in front keeps its values, to the block's scale."""
+    kv, dim, page, block = 2, 64, 32, 16
+    k, v, q = (normal((40, n, dim), BF, i) for i, n in enumerate((kv, kv, 4)))
+    v[10:14] *= 64  # taken back again, but the scale remembers
+    c = dict(k_cache=None)
+    (kc, ks), (vc, vs) = (cache8(2, page, kv, dim, block, i) for i in (1, 2))
+
+    def put(first, rows):
+        at = torch.arange(first, first + len(rows))
+        c.update(q=q[rows], k=k[rows], v=v[rows], k_cache=kc, v_cache=vc, k_scale=ks, v_scale=vs, pos=at.tolist(), slot=at.tolist(), n_pos=64, block=block,
+                 page=page, pairs=False, cos=None, sin=None, wq=None, wk=None, eps=1e-6)
+        check_store(c, first)
+
+    put(0, list(range(14)))
+    before = plain8.stands_for(vc, vs).flatten(0, 1)[:10]
+    put(10, [20, 21])
+    put(12, [22])
+    after = plain8.stands_for(vc, vs).flatten(0, 1)[:10]
+    assert torch.equal(before, after)  # the scale has not grown
+    put(0, [30])                       # and the first place begins again
+    assert (vs.view(torch.uint8)[0, 0] < 130).all()
+
+
+@pytest.mark.parametrize("old", [0, 1, 200, 254, 255])
+def test_blocks_that_have_any_scale(old):
+    """A scale that no store has left, in front of new tokens: a larger one stays, 255 stays what it is."""
+    c = store_case(BF, [(5, 2), (16, 1), (8, 3)], 2, 2, 64, 0, 16, 8, False, False, seed=3)
+    for x in ("k_scale", "v_scale"):
+        c[x].view(torch.uint8).fill_(old)
+    if old < 254:
+        check_store(c)
+        return
+    before = flat(c["v_cache"], c["v_scale"])
+    run_store(c)
+    after = flat(c["v_cache"], c["v_scale"])
+    first = {s // 8 for s in c["slot"] if s % 8 == 0} - {s // 8 for s in (c["slot"][0],)}
+    for b in range(len(after[1])):
+        begun = b in first
+        assert (after[1][b] < 200).all() if begun else (after[1][b] == old).all()
+    held = [s for s in range(c["slot"][0] // 8 * 8, c["slot"][0])]
+    assert torch.equal(after[0][held].view(torch.uint8), before[0][held].view(torch.uint8))
+
+
 def test_rows_that_are_not_stored():
     c = store_case(BF, [(0, 3), (4, 2), (9, 30), (7, 1), (2, 1)], 4, 2, 64, 64, 16, 8, False, True, seed=5)
     n_slots = c["k_cache"].shape[0] * 16
