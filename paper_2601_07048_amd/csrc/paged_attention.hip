@@ -24,7 +24,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(PagedArgs g) {
     const Join j = g.joins[blockIdx.x];
     const int count = j.pieces ? j.count - (int)blockIdx.y * 32 : 0;
     if (count <= 0 || e0 >= d) return;
-    const int wide = count <= 4 ? 8 : count <= 8 ? 16 : count <= 16 ? 32 : 64, side = 64 / wide;  // lanes of a piece, pieces side by side
+    const int wide = count <= 8 ? 16 : count <= 16 ? 32 : 64, side = 64 / wide;  // lanes of a piece, pieces side by side
     const int row = lane & (wide / 2 - 1), half = lane / (wide / 2) & 1;
     const float* parts = g.part + blockIdx.y * part_floats(NB);
     const int to_s = part_at(row, e0 + half * 4), to_m = NB * 1024 + row;
