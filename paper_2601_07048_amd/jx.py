@@ -431,6 +431,15 @@ def _real(t, i, dtype, *shape):
     return _array(t, i, dtype, *shape)
 
 
+def _two(a, b, i, dtype, shape):
+    """Two such arrays of a kind."""
+    if a.requires_grad or b.requires_grad:
+        _no_gradient()
+    assert a.get_device() == b.get_device() == i and a.dtype is b.dtype is dtype and a.shape == b.shape == shape and a.is_contiguous() and \
+        b.is_contiguous(), (a.device, b.device, i, a.dtype, b.dtype, tuple(a.shape), tuple(b.shape), shape)
+    return a.data_ptr(), b.data_ptr()
+
+
 def _alike(a, b, sa, sb):
     """Whether two tensors are laid out alike; the stride of a dimension of one has no meaning."""
     return a.shape == b.shape and (sa == sb or all(n <= 1 or x == y for n, x, y in zip(a.shape, sa, sb)))
@@ -444,12 +453,22 @@ _SCALES = struct.Struct("2qi4x")
 assert (_ROPE.size, _ATTEND.size, _FOUND.size, _SCALES.size) == tuple(C.sizeof(x) for x in (RopeArgs, AttendArgs, FoundArgs, KvScales))
 
 
+def _two_alike(a, b, i, dtype):
+    """Keys and values laid out alike, of any strides: their pointers, and the strides."""
+    sa, sb = a.stride(), b.stride()
+    if a.requires_grad or b.requires_grad:
+        _no_gradient()
+    assert a.get_device() == b.get_device() == i and a.dtype is b.dtype is dtype and (sa[-1] == 1 or a.shape[-1] == 1) and _alike(a, b, sa, sb), (
+        a.device, b.device, i, a.dtype, b.dtype, tuple(a.shape), tuple(b.shape), sa, sb)
+    return a.data_ptr(), b.data_ptr(), sa
+
+
 def _kv_cache(k_cache, v_cache, i, dtype, head_dim):
     """The fields of a jx_kv_cache."""
     pages, page, _, d = k_cache.shape
-    ks, vs = k_cache.stride(), v_cache.stride()
-    assert d == head_dim and _alike(k_cache, v_cache, ks, vs)
-    return _rows(k_cache, i, dtype, ks), _rows(v_cache, i, dtype, vs), ks[0], ks[1], ks[2], page, pages
+    assert d == head_dim, (d, head_dim)
+    k, v, strides = _two_alike(k_cache, v_cache, i, dtype)
+    return k, v, strides[0], strides[1], strides[2], page, pages
 
 
 def _kv_scales(k_cache, k_scale, v_scale, i):
@@ -457,7 +476,7 @@ def _kv_scales(k_cache, k_scale, v_scale, i):
     pages, page, kv, _ = k_cache.shape
     blocks = k_scale.shape[1]
     assert blocks >= 1 and page % blocks == 0, (page, blocks)
-    return _SCALES.pack(_real(k_scale, i, _E8M0, pages, blocks, kv), _real(v_scale, i, _E8M0, pages, blocks, kv), page // blocks)
+    return _SCALES.pack(*_two(k_scale, v_scale, i, _E8M0, (pages, blocks, kv)), page // blocks)
 
 
 def kv_plan(lens, new, table, free, n_free, page, n_tokens, out=None) -> KvPlan:
@@ -506,8 +525,7 @@ def _rope(q, k, v, k_cache, v_cache, pos, slot, cos, sin, q_weight, k_weight, ep
     return out, i, _ROPE.pack(
         _HEAD_TYPES[dt], h, kv, d, 2 * half, interleaved, t, n_pos, _rows(q, i, dt, qs), _rows(k, i, dt, ks), _rows(v, i, dt, vs), qs[0], qs[1],
         ks[0], ks[1], vs[0], vs[1], _real(q_weight, i, dt, d) if q_weight is not None else 0,
-        _real(k_weight, i, dt, d) if k_weight is not None else 0, eps, _real(cos, i, _F32, n_pos, half) if half else 0,
-        _real(sin, i, _F32, n_pos, half) if half else 0, _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
+        _real(k_weight, i, dt, d) if k_weight is not None else 0, eps, *(_two(cos, sin, i, _F32, (n_pos, half)) if half else (0, 0)), _array(pos, i, _I32, t), _array(slot, i, _I64, t), out.data_ptr(),
         *_kv_cache(k_cache, v_cache, i, of_cache or dt, d))
 
 
@@ -587,10 +605,11 @@ def _found(q, keys, values, ids, scale, part, out, of_rows):
     dt, i = q.dtype, _gpu(q)
     of_rows = of_rows or dt
     o, lse, p_out, p_lse = _outputs(out, q, i, t, h, d)
-    qs, ks, vs = q.stride(), keys.stride(), values.stride()
-    assert kd == d and _alike(keys, values, ks, vs)
+    assert kd == d, (kd, d)
+    qs = q.stride()
+    pk, pv, ks = _two_alike(keys, values, i, of_rows)
     return o, lse, i, _FOUND.pack(
-        _HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt, qs), qs[0], qs[1], _rows(keys, i, of_rows, ks), _rows(values, i, of_rows, vs), ks[0], ks[1], n,
+        _HEAD_TYPES[dt], h, kv, d, t, _rows(q, i, dt, qs), qs[0], qs[1], pk, pv, ks[0], ks[1], n,
         _array(ids, i, _I32, t, h, k), k, scale, _real(part[0], i, dt, t, h, d) if part else 0,
         _real(part[1], i, _F32, t, h) if part else 0, p_out, p_lse)
 
@@ -610,7 +629,7 @@ def found_attention8(q, keys, values, k_scale, v_scale, ids, scale, block, part=
     n, kv, _ = keys.shape
     assert block >= 1, block
     blocks = -(-n // block)
-    _run(_lib.jx_found_attention8, i, a, _SCALES.pack(_real(k_scale, i, _E8M0, blocks, kv), _real(v_scale, i, _E8M0, blocks, kv), block))
+    _run(_lib.jx_found_attention8, i, a, _SCALES.pack(*_two(k_scale, v_scale, i, _E8M0, (blocks, kv)), block))
     return o, lse
 
 
