@@ -53,6 +53,10 @@ __device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {
 // The shares of a workgroup follow each other, so that tiles which they cut are put together in LDS, and only those which the
 // workgroup itself found begun or leaves open are left for join_kernel.  Few short tiles are a workgroup's own (g.own) and joined by it.
 // 64 requests of up to 8,192 keys, 8 key heads of 128 elements: 138 us, 5.0 TB/s; 4 of up to 131,072: 255 us, 5.5 TB/s; one of 777: 8.
+// Codes: a conversion makes two elements of two codes and their scale, exactly, so keys become operands as they come out of their registers and
+// values on their way into LDS, 32 of each in work and 32 on their way.  The bound is the same, half the bytes: 75 us, 4.7 TB/s; 125 us, 5.6 TB/s;
+// 8.1.  Twice as many on their way were slower (97 and not 83 us a call of the first), and so were workgroups of neighbouring heads in
+// place of wavefronts (96): what counts is that one CU reads what lies side by side.
 template <typename T, typename C, int NC, int RB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void paged_few_kernel(PagedArgs g) {
     constexpr int ROWS = RB * 16, KEYS = 32, CH = NC <= 2 ? 8 : NC <= 4 ? 16 : 32, PITCH = CH * 16, TILE = KEYS * PITCH;

@@ -39,6 +39,11 @@ __device__ __forceinline__ float both_halves_sum(float x) {
 // 952 us a call with the join's 15, or 1.0 PFLOP/s of the products, at a clock that falls to 1.7 GHz.  32 rows a wavefront, since 64 need more registers than there are
 // (slower by the spills); 8 wavefronts over the same keys halve what is read again.  256 elements have one wavefront on a SIMD:
 // 0.5 to 0.6 PFLOP/s; two there, with 32 of the 64 keys each, were not faster (their registers spill).
+// Codes are read into the LDS place of the rows that their wavefront makes of them, and become elements (exactly: the results are those of
+// 16-bit rows with the same values, bit for bit) beside the matrix instructions of the second half, at 90 vector and 8 LDS instructions a
+// wavefront and step on top of 220 and 48.  That chunk: 1,017 us a call, on a card where 16-bit keys and values take 932 (1,040 where eight lanes
+// wrote to four places of the banks); 9 chunks of up to 301 over 4,001 keys of 256 elements 65 (all conversions at the step's end 68), 33 of up
+// to 509 with a window of 1,024, 64 elements, 64.  A place of their own, read a tile earlier, cost more in registers than it saved in waits (68).
 template <typename T, int NB>
 struct Rows32 {
     static constexpr int CH = NB <= 2 ? 8 : NB <= 4 ? 16 : 32, PITCH = CH * 16;
@@ -243,7 +248,8 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
                         off = ((uint32_t)(l / CHM) * token_chunks + l % CHM) * 16;
                     }
                     if (d == R::CH * 8) load_lds16(from + row * 16 + off, to + at * R::PITCH);
-                    else if ((int)(lane_chunk ^ odd) * 16 < d * (int)sizeof(C))  // the other places are never written: see above
+                    else if constexpr (CODED<C>) load_lds16((int)lane_chunk * 16 < d ? from + row * 16 + off : (const char*)zero_chunk, to + at * R::PITCH);
+                    else if ((int)(lane_chunk ^ odd) * 8 < d)  // the other places are never written: see above
                         load_lds16(from + row * 16 + off, to + at * R::PITCH);
                 }
                 return;
@@ -258,20 +264,23 @@ __global__ __launch_bounds__(WAVES * 64, NB <= 4 ? 2 : 1) void paged_many_kernel
             }
         };
         // Lane i's block among the scales, of a key whose page is `id`
+        const uint32_t page_scales = (uint32_t)(g.scales.per_page * a.n_kv_heads);
         auto scale_at = [&](int id, int key) {
-            return ((long long)id * g.scales.per_page + ((key & page_mask) >> g.scales.shift)) * a.n_kv_heads + head;
+            return (uint64_t)(uint32_t)id * page_scales + (uint32_t)(((key & page_mask) >> g.scales.shift) * a.n_kv_heads + head);
         };
         // Codes that have arrived, as elements: a wavefront's rows are its own, and it has read all of a load's codes before it writes.  `byte`:
-        // lane i has the scale of the i-th row.  What is not there arrives as zeros, whose scale has to be a number.
+        // lane i has the scale of the i-th row.  What is not there arrives as zeros, whose scale has to be a number.  Of a lane's two chunks every
+        // second four lanes write the second first: eight lanes then write to as many places of a row's banks.
         auto raw = [&](int l, int i, lds_ptr to) {
             const u32x4 w = *(const __attribute__((address_space(3))) u32x4*)(to + (i * (THREADS / CHM) + turn * (64 / CHM)) * R::PITCH + l * 16);
-            return l % CHM * 16 < d ? w : (u32x4)0u;
+            const bool flip = l & 4;
+            return (u32x4){flip ? w[2] : w[0], flip ? w[3] : w[1], flip ? w[0] : w[2], flip ? w[1] : w[3]};
         };
         auto scale = [&](int l, int i, uint32_t byte, int ids) {
             return scale_bits((uint32_t)__shfl((int)(ids < 0 ? 127 : byte), i * (THREADS / CHM) + turn * (64 / CHM) + l / CHM, 64));
         };
         auto put = [&](int l, int i, int half, u32x4 w, float scale, lds_ptr to) {
-            put_codes<T, R::CH>(w[2 * half], w[2 * half + 1], scale, to, i * (THREADS / CHM) + turn * (64 / CHM) + l / CHM, l % CHM * 2 + half);
+            put_codes<T, R::CH>(w[2 * half], w[2 * half + 1], scale, to, i * (THREADS / CHM) + turn * (64 / CHM) + l / CHM, (l % CHM * 2 + (l >> 2 & 1)) ^ half);
         };
         auto expand = [&](uint32_t byte, int ids, lds_ptr to) {
             const int l = fresh_lane();

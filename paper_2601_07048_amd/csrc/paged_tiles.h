@@ -188,7 +188,7 @@ __device__ __forceinline__ int part_at(int r, int e) { return ((e >> 3) * 64 + r
 constexpr int part_floats(int nb) { return nb * 1024 + 64; }
 
 // ---- tiles shared out ---------------------------------------------------------------------------------------------------
-// All tiles of all key heads, UNIT keys of one a unit, are cut into equal shares, whatever the lengths of the requests are, one for each
+// All tiles of all key heads, UNIT keys of one a unit (32 where few rows meet codes, whose shares are shorter), are cut into equal shares, whatever the lengths of the requests are, one for each
 // workgroup (many rows) or wavefront (few); where a cut falls into a tile, its parts are joined afterwards.  Every workgroup finds its
 // shares for itself: from the first rows and lengths of all requests (8 bytes each) it counts the units of every slot and adds them up
 // in LDS.  With more than MAX_SLOTS slots there are tiles enough to fill the card, and each is a share: that holds for like lengths (1,000
@@ -272,8 +272,9 @@ struct Shares {
         per_head = __builtin_amdgcn_readfirstlane(cum[g.slots]);
         const uint32_t units = per_head * a.n_kv_heads;
         // With enough units each of `columns` neighbouring key heads has wavefronts of its own in every workgroup, which then reads the same
-        // tokens of all of them: rows of 128 bytes that lie side by side, about the same time (64 single tokens of up to 8,192 keys, 8 key
-        // heads of 128 codes: MEASURE us, each workgroup with a head MEASURE).
+        // tokens of all of them: rows of 128 bytes that lie side by side, about the same time.  64 single tokens of up to 8,192 keys, 8 key
+        // heads of 128 codes, a call: 83 us with four heads a workgroup, 86 with two, 92 with one; eight, 83, leave more to join (4 tokens of
+        // up to 131,072: 137 us with four, 143 with eight, 160 with one).
         columns = PER == 1 || units < (uint32_t)g.n_work ? 1 : g.columns;
         const int of_column = PER / columns, at = sub % of_column;
         column = sub / of_column;
