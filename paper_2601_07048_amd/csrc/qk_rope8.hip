@@ -1,5 +1,6 @@
 // Queries and keys of a step made ready for attention over a cache of 8 bits: RMS norm per head, rotation by position, keys and
 // values put into their blocks as e4m3 beside one power of two for each block and key head.
+#include <type_traits>
 #include "attend_walk.h"
 #include "codes8.h"
 #include "rope_row.h"
@@ -59,12 +60,9 @@ constexpr uint32_t INFINITE = 0x7F800000u;
 template <typename T>
 constexpr uint32_t MOST_BYTE = __is_same(T, _Float16) ? 127 + 15 - 7 : 127 + 127 - 7;
 
-// The largest |x| of eight elements, as bits: those of numbers are in order, and what is none is at least INFINITE
-__device__ __forceinline__ uint32_t largest_bits(f32x8 x) {
-    uint32_t m = 0;
-    for (int j = 0; j < 8; j++) m = max(m, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-    return m;
-}
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ uint32_t largest_number(f32x8 x) {
     uint32_t m = 0;
     for (int j = 0; j < 8; j++) {
@@ -72,6 +70,39 @@ __device__ __forceinline__ uint32_t largest_number(f32x8 x) {
         m = y < INFINITE ? max(m, y) : m;
     }
     return m;
+}
+
+// The largest |x| of eight elements that is a number, as the bits of a float32: those are in order.  Maxima pass over what is not a number; an
+// infinity has the eight looked at again.
+__device__ __forceinline__ uint32_t largest(f32x8 x) {
+    float m = 0.0f;
+    for (int j = 0; j < 8; j += 2) m = fmaxf(fmaxf(m, fabsf(x[j])), fabsf(x[j + 1]));
+    uint32_t bits = __float_as_uint(m);
+    if (ballot(bits >= INFINITE)) bits = largest_number(x);
+    return bits;
+}
+// ... of elements of type T, two at a time
+template <typename T>
+__device__ __forceinline__ uint32_t largest(typename Vec<T>::x8 x) {
+    const u32x4 w = __builtin_bit_cast(u32x4, x) & 0x7FFF7FFFu;
+    auto pair = [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    };
+    const uint32_t p = pair(pair(w[0], w[1]), pair(w[2], w[3])), m = max(p & 0xFFFFu, p >> 16);
+    if (ballot(m >= (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u))) return largest_number(__builtin_convertvector(x, f32x8));
+    if constexpr (__is_same(T, __bf16)) return m << 16;
+    else return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)m));
+}
+
+// The largest over a team of 8 to 64 lanes
+__device__ __forceinline__ uint32_t team_max(uint32_t v, int team) {
+    v = max(v, dpp_u32<0xB1>(v));
+    v = max(v, dpp_u32<0x4E>(v));
+    v = max(v, dpp_u32<0x141>(v));
+    if (team >= 16) v = max(v, dpp_u32<0x140>(v));
+    if (team >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+    if (team >= 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+    return v;
 }
 
 // The scale's byte, from the largest of a block's new rows and what the block has
@@ -86,6 +117,22 @@ __device__ __forceinline__ uint2 encode(f32x8 x, float scale, bool held) {
     if (held)
         for (int j = 0; j < 8; j++) x[j] = fabsf(x[j]) < INFINITY ? fminf(fmaxf(x[j], -LARGEST<T>), LARGEST<T>) : x[j];
     return make_uint2(codes_of(x[0], x[1], x[2], x[3], scale), codes_of(x[4], x[5], x[6], x[7], scale));
+}
+// ... elements of type T, two at a time
+template <typename T>
+__device__ __forceinline__ uint2 encode(typename Vec<T>::x8 x, float scale, bool held) {
+    if (held) return encode<T>(__builtin_convertvector(x, f32x8), scale, true);
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    auto two = [&](s16x2 w, T a, T b, auto high) {
+        const typename Vec<T>::x2 y = {a, b};
+        if constexpr (__is_same(T, __bf16)) return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, y, scale, high());
+        else return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, y, scale, high());
+    };
+    auto four = [&](int j) {
+        const s16x2 w = two(s16x2{0, 0}, x[j], x[j + 1], std::false_type());
+        return __builtin_bit_cast(uint32_t, two(w, x[j + 2], x[j + 3], std::true_type()));
+    };
+    return make_uint2(four(0), four(4));
 }
 
 // ITER: rows of a block / rows that the team holds at a time
@@ -148,19 +195,11 @@ __device__ __forceinline__ void keys_values(const Args& g, uint32_t (&red)[2][4]
         for (int r = 0; r < ITER; r++) {
             if (!ballot(places[r] >= 0)) continue;
             x[r] = turned(a, x[r], EARLY ? angles[EARLY ? r : 0] : angles_at(a, rows[r].pos, places[r] >= 0, c));
-            const f32x8 y = __builtin_convertvector(v[r], f32x8);
-            uint32_t m_k = largest_bits(x[r]), m_v = largest_bits(y);
-            if (ballot(max(m_k, m_v) >= INFINITE)) {
-                m_k = largest_number(x[r]);
-                m_v = largest_number(y);
-            }
-            most_k = max(most_k, m_k);
-            most_v = max(most_v, m_v);
+            most_k = max(most_k, largest(x[r]));
+            most_v = max(most_v, largest<T>(v[r]));
         }
-        for (int d = 1; d < min(team, 64); d *= 2) {
-            most_k = max(most_k, (uint32_t)__shfl_xor((int)most_k, d, 64));
-            most_v = max(most_v, (uint32_t)__shfl_xor((int)most_v, d, 64));
-        }
+        most_k = team_max(most_k, team);
+        most_v = team_max(most_v, team);
         if (WIDE) {
             if (lane == 0) {
                 red[0][tid >> 6] = most_k;
@@ -177,7 +216,7 @@ __device__ __forceinline__ void keys_values(const Args& g, uint32_t (&red)[2][4]
             if (places[r] >= 0) {
                 const int64_t row = places[r] * a.cache.token_stride + c8;
                 *(uint2*)(to_k + row) = encode<T>(x[r], scale_bits(byte_k), held);
-                *(uint2*)(to_v + row) = encode<T>(__builtin_convertvector(v[r], f32x8), scale_bits(byte_v), held);
+                *(uint2*)(to_v + row) = encode<T>(v[r], scale_bits(byte_v), held);
             }
         auto move = [&](uint8_t* cache, uint32_t from, uint32_t to) {
             if (first && from != to && inside)
