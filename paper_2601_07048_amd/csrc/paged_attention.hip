@@ -83,7 +83,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(PagedArgs g) {
 }
 
 struct Plan {
-    int rows;  // of a tile: 16, 32: few rows, 128, 256: many
+    int rows;  // of a tile: 16, 32: few rows, 64, 128, 256: many
     int slots, groups, n_work, columns, part_rows, own;
     int64_t joins, total;  // bytes before the joins, in all
 };
@@ -104,6 +104,11 @@ Plan make_plan(const jx_attend_args& a, bool coded) {
     if (pages && rows <= 16ll * a.n_req) p.rows = 16;
     else if (pages && little && rows <= 32ll * a.n_req) p.rows = 32;
     else p.rows = nb <= 4 && rows >= full * a.n_req ? 256 : 128;
+    // Of codes with a key head for each query head, 64 of up to 64 elements: a conversion serves few rows then, and what waits for it is hidden by
+    // more workgroups on a CU.  16 heads, 64 or 128 rows: 50 chunks of 1 to 400 tokens, 2,000 keys 67 or 76 us, 20 of 1 to 700, 6,000 keys 77 or
+    // 79, 60 prompts of 120 tokens 29.7 or 31.5; alike chunks of two such tiles the other way, 20 of 128 over 3,000 keys 102 or 85.  4 or 2 query
+    // heads to a key head, 64 chunks of up to 33 over 1,000 keys: 42 or 39.
+    if (coded && nb == 2 && a.n_heads == a.n_kv_heads && p.rows == 128 && rows <= 192ll * a.n_req) p.rows = 64;
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     // Few tiles of few rows and few keys (a table with little room, a short window): a workgroup a tile, which its wavefronts put
@@ -112,21 +117,21 @@ Plan make_plan(const jx_attend_args& a, bool coded) {
     // 11.1 or 12.5; 64 requests 18 or 16.  64 elements, 16 key heads, 16 requests of up to 1,024 keys: 10.9, shared out 18.4.
     const int64_t room = (int64_t)a.table_pages * a.cache.page, keys = a.window ? std::min<int64_t>(room, (int64_t)a.window + 16) : room;
     const int64_t tiles = (int64_t)p.slots * a.n_kv_heads, few = 1024 / (nb <= 2 ? 1 : nb);
-    p.own = p.rows < 128 && tiles <= 384 && keys <= few;
+    p.own = p.rows < 64 && tiles <= 384 && keys <= few;
     // Of codes also where there are tiles for most CUs: 8 key heads of 128, single tokens of 250 / 500 / 1,000 keys, a request 10.0 / 11.7 / 14.7 us
     // (shared out 10.4 / 10.5 / 11.9), 4 requests 10.3 / 12.2 / 15.1 (11.5 / 12.0 / 13.2), 16 requests 10.5 / 12.4 / 16.0 (13.7 / 18.9 / 21.2).
-    if (coded && p.rows < 128 && tiles <= 256) p.own = p.own || keys <= std::min(4 * few, tiles * 64 / nb);
+    if (coded && p.rows < 64 && tiles <= 256) p.own = p.own || keys <= std::min(4 * few, tiles * 64 / nb);
     const double units = ((double)a.table_pages * a.cache.page / (coded ? UNIT / 2 : UNIT) + 1) * p.slots * a.n_kv_heads;  // at most
     // as many shares as the card holds workgroups (many rows) or wavefronts (few) at a time
     if (p.slots && !p.own && p.slots <= MAX_SLOTS && units < 2e9) {
-        p.groups = 256 * (p.rows >= 128 ? MANY_PER_CU(nb, p.rows) : nb <= 2 ? 2 : 1);
-        p.n_work = p.rows >= 128 ? p.groups : p.groups * FEW_WAVES(nb);
+        p.groups = 256 * (p.rows >= 64 ? MANY_PER_CU(nb, p.rows) : nb <= 2 ? 2 : 1);
+        p.n_work = p.rows >= 64 ? p.groups : p.groups * FEW_WAVES(nb);
     }
     p.columns = 1;
-    if (coded && p.rows < 128)
+    if (coded && p.rows < 64)
         while (p.columns < 4 && a.n_kv_heads % (2 * p.columns) == 0) p.columns *= 2;
     auto up = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
-    p.joins = up(((int64_t)2 * p.groups * p.columns * p.part_rows + (p.rows >= 128 ? 0 : p.n_work)) * part_floats(nb) * 4);
+    p.joins = up(((int64_t)2 * p.groups * p.columns * p.part_rows + (p.rows >= 64 ? 0 : p.n_work)) * part_floats(nb) * 4);
     p.total = p.joins + up((int64_t)p.groups * p.columns * sizeof(Join));
     return p;
 }
@@ -160,7 +165,7 @@ hipError_t launch(const jx_attend_args& a, const jx_kv_scales* s, uint8_t* work,
     const Scales scales = s ? Scales{s->d_k, s->d_v, log2_of(s->block), a.cache.page / s->block} : Scales{};
     const PagedArgs g = {a, scales, log2_of(a.cache.page), group, mul, (uint32_t)bits - 1, near, p.slots, p.groups, p.n_work, p.columns, p.part_rows, p.own,
                          (float*)work, (Join*)(work + p.joins)};
-    hipError_t e = p.rows >= 128 ? (s ? launch_paged_many8 : launch_paged_many)(g, p.rows, st) : (s ? launch_paged_few8 : launch_paged_few)(g, p.rows, st);
+    hipError_t e = p.rows >= 64 ? (s ? launch_paged_many8 : launch_paged_many)(g, p.rows, st) : (s ? launch_paged_few8 : launch_paged_few)(g, p.rows, st);
     if (e != hipSuccess || !p.n_work) return e;
     if (a.dtype == JX_BF16) join_dim<__bf16>(g, st);
     else join_dim<_Float16>(g, st);

@@ -1,4 +1,4 @@
-// Paged attention of chunks: tiles of 128 or 256 rows.
+// Paged attention of chunks: tiles of 64, 128 or 256 rows.
 #pragma once
 #include "paged_tiles.h"
 
@@ -30,7 +30,7 @@ __device__ __forceinline__ float both_halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// ---- many rows: four or eight wavefronts of 32 rows each over the same keys ---------------------------------------------
+// ---- many rows: two, four or eight wavefronts of 32 rows each over the same keys ---------------------------------------------
 // S^T = K Q^T, 64 keys by 32 rows at a time, so that a lane holds 32 scores of one row (the other lane with that row, 32 further on,
 // the rest); then O^T += V^T P^T, where the scores' registers are already the second operand of the matrix instruction if the keys
 // of the first are taken in the same order.  The running maximum moves only when a row's scores rise by more than 2^8 over it:
@@ -39,11 +39,11 @@ __device__ __forceinline__ float both_halves_sum(float x) {
 // 952 us a call with the join's 15, or 1.0 PFLOP/s of the products, at a clock that falls to 1.7 GHz.  32 rows a wavefront, since 64 need more registers than there are
 // (slower by the spills); 8 wavefronts over the same keys halve what is read again.  256 elements have one wavefront on a SIMD:
 // 0.5 to 0.6 PFLOP/s; two there, with 32 of the 64 keys each, were not faster (their registers spill).
-// Codes are read into the LDS place of the rows that their wavefront makes of them, and become elements (exactly: the results are those of
-// 16-bit rows with the same values, bit for bit) beside the matrix instructions of the second half, at 90 vector and 8 LDS instructions a
+// Codes are read into the LDS place of the rows that their wavefront makes of them, and become elements (exactly: in tiles of the same height the
+// results are those of 16-bit rows with the same values, bit for bit) beside the matrix instructions of the second half, at 90 vector and 8 LDS instructions a
 // wavefront and step on top of 220 and 48.  That chunk: 1,017 us a call, on a card where 16-bit keys and values take 932 (1,040 where eight lanes
 // wrote to four places of the banks); 9 chunks of up to 301 over 4,001 keys of 256 elements 65 (all conversions at the step's end 68), 33 of up
-// to 509 with a window of 1,024, 64 elements, 64.  A place of their own, read a tile earlier, cost more in registers than it saved in waits (68).
+// to 509 with a window of 1,024, 64 elements, 59.  A place of their own, read a tile earlier, cost more in registers than it saved in waits (68).
 template <typename T, int NB>
 struct Rows32 {
     static constexpr int CH = NB <= 2 ? 8 : NB <= 4 ? 16 : 32, PITCH = CH * 16;
@@ -487,6 +487,8 @@ hipError_t launch_many(const PagedArgs& g, hipStream_t st) {
 template <typename T, typename C>
 hipError_t launch_many_dim(const PagedArgs& g, int rows, hipStream_t st) {
     const bool wide = rows == 256;
+    if constexpr (CODED<C>)
+        if (rows == 64) return launch_many<T, C, 2, 2>(g, st);
     switch (blocks_of(g.a.head_dim)) {
         case 2: return wide ? launch_many<T, C, 2, 8>(g, st) : launch_many<T, C, 2, 4>(g, st);
         case 3: return wide ? launch_many<T, C, 3, 8>(g, st) : launch_many<T, C, 3, 4>(g, st);

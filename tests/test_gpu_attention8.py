@@ -556,6 +556,39 @@ def test_long_chunks(dim, lens, new):
     p.check(window=100, rows=rows)
 
 
+@pytest.mark.parametrize("heads,dim,page,block", [(3, 64, 16, 16), (16, 64, 8, 4), (5, 48, 64, 64), (2, 16, 1, 1)])
+@pytest.mark.parametrize("window", [0, 33, 1024])
+def test_a_key_head_for_each_query_head(heads, dim, page, block, window):
+    lens, new = [2300, 1, 64, 65, 129, 0, 1900, 700], [250, 1, 64, 65, 63, 0, 1, 128]
+    rows = sorted({0, 1, 249, 250, 251, 314, 315, 379, 380, 442, 443, 444, 507, 508, 571})
+    for dtype in TYPES:
+        Paged8(dtype, heads, heads, dim, page, block, lens, new, seed=window + dim, pad=2).check(window, rows)
+
+
+def test_a_key_head_for_each_query_head_and_more_tiles_than_are_shared_out():
+    new = [17 + i % 2 * 60 for i in range(700)]
+    p = Paged8(F16, 2, 2, 64, 16, 8, [n + i % 5 for i, n in enumerate(new)], new, seed=9)
+    p.check(rows=list(range(0, sum(new), 997)))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("new", [[20], [100, 1]], ids=["one", "two"])
+def test_a_key_head_for_each_query_head_and_values_that_are_not_numbers(dtype, new):
+    lens = [1500, 70][:len(new)]
+    p = Paged8(dtype, 3, 3, 64, 16, 8, lens, new, seed=4)
+    at = 1500 - new[0] + 10
+    page, place = p.place(0, at)
+    p.v.view(torch.uint8)[page, place, 1, 3] = NAN_CODE
+    got = p.run()
+    assert got[0][10:new[0], 1, 3].isnan().all()
+    hidden = torch.ones_like(got[0], dtype=torch.bool)
+    hidden[10:new[0], 1, 3] = False
+    assert torch.isfinite(got[0][hidden]).all()
+    without = Paged8(dtype, 3, 3, 64, 16, 8, lens, new, seed=4)
+    got[0][~hidden] = without.check()[0][~hidden]
+    plain.check(got, without.want())
+
+
 def test_more_tiles_than_are_shared_out():
     rng = np.random.default_rng(3)
     lens = rng.integers(6, 80, 1100).tolist()
