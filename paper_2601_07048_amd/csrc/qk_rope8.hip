@@ -17,8 +17,9 @@ namespace {
 // values: LPR lanes a row as for the queries, rows held in registers from their one read to their store.  A team is as many lanes as
 // the block has rows for, up to a wavefront (with four rows a lane), and a workgroup for larger blocks, whose largest value goes through LDS.
 // With very many tokens the queries are a launch of their own, which has more wavefronts resident than these have registers for: 8,191
-// tokens, 32 + 16 heads of 128 elements, blocks of 32: 29.5 us for the queries, 4.5 TB/s read and written, 20.5 for keys and values, where the vector
-// instructions (700 a wavefront) and the chain share the time; 56 to 63 in one launch.  64 tokens 5.6 us, 1,111 with a scale each 9.
+// tokens, 32 + 16 heads of 128 elements, blocks of 32: 29.4 us for the queries, 4.5 TB/s read and written, 17.6 for keys and values, where the vector
+// instructions (590 a wavefront) and the chain share the time (20.3 where maxima and conversions of values take one element at a time); 56 to 63
+// in one launch.  64 tokens 5.6 us, 1,111 with a scale each 9.
 struct Args {
     jx_rope_args a;
     uint8_t *k_scale, *v_scale;

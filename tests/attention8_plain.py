@@ -77,7 +77,7 @@ def check_store(y, d, slot, found, before, after, block, dtype, exact, what=""):
         for c in range(y.shape[1]):
             x = y[t:t + n, c]
             size = torch.where(x.abs() < math.inf, x.abs(), torch.zeros_like(x)).clamp(max=most)
-            err = d[t:t + n, c]
+            err = torch.where(x.abs() < math.inf, d[t:t + n, c], torch.zeros_like(x))  # what is not a number has no part in E
             old = int(before[1][b, c]) if first else 0
             low, high = (max(math.floor(math.log2(float(s.max()))) + 120 if float(s.max()) > 0 else 1, 1, old) for s in (size - err, size + err))
             got = int(after[1][b, c])

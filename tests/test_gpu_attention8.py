@@ -252,6 +252,21 @@ def test_store_of_extreme_values(dtype):
     check_store(c)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("rot", [0, 16])
+def test_store_of_what_signals_that_it_is_not_a_number(dtype, rot):
+    """The largest value stands before such a one, after it, or is one of the same pair; the rest is smaller."""
+    c = store_case(dtype, [(0, 16), (16, 16)], 1, 1, 32, rot, 16, 4, False, False, seed=8, size=0.01)
+    bits = 0x7F81 if dtype is BF else 0x7C01
+    for name in ("k", "v"):
+        x = c[name]
+        for t in range(32):
+            x[t, 0, 16 + (t + 3) % 16] = 100.0
+            x.view(torch.int16)[t, 0, 16 + t % 16] = bits
+            x.view(torch.int16)[t, 0, 16 + (t + 1 + t // 16) % 16] = bits
+    check_store(c)
+
+
 def test_tokens_one_by_one_and_at_once():
     """The same tokens in chunks of different lengths: values that the codes stand for agree to their roundings, and a scale is that of
     the largest so far."""
@@ -563,6 +578,13 @@ def test_a_key_head_for_each_query_head(heads, dim, page, block, window):
     rows = sorted({0, 1, 249, 250, 251, 314, 315, 379, 380, 442, 443, 444, 507, 508, 571})
     for dtype in TYPES:
         Paged8(dtype, heads, heads, dim, page, block, lens, new, seed=window + dim, pad=2).check(window, rows)
+
+
+def test_a_key_head_for_each_query_head_and_many_requests():
+    rng = np.random.default_rng(12)
+    new = rng.integers(0, 40, 400).tolist() + [130]
+    p = Paged8(BF, 2, 2, 64, 16, 8, [n + int(rng.integers(0, 200)) for n in new], new, seed=12)
+    p.check(rows=list(range(0, sum(new), 331)))
 
 
 def test_a_key_head_for_each_query_head_and_more_tiles_than_are_shared_out():
