@@ -108,7 +108,13 @@ Plan make_plan(const jx_attend_args& a, bool coded) {
     // more workgroups on a CU.  16 heads, 64 or 128 rows: 50 chunks of 1 to 400 tokens, 2,000 keys 67 or 76 us, 20 of 1 to 700, 6,000 keys 77 or
     // 79, 60 prompts of 120 tokens 29.7 or 31.5; alike chunks of two such tiles the other way, 20 of 128 over 3,000 keys 102 or 85.  4 or 2 query
     // heads to a key head, 64 chunks of up to 33 over 1,000 keys: 42 or 39.
-    if (coded && nb == 2 && a.n_heads == a.n_kv_heads && p.rows == 128 && rows <= 192ll * a.n_req) p.rows = 64;
+    // Four workgroups of 64 rows have room on a CU while what each holds of the requests for the shares fits into the rest of its quarter of the LDS
+    // (with more tiles than are shared out it holds nothing). Beyond that three do, and a fourth of the shares runs after the others: requests
+    // of 1 to 79 tokens, up to 600 keys, 440 of them with 8 heads 108 us or, of 128 rows, 122, 460 of them with 4 heads 73 or 81; 480 of them with
+    // 8 heads 180 or 136, with 4 heads 117 or 81.
+    const int low = (int)(rows / 64 + a.n_req);
+    const bool four = low > MAX_SLOTS || (int64_t)shares_bytes(a.n_req, low) <= MANY_LDS / MANY_PER_CU(2, 64) - 4 * UNIT * 128;
+    if (coded && nb == 2 && a.n_heads == a.n_kv_heads && p.rows == 128 && rows <= 192ll * a.n_req && four) p.rows = 64;
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     // Few tiles of few rows and few keys (a table with little room, a short window): a workgroup a tile, which its wavefronts put

@@ -477,7 +477,7 @@ template <typename T, typename C, int NB, int WAVES>
 hipError_t launch_many(const PagedArgs& g, hipStream_t st) {
     constexpr int TILE = UNIT * Rows32<T, NB>::PITCH;
     const size_t lds = 4 * TILE + (g.n_work ? shares_bytes(g.a.n_req, g.slots) : 0);
-    hipError_t e = allow_lds<paged_many_kernel<T, C, NB, WAVES>>(160 * 1024);
+    hipError_t e = allow_lds<paged_many_kernel<T, C, NB, WAVES>>(MANY_LDS);
     if (e != hipSuccess) return e;
     const unsigned blocks = g.n_work ? g.groups : (unsigned)(g.slots * g.a.n_kv_heads);
     paged_many_kernel<T, C, NB, WAVES><<<blocks ? blocks : 256, WAVES * 64, lds, st>>>(g);

@@ -43,7 +43,8 @@ hipError_t launch_paged_few8(const PagedArgs& g, int rows, hipStream_t st);
 // wavefronts of a workgroup that takes few rows, by blocks of 32 elements: as many as have room for their values in LDS
 constexpr int FEW_WAVES(int nb) { return nb <= 4 ? 8 : 4; }
 
-// workgroups for many rows that a CU holds, by their registers
+// workgroups for many rows that a CU holds, by their registers, and its LDS
+constexpr int MANY_LDS = 160 * 1024;
 constexpr int MANY_PER_CU(int nb, int rows) { return nb <= 2 && rows == 64 ? 4 : nb <= 4 && rows == 128 ? 2 : 1; }
 
 // blocks of 32 elements that hold a head: those for which there is a kernel
