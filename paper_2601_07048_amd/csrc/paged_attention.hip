@@ -104,17 +104,19 @@ Plan make_plan(const jx_attend_args& a, bool coded) {
     if (pages && rows <= 16ll * a.n_req) p.rows = 16;
     else if (pages && little && rows <= 32ll * a.n_req) p.rows = 32;
     else p.rows = nb <= 4 && rows >= full * a.n_req ? 256 : 128;
-    // Of codes with a key head for each query head, 64 of up to 64 elements: a conversion serves few rows then, and what waits for it is hidden by
-    // more workgroups on a CU.  16 heads, 64 or 128 rows: 50 chunks of 1 to 400 tokens, 2,000 keys 67 or 76 us, 20 of 1 to 700, 6,000 keys 77 or
-    // 79, 60 prompts of 120 tokens 29.7 or 31.5; alike chunks of two such tiles the other way, 20 of 128 over 3,000 keys 102 or 85.  4 or 2 query
-    // heads to a key head, 64 chunks of up to 33 over 1,000 keys: 42 or 39.
+    // Of codes with a key head for each query head, 64 of up to 64 elements, where requests have as many on the mean: a conversion serves few rows then,
+    // and what waits for it is hidden by more workgroups on a CU.  Means of up to 64 rows, 4 to 16 heads, 12 to 100 requests: tiles of 128 take
+    // 1.07 of the time (0.76 to 1.39), alike chunks without a window 1.16 (60 of 64 tokens, 600 keys, 16 heads 46 or 59 us).  65 to 128: alike chunks 0.82 to 0.97
+    // (20 of 128 over 3,000 keys 92 or 76), mixes 0.96 to 1.03 (33 of 1 to 509, most of them short, over 500 to 8,000 keys with a window of 1,024: 69 or
+    // 77, without 128 or 139).  129 to 192: 0.94 to 1.01 (50 of 1 to 256 over 2,000 keys 131 or 122).  4 or 2 query heads to a key head, 64 chunks of up
+    // to 33 over 1,000 keys: 42 or 39.
     // Four workgroups of 64 rows have room on a CU while what each holds of the requests for the shares fits into the rest of its quarter of the LDS
     // (with more tiles than are shared out it holds nothing). Beyond that three do, and a fourth of the shares runs after the others: requests
     // of 1 to 79 tokens, up to 600 keys, 440 of them with 8 heads 108 us or, of 128 rows, 122, 460 of them with 4 heads 73 or 81; 480 of them with
     // 8 heads 180 or 136, with 4 heads 117 or 81.
     const int low = (int)(rows / 64 + a.n_req);
     const bool four = low > MAX_SLOTS || (int64_t)shares_bytes(a.n_req, low) <= MANY_LDS / MANY_PER_CU(2, 64) - 4 * UNIT * 128;
-    if (coded && nb == 2 && a.n_heads == a.n_kv_heads && p.rows == 128 && rows <= 192ll * a.n_req && four) p.rows = 64;
+    if (coded && nb == 2 && a.n_heads == a.n_kv_heads && p.rows == 128 && rows <= 64ll * a.n_req && four) p.rows = 64;
     p.part_rows = (p.rows + 31) / 32;
     p.slots = a.n_req ? (int)(rows / p.rows + a.n_req) : 0;
     // Few tiles of few rows and few keys (a table with little room, a short window): a workgroup a tile, which its wavefronts put

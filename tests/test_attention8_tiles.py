@@ -32,3 +32,11 @@ def test_tiles_of_64_rows_where_four_workgroups_have_room_on_a_cu(jx, n_req, mea
     shares = 8 * (n_req + 1) + 4 * (slots + 1) + 2 * slots
     if slots <= 1024:
         assert low_tiles(jx, n_req, n_req * mean) == (shares <= 8192), (slots, shares)
+
+
+@pytest.mark.parametrize("n_req", [1, 12, 33, 100, 300])
+def test_tiles_of_64_rows_where_requests_have_as_many_on_the_mean(jx, n_req):  # noqa: F811
+    """Alike chunks of 65 to 128 tokens are two tiles of 64 rows, of which the second reads all keys again, or one of 128."""
+    for tokens, want in ((33 * n_req, True), (64 * n_req, True), (64 * n_req + 1, False), (65 * n_req, False), (96 * n_req, False), (128 * n_req, False),
+                         (192 * n_req, False), (300 * n_req, False)):
+        assert low_tiles(jx, n_req, tokens) == want, tokens
