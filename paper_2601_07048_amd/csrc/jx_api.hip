@@ -394,7 +394,9 @@ int check_attend(const jx_attend_args* a, int chunk = 8) {
     if (int rc = check_table(a->d_table, a->table_pages, a->cache.page, a->n_req)) return rc;
     if (a->window < 0) return fail(JX_EINVAL, "window < 0");
     if (int rc = check_scale(a->scale)) return rc;
-    // 256 threads for each tile, of which there are at most n_tokens * n_heads / 128 < 2^22, and one for each request and key head
+    // Threads: of tiles of 128 rows 256 each, at most n_tokens * n_heads / 128 <= 2^22 and one for each request and key head; of 64 rows 128 each, at
+    // most 2^23 and those; of 256 rows 512 each, at most 2^21 and half as many again; of 32 and 16 rows 64 each, two for each request and key head.  All
+    // are less than 2^32.
     if ((int64_t)a->n_req * a->n_kv_heads > 1 << 23) return fail(JX_EINVAL, "n_req * n_kv_heads out of range");
     return JX_OK;
 }
