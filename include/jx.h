@@ -586,7 +586,9 @@ typedef struct {
  */
 int jx_qk_norm_rope8(const jx_rope_args* args, const jx_kv_scales* scales, void* stream);
 
-/* jx_paged_attention over such a cache; work_bytes as jx_paged_attention8_bytes says. */
+/* jx_paged_attention over such a cache; work_bytes as jx_paged_attention8_bytes says: none where each tile is one
+ * workgroup's, else up to 70 MB for heads of up to 128 elements and 102 MB for longer ones, however short the
+ * requests are (single tokens over 8 key heads of 128: 68 MB, 43 for 16 bits). */
 int64_t jx_paged_attention8_bytes(const jx_attend_args* args, const jx_kv_scales* scales);
 int jx_paged_attention8(const jx_attend_args* args, const jx_kv_scales* scales, void* d_work, int64_t work_bytes, void* stream);
 

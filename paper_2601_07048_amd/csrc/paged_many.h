@@ -43,7 +43,7 @@ __device__ __forceinline__ float both_halves_sum(float x) {
 // results are those of 16-bit rows with the same values, bit for bit) beside the matrix instructions of the second half, at 90 vector and 8 LDS instructions a
 // wavefront and step on top of 220 and 48.  That chunk: 1,017 us a call, on a card where 16-bit keys and values take 932 (1,040 where eight lanes
 // wrote to four places of the banks); 9 chunks of up to 301 over 4,001 keys of 256 elements 65 (all conversions at the step's end 68), 33 of up
-// to 509 with a window of 1,024, 64 elements, 59.  A place of their own, read a tile earlier, cost more in registers than it saved in waits (68).
+// to 509 with a window of 1,024, 64 elements, 64.  A place of their own, read a tile earlier, cost more in registers than it saved in waits (68).
 template <typename T, int NB>
 struct Rows32 {
     static constexpr int CH = NB <= 2 ? 8 : NB <= 4 ? 16 : 32, PITCH = CH * 16;

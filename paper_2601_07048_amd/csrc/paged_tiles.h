@@ -26,7 +26,7 @@ struct PagedArgs {
     int near;               // whether the rows that one load of a wavefront takes lie in one page, less than 2^31 bytes apart
     int slots;              // tiles at most
     int groups, n_work;     // workgroups, and shares of all tiles (1 or FEW_WAVES for each workgroup); 0 = a share a tile
-    int columns;            // of few rows: key heads that the wavefronts of a workgroup share between them, see Shares
+    int columns;            // of few rows: key heads that the wavefronts of a workgroup share between them, see Shares; each has parts of its own
     int part_rows;          // tiles' rows / 32
     int own;                // few rows, n_work = 0: whether a workgroup takes a tile, not a wavefront
     float* part;            // [2 groups columns][part_rows], and [n_work] of few rows inside workgroups: of 32 rows, over a part of a tile's
